@@ -344,6 +344,131 @@ int fuse_row_out_count(const fuse_expr *expr, const fuse_dense *Xd, const fuse_c
  * the first row that shows it; FUSE_EINVAL for NULL arrays. */
 int fuse_check_csr(const fuse_csr *X, void *stream);
 
+/* --------------------------------------------------------------------------
+ * Operators of a transformer block: what training and serving one needs beside the templates, of the same three
+ * kinds -- the norms around a block (row-wise), attention (an outer product that is never formed) and the norm of
+ * all gradients (a full aggregate over many inputs).  They are compiled with the library: no descriptor, no plan
+ * cache, nothing to warm up.  They differ from the calls above in two points:
+ *   - element types: fuse_dtype; sums, statistics and all arithmetic in between are fp64 for fp64 and fp32 for the others,
+ *     and every result is rounded once;
+ *   - workspaces are the caller's (device memory on 16 bytes, as many bytes as the *_bytes call says; its contents are
+ *     of no meaning before and after a call), so calls never allocate, and two graphs or two streams share nothing that the
+ *     caller does not give to both.
+ * All results are run-to-run deterministic.  `last kernel` names the call's main kernel.
+ */
+typedef enum { FUSE_F64 = 0, FUSE_F32 = 1, FUSE_BF16 = 2, FUSE_F16 = 3 } fuse_dtype;
+typedef enum { FUSE_NORM_RMS = 0, FUSE_NORM_LAYER = 1 } fuse_norm_kind;
+#define FUSE_GATE_NONE (-1)
+
+/* Norms before and after a block, with the block's gate and residual scale:
+ *     u = N_post(z), or z without post_weight
+ *     h = x + scale * gate o u                       (the residual stream; h = x without z)
+ *     y = N_pre(h)                                   (the next block's input; none without pre_weight)
+ *   FUSE_NORM_RMS   : N(v) = v / sqrt(mean(v^2) + eps) o weight
+ *   FUSE_NORM_LAYER : N(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) o weight + bias
+ * Matrices are rows x cols with unit column stride and a leading dimension in elements; weights and biases have cols
+ * values.  The gate is addressed like a side input: FUSE_SIDE_ROWVEC (cols values), FUSE_SIDE_COLVEC (rows values,
+ * gate_ld apart) or FUSE_SIDE_MATRIX.  cols <= 32768 (FUSE_EUNSUPPORTED beyond).  Rows of any alignment; 16-byte
+ * aligned rows of a multiple of 8 columns are faster. */
+typedef struct {
+    int32_t dtype;                          /* fuse_dtype of every array                              */
+    int32_t norm;                           /* fuse_norm_kind of both norms                           */
+    int64_t rows, cols;
+    double eps, scale;
+    const void *z;                          /* the block's result, or NULL: no block, only N_pre(x)   */
+    int64_t z_ld;
+    const void *post_weight, *post_bias;    /* norm after the block; NULL weight: none; NULL bias: 0  */
+    const void *pre_weight, *pre_bias;      /* norm before the next block, likewise                   */
+    int32_t gate_kind;                      /* FUSE_GATE_NONE or a fuse_side_kind (see above)         */
+    const void *gate;
+    int64_t gate_ld;
+} fuse_block;
+
+/* h (NULL without z, or where it is not wanted) may be x itself, with the same leading dimension; other overlaps of outputs with
+ * inputs are not allowed.  y goes with pre_weight. */
+int fuse_block_norm(const fuse_block *block, const void *x, int64_t x_ld, void *h, int64_t h_ld, void *y, int64_t y_ld,
+                    void *stream);
+
+/* Gradients that are not wanted are NULL.  dgate has the gate's shape (sums over the rows for FUSE_SIDE_ROWVEC, over a row for
+ * FUSE_SIDE_COLVEC, whose values are dgate_ld apart). */
+typedef struct {
+    void *dx;  int64_t dx_ld;
+    void *dz;  int64_t dz_ld;
+    void *dgate;  int64_t dgate_ld;
+    void *dpost_weight, *dpost_bias, *dpre_weight, *dpre_bias;
+} fuse_block_grads;
+
+/* The gradient of fuse_block_norm: dh and dy are the gradients of h and y (one of them may be NULL: zero), h is the forward
+ * call's (x where there is no z); statistics are taken from h and z again.  dx is the gradient of x.
+ *   fuse_block_norm_backward_bytes : bytes of the workspace (0 for a block that is refused). */
+size_t fuse_block_norm_backward_bytes(const fuse_block *block);
+int fuse_block_norm_backward(const fuse_block *block, const void *dh, int64_t dh_ld, const void *dy, int64_t dy_ld, const void *h,
+                             int64_t h_ld, const fuse_block_grads *grads, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention over packed sequences: for every sequence and query head
+ *     S = scale * Q t(K),  lse_i = log(sum_j exp(S_ij)),  out = exp(S - lse) V
+ * over the keys j that query i may see: all of the sequence's, or with `causal` those up to its own place, where the
+ * last query stands at the last key (j <= i + keys - queries).  A query that sees no key gets out = 0 and lse = -inf.  What
+ * masked keys and values hold, NaN and infinities included, has no influence.
+ * Query head h reads key head h / (heads / kv_heads).  q: q_tokens x heads x dim, k and v: k_tokens x kv_heads x dim, unit
+ * stride along dim; strides between tokens and between heads in elements, so parts of one projection can be passed as they
+ * are.  Every row on 16 bytes (pointers on 16 bytes, strides a multiple of 8), dim a multiple of 8 up to 128, dtype FUSE_BF16
+ * or FUSE_F16 (FUSE_EUNSUPPORTED otherwise).
+ * Sequence s has the queries q_offsets[s] .. q_offsets[s + 1] and the keys k_offsets[s] .. k_offsets[s + 1] (k_offsets NULL: the
+ * queries' offsets); with k_lengths only the first k_lengths[s] of those keys: a cache with room for more.  Offsets and lengths are
+ * device arrays of int32 or int64, non-decreasing from 0; they are not read on the host.  Values beyond
+ * the arrays are cut down to them: no access leaves the arrays, whatever the offsets say.  Rows that belong to no sequence are
+ * neither read nor written.
+ * S and sums are fp32; exp(S - max) and the gradient of S are rounded to dtype before their products with V, Q, K and dout, as the
+ * matrix units take them. */
+typedef struct {
+    int32_t dtype, heads, kv_heads, dim;
+    int32_t causal, offsets_are_64;
+    int64_t q_tokens, k_tokens, seqs;
+    const void *q_offsets, *k_offsets, *k_lengths;
+    double scale;                           /* > 0 */
+    const void *q, *k, *v;
+    int64_t q_token_ld, q_head_ld, k_token_ld, k_head_ld, v_token_ld, v_head_ld;
+} fuse_attn;
+
+/* lse: q_tokens x heads fp32, contiguous; NULL where it is not wanted.
+ *   fuse_attention_bytes : bytes of the workspace (0 where none is needed, and for a call that is refused). */
+size_t fuse_attention_bytes(const fuse_attn *attn);
+int fuse_attention(const fuse_attn *attn, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/* The gradients of q, k and v, given dout, the gradient of out, and the forward call's out and lse.  Keys that no query sees
+ * get 0.  Gradients of a shared key head are summed over its query heads. */
+typedef struct {
+    const void *dout, *out;  const float *lse;
+    int64_t dout_token_ld, dout_head_ld, out_token_ld, out_head_ld;
+    void *dq, *dk, *dv;
+    int64_t dq_token_ld, dq_head_ld, dk_token_ld, dk_head_ld, dv_token_ld, dv_head_ld;
+} fuse_attn_grads;
+size_t fuse_attention_backward_bytes(const fuse_attn *attn);
+int fuse_attention_backward(const fuse_attn *attn, const fuse_attn_grads *grads, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/* The norm of all gradients, and clipping by it.
+ *   fuse_grad_norm : norm[0] = sqrt(sum over the tensors of the sum of squares of their cells), one fp64 value
+ *   fuse_grad_clip : out = data * min(1, max_norm / (norm + eps)) for every tensor; out NULL: in place.  The norm is taken from
+ *                    norm_in[0] (a device value: for instance one that several processes have summed up), or with norm_in NULL
+ *                    it is computed as by fuse_grad_norm and left in norm_out[0].  Exactly one of the two is given.
+ * Tensors are contiguous arrays of any fuse_dtype, mixed freely, of any alignment of their type; empty ones are allowed.  Outputs
+ * may overlap neither each other nor the data of another tensor (FUSE_EINVAL).  The list is read during the call only (host memory).
+ * A norm that is NaN makes every result NaN; an infinite one makes finite cells 0.
+ *   fuse_grad_norm_bytes : bytes of the workspace of both (0 for a list that is refused). */
+typedef struct {
+    const void *data;
+    void *out;
+    int64_t count;
+    int32_t dtype;
+} fuse_tensor;
+size_t fuse_grad_norm_bytes(const fuse_tensor *tensors, int64_t n);
+int fuse_grad_norm(const fuse_tensor *tensors, int64_t n, double *norm, void *workspace, size_t workspace_bytes, void *stream);
+int fuse_grad_clip(const fuse_tensor *tensors, int64_t n, double max_norm, double eps, const double *norm_in, double *norm_out,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
 /* Message of the calling thread's last failed call ("" if none).  The pointer
  * stays valid until that thread's next libfuse call. */
 const char *fuse_last_error(void);

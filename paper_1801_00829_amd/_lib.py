@@ -32,6 +32,39 @@ class Expr(ctypes.Structure):
     _fields_ = [("toks", ctypes.POINTER(Tok)), ("ntoks", ctypes.c_int32)]
 
 
+class Block(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("eps", ctypes.c_double), ("scale", ctypes.c_double), ("z", ctypes.c_void_p), ("z_ld", ctypes.c_int64),
+                ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p),
+                ("gate_kind", ctypes.c_int32), ("gate", ctypes.c_void_p), ("gate_ld", ctypes.c_int64)]
+
+
+class BlockGrads(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dx_ld", ctypes.c_int64), ("dz", ctypes.c_void_p), ("dz_ld", ctypes.c_int64),
+                ("dgate", ctypes.c_void_p), ("dgate_ld", ctypes.c_int64), ("dpost_weight", ctypes.c_void_p),
+                ("dpost_bias", ctypes.c_void_p), ("dpre_weight", ctypes.c_void_p), ("dpre_bias", ctypes.c_void_p)]
+
+
+class Attn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "dim", "causal", "offsets_are_64")] + \
+               [(n, ctypes.c_int64) for n in ("q_tokens", "k_tokens", "seqs")] + \
+               [(n, ctypes.c_void_p) for n in ("q_offsets", "k_offsets", "k_lengths")] + [("scale", ctypes.c_double)] + \
+               [(n, ctypes.c_void_p) for n in ("q", "k", "v")] + \
+               [(n, ctypes.c_int64) for n in ("q_token_ld", "q_head_ld", "k_token_ld", "k_head_ld", "v_token_ld", "v_head_ld")]
+
+
+class AttnGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dout", "out", "lse")] + \
+               [(n, ctypes.c_int64) for n in ("dout_token_ld", "dout_head_ld", "out_token_ld", "out_head_ld")] + \
+               [(n, ctypes.c_void_p) for n in ("dq", "dk", "dv")] + \
+               [(n, ctypes.c_int64) for n in ("dq_token_ld", "dq_head_ld", "dk_token_ld", "dk_head_ld", "dv_token_ld", "dv_head_ld")]
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -83,6 +116,17 @@ def load():
               lib.fuse_cell, lib.fuse_magg, lib.fuse_magg_noalloc, lib.fuse_row, lib.fuse_outer, lib.fuse_prepare_cell,
               lib.fuse_prepare_magg, lib.fuse_prepare_row, lib.fuse_prepare_outer):
         f.restype = ci
+    i64, f64, size = ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
+    for name, args in (("fuse_block_norm", [P(Block), vp, i64, vp, i64, vp, i64, vp]),
+                       ("fuse_block_norm_backward", [P(Block), vp, i64, vp, i64, vp, i64, P(BlockGrads), vp, size, vp]),
+                       ("fuse_attention", [P(Attn), vp, i64, i64, vp, vp, size, vp]),
+                       ("fuse_attention_backward", [P(Attn), P(AttnGrads), vp, size, vp]),
+                       ("fuse_grad_norm", [P(Tensor), i64, vp, vp, size, vp]),
+                       ("fuse_grad_clip", [P(Tensor), i64, f64, f64, vp, vp, vp, size, vp])):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = args, ci
+    for name, args in (("fuse_block_norm_backward_bytes", [P(Block)]), ("fuse_attention_bytes", [P(Attn)]),
+                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_grad_norm_bytes", [P(Tensor), i64])):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = args, size
     lib.fuse_last_error.restype = ctypes.c_char_p
     lib.fuse_last_kernel.restype = ctypes.c_char_p
     lib.fuse_cache_stats.argtypes = [i64p, i64p, dp]

@@ -2,6 +2,7 @@
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -9,9 +10,10 @@ LIB = os.path.join(HERE, "libfuse.so")
 ARCH = "gfx950"
 
 HOST_SOURCES = ["libfuse.cpp", "expr.cpp", "runtime.cpp"]
-DEVICE_SOURCES = ["probe.hip", "check.hip", "transpose.hip", "noalloc.hip"]
+DEVICE_SOURCES = ["probe.hip", "check.hip", "transpose.hip", "noalloc.hip", "block_norm.hip", "grad_clip.hip",
+                  "attention.hip", "attention_grad.hip"]
 TEXT_DEPS = ["fuse_args.h", "skel_common.inc", "skel_cell.inc", "skel_row_dense.inc", "skel_row_csr.inc", "skel_row_csr_stream.inc", "skel_row_mfma.inc", "skel_row_mfma_wave.inc", "skel_row_mfma_pipe.inc", "skel_row_stored.inc",
-             "skel_outer.inc", "expr.h", "runtime.h"]
+             "skel_outer.inc", "expr.h", "runtime.h", "block_ops.h", "attention.h"]
 
 
 def _gen_args_text():
@@ -42,7 +44,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     _gen_args_text()
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     common = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result", "--offload-arch=" + ARCH]
-    objs = []
+    objs, cmds = [], []
     for s in HOST_SOURCES + DEVICE_SOURCES:
         obj = os.path.join(CSRC, os.path.splitext(s)[0] + ".o")
         if s.endswith(".hip"):
@@ -52,16 +54,20 @@ def build(force: bool = True, verbose: bool = False) -> str:
         else:
             # host-only translation units (no kernels inside); built as HIP for the runtime headers
             cmd = [hipcc] + common + ["-x", "hip", "-c", os.path.join(CSRC, s), "-o", obj]
+        cmds.append(cmd)
+        objs.append(obj)
+
+    def run(cmd):
         if verbose:
             print(" ".join(cmd))
         subprocess.run(cmd, check=True)
-        objs.append(obj)
+
+    with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+        list(pool.map(run, cmds))
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [hipcc, "-shared", "-fPIC", "--offload-arch=" + ARCH, "-o", tmp] + objs + \
           ["-L/opt/rocm/lib", "-lhiprtc", "-Wl,-rpath,/opt/rocm/lib"]
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.run(cmd, check=True)
+    run(cmd)
     os.replace(tmp, LIB)
     return LIB
 

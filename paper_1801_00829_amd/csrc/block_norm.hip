@@ -1,0 +1,750 @@
+// Norms before and after a block, fused with the block's gate and its residual scale (fuse_block_norm and its gradient).
+//
+//   u = N_post(z) or z;   h = x + scale * gate o u;   y = N_pre(h)
+//   N(v) = v r w, r = 1 / sqrt(mean(v^2) + eps)                        (rms)
+//   N(v) = (v - m) r w + b, r = 1 / sqrt(mean((v - m)^2) + eps)        (layer)
+//
+// Gradient, with n = v r (or (v - m) r) the normalised row, g = dy o w:
+//   dv = r (g - n mean(g n) [- mean(g)]),  dw = sum over the rows of dy o n,  db = sum over the rows of dy
+//   dx = dh + dv(h);  dgate = scale dx o u, summed over what the gate is broadcast over;  dz = dv(z) of scale dx o gate
+//
+// Bound by memory: a row is read once and stays in registers through all its statistics.  A group of G threads owns a row,
+// eight columns per thread and step, so a row of up to 8192 columns is one step; up to 32768 columns are four.  Statistics
+// of a layer norm are taken in two passes over the registers (mean, then squares of the differences): one pass of sums of
+// squares would lose the digits that a large mean has.
+#include "block_ops.h"
+
+namespace {
+
+using namespace fuse;
+
+constexpr int V = 8;                       // columns per thread and step
+constexpr int kMaxCols = 32768;            // 1024 threads x 4 steps
+constexpr int kMaxThreads = 1024;
+constexpr int kGradBlocks = 256;           // blocks of a gradient call: each leaves one partial row of every column sum
+
+struct Gate {
+    int kind;                              // 0: none, 1: per column, 2: per row, 3: per cell
+    const void *p;
+    long long ld;
+};
+
+struct FwdArgs {
+    const void *x, *z, *post_w, *post_b, *pre_w, *pre_b;
+    void *h, *y;
+    long long x_ld, z_ld, h_ld, y_ld, rows;
+    int cols, group;                       // group: threads per row
+    Gate gate;
+    double eps, scale;
+};
+
+struct BwdArgs {
+    const void *dh, *dy, *h, *z, *post_w, *post_b, *pre_w;
+    void *dx, *dz, *dgate, *partial;       // partial: [5][blocks][cols]
+    long long dh_ld, dy_ld, h_ld, z_ld, dx_ld, dz_ld, dgate_ld, rows;
+    int cols, group;
+    Gate gate;
+    double eps, scale;
+    int want_dpre_w, want_dpre_b, want_dpost_w, want_dpost_b;
+};
+
+struct SumArgs {
+    const void *partial;                   // [5][blocks][cols]
+    void *out[5];                          // NULL: not asked for
+    int blocks, cols;
+};
+
+// Column of element j of a thread's step k.  VEC: eight neighbours, loaded 16 bytes at a time (every row and pointer on
+// 16 bytes, columns a multiple of 8).  Else neighbouring threads take neighbouring columns, so that loads of single
+// elements still cover whole cache lines.
+template <bool VEC>
+__device__ __forceinline__ int col_of(int k, int j, int lane, int group)
+{
+    return VEC ? (k * group + lane) * V + j : (k * V + j) * group + lane;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_row(const T *__restrict__ p, int k, int lane, int group, int cols,
+                                         typename acc_of<T>::type (&v)[V])
+{
+    using A = typename acc_of<T>::type;
+    if (VEC) {
+        const int c = col_of<true>(k, 0, lane, group);
+        if (c < cols) {
+            struct alignas(16) Pack { T t[16 / sizeof(T)]; };
+            constexpr int N = 16 / sizeof(T);
+#pragma unroll
+            for (int i = 0; i < V / N; ++i) {
+                const Pack q = *reinterpret_cast<const Pack *>(p + c + i * N);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    v[i * N + j] = (A)q.t[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                v[j] = (A)0;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = col_of<false>(k, j, lane, group);
+            v[j] = c < cols ? (A)p[c] : (A)0;
+        }
+    }
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_row(T *__restrict__ p, int k, int lane, int group, int cols,
+                                          const typename acc_of<T>::type (&v)[V])
+{
+    if (VEC) {
+        const int c = col_of<true>(k, 0, lane, group);
+        if (c < cols) {
+            struct alignas(16) Pack { T t[16 / sizeof(T)]; };
+            constexpr int N = 16 / sizeof(T);
+#pragma unroll
+            for (int i = 0; i < V / N; ++i) {
+                Pack q;
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    q.t[j] = (T)v[i * N + j];
+                *reinterpret_cast<Pack *>(p + c + i * N) = q;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = col_of<false>(k, j, lane, group);
+            if (c < cols)
+                p[c] = (T)v[j];
+        }
+    }
+}
+
+// Sums over a row's group of threads of N values at once; every thread of the block calls it (rows behind the last one with
+// zeros), and two calls in a row take different `buf`s, so that one barrier per sum is enough.
+template <typename A, int N>
+__device__ __forceinline__ void group_sum(A (&v)[N], int group, A *buf)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] = wave_sum(v[i]);
+    if (group == 64)
+        return;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            buf[wave * N + i] = v[i];
+    __syncthreads();
+    const int per = group >> 6, first = wave / per * per;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] = buf[first * N + i];
+    for (int w = 1; w < per; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] += buf[(first + w) * N + i];
+}
+
+template <typename A> struct Stats {
+    A mean, r;
+};
+
+__device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
+__device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
+
+template <typename A, int K, bool VEC, bool LAYER>
+__device__ __forceinline__ Stats<A> stats_of(const A (&v)[K][V], int lane, int group, int cols, A eps, A *buf)
+{
+    Stats<A> st;
+    st.mean = (A)0;
+    A s[1] = {(A)0};
+    if (LAYER) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                s[0] += v[k][j];
+        group_sum<A, 1>(s, group, buf);
+        st.mean = s[0] / (A)cols;
+        s[0] = (A)0;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const A d = LAYER ? (col_of<VEC>(k, j, lane, group) < cols ? v[k][j] - st.mean : (A)0) : v[k][j];
+            s[0] += d * d;
+        }
+    group_sum<A, 1>(s, group, buf + 32);
+    st.r = inv_sqrt(s[0] / (A)cols + eps);
+    return st;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void gate_of(const Gate &gate, long long row, int k, int lane, int group, int cols,
+                                        typename acc_of<T>::type (&g)[V])
+{
+    using A = typename acc_of<T>::type;
+    const T *p = static_cast<const T *>(gate.p);
+    if (gate.kind == 1 || gate.kind == 3) {
+        load_row<T, VEC>(gate.kind == 1 ? p : p + row * gate.ld, k, lane, group, cols, g);
+    } else {
+        const A s = gate.kind == 2 ? (A)p[row * gate.ld] : (A)1;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            g[j] = s;
+    }
+}
+
+template <typename T, int K, bool VEC, bool LAYER>
+__global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const FwdArgs a)
+{
+    using A = typename acc_of<T>::type;
+    __shared__ A buf[2][64];               // one half per norm
+    const int group = a.group, per_block = blockDim.x / group, lane = threadIdx.x % group;
+    for (long long first = (long long)blockIdx.x * per_block; first < a.rows; first += (long long)gridDim.x * per_block) {
+        const long long row = first + threadIdx.x / group;
+        const bool in = row < a.rows;
+        A h[K][V], u[K][V];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (in) {
+                load_row<T, VEC>(static_cast<const T *>(a.x) + row * a.x_ld, k, lane, group, a.cols, h[k]);
+                if (a.z)
+                    load_row<T, VEC>(static_cast<const T *>(a.z) + row * a.z_ld, k, lane, group, a.cols, u[k]);
+            }
+            if (!in || !a.z)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    u[k][j] = (A)0;
+                    if (!in)
+                        h[k][j] = (A)0;
+                }
+        }
+        if (a.z) {
+            if (a.post_w) {
+                const Stats<A> st = stats_of<A, K, VEC, LAYER>(u, lane, group, a.cols, (A)a.eps, buf[0]);
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    A w[V], b[V];
+                    load_row<T, VEC>(static_cast<const T *>(a.post_w), k, lane, group, a.cols, w);
+                    if (LAYER && a.post_b)
+                        load_row<T, VEC>(static_cast<const T *>(a.post_b), k, lane, group, a.cols, b);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        u[k][j] = (u[k][j] - st.mean) * st.r * w[j];
+                        if (LAYER && a.post_b)
+                            u[k][j] += b[j];
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (in) {
+                    A g[V];
+                    gate_of<T, VEC>(a.gate, row, k, lane, group, a.cols, g);
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (col_of<VEC>(k, j, lane, group) < a.cols)
+                            h[k][j] += (A)a.scale * g[j] * u[k][j];
+                    if (a.h)
+                        store_row<T, VEC>(static_cast<T *>(a.h) + row * a.h_ld, k, lane, group, a.cols, h[k]);
+                }
+            }
+        }
+        if (a.y) {
+            // the norm is that of h before its rounding: it is in registers, and y is rounded once
+            const Stats<A> st = stats_of<A, K, VEC, LAYER>(h, lane, group, a.cols, (A)a.eps, buf[1]);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                A w[V], b[V], y[V];
+                load_row<T, VEC>(static_cast<const T *>(a.pre_w), k, lane, group, a.cols, w);
+                if (LAYER && a.pre_b)
+                    load_row<T, VEC>(static_cast<const T *>(a.pre_b), k, lane, group, a.cols, b);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    y[j] = (h[k][j] - st.mean) * st.r * w[j];
+                    if (LAYER && a.pre_b)
+                        y[j] += b[j];
+                }
+                if (in)
+                    store_row<T, VEC>(static_cast<T *>(a.y) + row * a.y_ld, k, lane, group, a.cols, y);
+            }
+        }
+        if (group > 64)
+            __syncthreads();               // the next rows' sums take the same buffers
+    }
+}
+
+// d = r (g - n mean(g n) [- mean(g)]) with g = dy o w, and the terms of the two column sums.
+template <typename T, int K, bool VEC, bool LAYER>
+__device__ __forceinline__ void norm_back(const typename acc_of<T>::type (&v)[K][V], typename acc_of<T>::type (&dy)[K][V],
+                                          const T *w_, bool in, int lane, int group, int cols, double eps,
+                                          typename acc_of<T>::type (&sum_w)[K][V], typename acc_of<T>::type (&sum_b)[LAYER ? K : 1][V],
+                                          typename acc_of<T>::type *buf)
+{
+    using A = typename acc_of<T>::type;
+    Stats<A> st = stats_of<A, K, VEC, LAYER>(v, lane, group, cols, (A)eps, buf);
+    if (!in)
+        st.r = (A)0;                       // a row behind the last one adds 0 to the column sums, eps = 0 included
+    A s[2] = {(A)0, (A)0};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        A w[V];
+        load_row<T, VEC>(w_, k, lane, group, cols, w);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const A n = (v[k][j] - st.mean) * st.r;
+            if (LAYER)
+                sum_b[LAYER ? k : 0][j] += dy[k][j];
+            sum_w[k][j] += dy[k][j] * n;
+            dy[k][j] *= w[j];
+            s[0] += dy[k][j] * n;          // (0 behind the row's end: dy is)
+            if (LAYER)
+                s[1] += dy[k][j];
+        }
+    }
+    group_sum<A, 2>(s, group, buf + 64);
+    s[0] /= (A)cols;
+    s[1] = LAYER ? s[1] / (A)cols : (A)0;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            dy[k][j] = st.r * (dy[k][j] - (v[k][j] - st.mean) * st.r * s[0] - s[1]);
+}
+
+// One block's rows of a column sum: the groups of a block are added in order, then the block's partial row is written.
+template <typename A, int K, bool VEC>
+__device__ __forceinline__ void leave_sum(const A (&v)[K][V], int lane, int group, int cols, A *out, A *add)
+{
+    const int per_block = blockDim.x / group, mine = threadIdx.x / group;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = col_of<VEC>(k, j, lane, group);
+            A s = v[k][j];
+            if (per_block > 1) {
+                add[threadIdx.x] = s;
+                __syncthreads();
+                if (mine == 0)
+                    for (int g = 1; g < per_block; ++g)
+                        s += add[g * group + lane];
+                __syncthreads();
+            }
+            if (mine == 0 && c < cols)
+                out[c] = s;
+        }
+}
+
+template <typename T, int K, bool VEC, bool LAYER>
+__global__ void __launch_bounds__(kMaxThreads) block_norm_grad_kernel(const BwdArgs a)
+{
+    using A = typename acc_of<T>::type;
+    __shared__ A buf[2][96];
+    __shared__ A add[kMaxThreads];
+    const int group = a.group, per_block = blockDim.x / group, lane = threadIdx.x % group;
+    A sum_pre[K][V] = {}, sum_post[K][V] = {}, sum_gate[K][V] = {};
+    A sum_pre_b[LAYER ? K : 1][V] = {}, sum_post_b[LAYER ? K : 1][V] = {};
+    for (long long first = (long long)blockIdx.x * per_block; first < a.rows; first += (long long)gridDim.x * per_block) {
+        const long long row = first + threadIdx.x / group;
+        const bool in = row < a.rows;
+        A v[K][V], d[K][V];                // h and dy, then z and dx
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (in && a.dy) {
+                load_row<T, VEC>(static_cast<const T *>(a.h) + row * a.h_ld, k, lane, group, a.cols, v[k]);
+                load_row<T, VEC>(static_cast<const T *>(a.dy) + row * a.dy_ld, k, lane, group, a.cols, d[k]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    v[k][j] = d[k][j] = (A)0;
+            }
+        }
+        if (a.dy)
+            norm_back<T, K, VEC, LAYER>(v, d, static_cast<const T *>(a.pre_w), in, lane, group, a.cols, a.eps, sum_pre, sum_pre_b, buf[0]);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (in && a.dh) {
+                A t[V];
+                load_row<T, VEC>(static_cast<const T *>(a.dh) + row * a.dh_ld, k, lane, group, a.cols, t);
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    d[k][j] += t[j];
+            }
+            if (in && a.dx)
+                store_row<T, VEC>(static_cast<T *>(a.dx) + row * a.dx_ld, k, lane, group, a.cols, d[k]);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                d[k][j] = in && col_of<VEC>(k, j, lane, group) < a.cols ? d[k][j] * (A)a.scale : (A)0;
+        }
+        if (a.z) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (in)
+                    load_row<T, VEC>(static_cast<const T *>(a.z) + row * a.z_ld, k, lane, group, a.cols, v[k]);
+                else
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        v[k][j] = (A)0;
+            }
+            if (a.gate.kind != 0) {
+                // dgate needs u, the gate's other factor; then d becomes the gradient of u
+                Stats<A> st;
+                st.mean = (A)0;
+                st.r = (A)1;
+                if (a.post_w)
+                    st = stats_of<A, K, VEC, LAYER>(v, lane, group, a.cols, (A)a.eps, buf[1]);
+                A s[1] = {(A)0};
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    A w[V], b[V], g[V], t[V];
+                    if (a.post_w)
+                        load_row<T, VEC>(static_cast<const T *>(a.post_w), k, lane, group, a.cols, w);
+                    if (LAYER && a.post_b)
+                        load_row<T, VEC>(static_cast<const T *>(a.post_b), k, lane, group, a.cols, b);
+                    if (in)
+                        gate_of<T, VEC>(a.gate, row, k, lane, group, a.cols, g);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        A u = (v[k][j] - st.mean) * st.r;
+                        if (a.post_w)
+                            u *= w[j];
+                        if (LAYER && a.post_b)
+                            u += b[j];
+                        t[j] = in ? d[k][j] * u : (A)0;
+                        s[0] += t[j];
+                        d[k][j] = in ? d[k][j] * g[j] : (A)0;
+                    }
+                    if (a.gate.kind == 1)
+#pragma unroll
+                        for (int j = 0; j < V; ++j)
+                            sum_gate[k][j] += t[j];
+                    else if (a.gate.kind == 3 && in && a.dgate)
+                        store_row<T, VEC>(static_cast<T *>(a.dgate) + row * a.dgate_ld, k, lane, group, a.cols, t);
+                }
+                if (a.gate.kind == 2 && a.dgate) {
+                    if (group > 64)
+                        __syncthreads();   // (the sums of the statistics have been read)
+                    group_sum<A, 1>(s, group, buf[1] + 64);
+                    if (in && lane == 0)
+                        static_cast<T *>(a.dgate)[row * a.dgate_ld] = (T)s[0];
+                }
+                if (group > 64)
+                    __syncthreads();
+            }
+            if (a.post_w)
+                norm_back<T, K, VEC, LAYER>(v, d, static_cast<const T *>(a.post_w), in, lane, group, a.cols, a.eps, sum_post, sum_post_b, buf[1]);
+            if (in && a.dz)
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+                    store_row<T, VEC>(static_cast<T *>(a.dz) + row * a.dz_ld, k, lane, group, a.cols, d[k]);
+        }
+        if (group > 64)
+            __syncthreads();
+    }
+    A *out = static_cast<A *>(a.partial) + (long long)blockIdx.x * a.cols;
+    const long long step = (long long)gridDim.x * a.cols;
+    if (a.want_dpre_w)
+        leave_sum<A, K, VEC>(sum_pre, lane, group, a.cols, out, add);
+    if (a.want_dpost_w)
+        leave_sum<A, K, VEC>(sum_post, lane, group, a.cols, out + step, add);
+    if (a.gate.kind == 1 && a.dgate)
+        leave_sum<A, K, VEC>(sum_gate, lane, group, a.cols, out + 2 * step, add);
+    if (LAYER) {
+        if (a.want_dpre_b)
+            leave_sum<A, LAYER ? K : 1, VEC>(sum_pre_b, lane, group, a.cols, out + 3 * step, add);
+        if (a.want_dpost_b)
+            leave_sum<A, LAYER ? K : 1, VEC>(sum_post_b, lane, group, a.cols, out + 4 * step, add);
+    }
+}
+
+// Column sums over the blocks' partial rows, in order: 64 columns of one sum per block, 16 slices of the partial rows.
+template <typename T>
+__global__ void __launch_bounds__(1024) block_norm_sums_kernel(const SumArgs a)
+{
+    using A = typename acc_of<T>::type;
+    __shared__ A part[16][64];
+    if (!a.out[blockIdx.y])
+        return;
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    const A *p = static_cast<const A *>(a.partial) + (long long)blockIdx.y * a.blocks * a.cols;
+    const int per = (a.blocks + 15) / 16, end = min(a.blocks, (slice + 1) * per);
+    A s = (A)0;
+    if (c < a.cols)
+        for (int b = slice * per; b < end; ++b)
+            s += p[(long long)b * a.cols + c];
+    part[slice][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (slice == 0 && c < a.cols) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i)
+            s += part[i][threadIdx.x & 63];
+        static_cast<T *>(a.out[blockIdx.y])[c] = (T)s;
+    }
+}
+
+// Threads per row: a wave or a power of two of them, so that a row of up to 8192 columns is one step.
+int group_for(int64_t cols)
+{
+    int g = 64;
+    while (g < kMaxThreads && (int64_t)g * V < cols)
+        g *= 2;
+    return g;
+}
+
+int steps_for(int64_t cols)
+{
+    const int64_t k = (cols + (int64_t)V * kMaxThreads - 1) / ((int64_t)V * kMaxThreads);
+    return k <= 1 ? 1 : k <= 2 ? 2 : 4;
+}
+
+int grad_blocks(const fuse_block *b)
+{
+    const int64_t per = kMaxThreads / group_for(b->cols), want = (b->rows + per - 1) / per;
+    return (int)(want < 1 ? 1 : want > kGradBlocks ? kGradBlocks : want);
+}
+
+template <typename T, int K, bool VEC>
+void launch_fwd_kvl(const FwdArgs &a, bool layer, unsigned blocks, unsigned threads, hipStream_t s)
+{
+    if (layer)
+        block_norm_kernel<T, K, VEC, true><<<blocks, threads, 0, s>>>(a);
+    else
+        block_norm_kernel<T, K, VEC, false><<<blocks, threads, 0, s>>>(a);
+}
+
+template <typename T, int K, bool VEC>
+void launch_bwd_kvl(const BwdArgs &a, bool layer, unsigned blocks, unsigned threads, hipStream_t s)
+{
+    if (layer)
+        block_norm_grad_kernel<T, K, VEC, true><<<blocks, threads, 0, s>>>(a);
+    else
+        block_norm_grad_kernel<T, K, VEC, false><<<blocks, threads, 0, s>>>(a);
+}
+
+#define FUSE_BY_STEPS(call, k, vec, ...)                                                                                   \
+    do {                                                                                                                  \
+        if (vec) {                                                                                                        \
+            if (k == 1) call<T, 1, true>(__VA_ARGS__); else if (k == 2) call<T, 2, true>(__VA_ARGS__); else call<T, 4, true>(__VA_ARGS__);     \
+        } else {                                                                                                          \
+            if (k == 1) call<T, 1, false>(__VA_ARGS__); else if (k == 2) call<T, 2, false>(__VA_ARGS__); else call<T, 4, false>(__VA_ARGS__);  \
+        }                                                                                                                 \
+    } while (0)
+
+template <typename T>
+void launch_fwd(const FwdArgs &a, bool layer, int k, bool vec, unsigned blocks, unsigned threads, hipStream_t s)
+{
+    FUSE_BY_STEPS(launch_fwd_kvl, k, vec, a, layer, blocks, threads, s);
+}
+
+template <typename T>
+void launch_bwd(const BwdArgs &a, bool layer, int k, bool vec, unsigned blocks, unsigned threads, hipStream_t s)
+{
+    FUSE_BY_STEPS(launch_bwd_kvl, k, vec, a, layer, blocks, threads, s);
+}
+
+template <typename T>
+void launch_sums(const SumArgs &a, hipStream_t s)
+{
+    block_norm_sums_kernel<T><<<dim3((a.cols + 63) / 64, 5), 1024, 0, s>>>(a);
+}
+
+#define FUSE_BY_DTYPE(dtype, call, ...)                                                                                    \
+    do {                                                                                                                  \
+        switch (dtype) {                                                                                                  \
+        case FUSE_F64: call<double>(__VA_ARGS__); break;                                                                  \
+        case FUSE_F32: call<float>(__VA_ARGS__); break;                                                                   \
+        case FUSE_BF16: call<__bf16>(__VA_ARGS__); break;                                                                 \
+        default: call<_Float16>(__VA_ARGS__); break;                                                                      \
+        }                                                                                                                 \
+    } while (0)
+
+int check_block(const fuse_block *b)
+{
+    if (!b)
+        return report(FUSE_EINVAL, "block is NULL");
+    if (!known_dtype(b->dtype))
+        return report(FUSE_EINVAL, "dtype is not a fuse_dtype");
+    if (b->norm != FUSE_NORM_RMS && b->norm != FUSE_NORM_LAYER)
+        return report(FUSE_EINVAL, "norm is not a fuse_norm_kind");
+    if (b->rows < 0 || b->cols < 1)
+        return report(FUSE_EINVAL, "rows must not be negative and cols must be positive");
+    if (b->cols > kMaxCols)
+        return report(FUSE_EUNSUPPORTED, "cols " + std::to_string(b->cols) + " > " + std::to_string(kMaxCols));
+    if (b->rows > (INT64_C(1) << 40))
+        return report(FUSE_EUNSUPPORTED, "rows " + std::to_string(b->rows) + " > 2^40");
+    if (!(b->eps >= 0.0))
+        return report(FUSE_EINVAL, "eps must not be negative");
+    if (!b->z && (b->post_weight || b->gate_kind != FUSE_GATE_NONE))
+        return report(FUSE_EINVAL, "a norm after the block and a gate need the block's result z");
+    if (b->norm == FUSE_NORM_RMS && (b->post_bias || b->pre_bias))
+        return report(FUSE_EINVAL, "a bias needs FUSE_NORM_LAYER");
+    if ((b->post_bias && !b->post_weight) || (b->pre_bias && !b->pre_weight))
+        return report(FUSE_EINVAL, "a bias needs its norm's weight");
+    if (b->gate_kind != FUSE_GATE_NONE && b->gate_kind != FUSE_SIDE_ROWVEC && b->gate_kind != FUSE_SIDE_COLVEC &&
+        b->gate_kind != FUSE_SIDE_MATRIX)
+        return report(FUSE_EINVAL, "gate_kind is none of FUSE_GATE_NONE, FUSE_SIDE_ROWVEC, FUSE_SIDE_COLVEC, FUSE_SIDE_MATRIX");
+    if (b->gate_kind != FUSE_GATE_NONE && !b->gate)
+        return report(FUSE_EINVAL, "gate is NULL");
+    return FUSE_OK;
+}
+
+int check_ld(const fuse_block *b, const void *p, int64_t ld, const char *what)
+{
+    return p && b->rows > 1 && ld < b->cols ? report(FUSE_ESHAPE, std::string(what) + ": leading dimension < cols") : FUSE_OK;
+}
+
+int gate_code(const fuse_block *b)
+{
+    return b->gate_kind == FUSE_GATE_NONE ? 0 : b->gate_kind == FUSE_SIDE_ROWVEC ? 1 : b->gate_kind == FUSE_SIDE_COLVEC ? 2 : 3;
+}
+
+// 16-byte loads: whole rows of vectors, every row of every matrix on 16 bytes.
+bool rows_on_16(const fuse_block *b, const void *p, int64_t ld)
+{
+    return !p || (on_16_bytes(p) && (b->rows <= 1 || (ld * (int64_t)dtype_size(b->dtype)) % 16 == 0));
+}
+
+bool block_on_16(const fuse_block *b)
+{
+    return b->cols % V == 0 && rows_on_16(b, b->z, b->z_ld) && on_16_bytes(b->post_weight) && on_16_bytes(b->post_bias) &&
+           on_16_bytes(b->pre_weight) && on_16_bytes(b->pre_bias) &&
+           (b->gate_kind == FUSE_GATE_NONE || b->gate_kind == FUSE_SIDE_COLVEC ||
+            (b->gate_kind == FUSE_SIDE_ROWVEC ? on_16_bytes(b->gate) : rows_on_16(b, b->gate, b->gate_ld)));
+}
+
+int check_gate_ld(const fuse_block *b)
+{
+    if (b->gate_kind == FUSE_SIDE_MATRIX)
+        return check_ld(b, b->gate, b->gate_ld, "gate");
+    if (b->gate_kind == FUSE_SIDE_COLVEC && b->rows > 1 && b->gate_ld < 1)
+        return report(FUSE_ESHAPE, "gate: stride < 1");
+    return FUSE_OK;
+}
+
+int norm_impl(const fuse_block *b, const void *x, int64_t x_ld, void *h, int64_t h_ld, void *y, int64_t y_ld, void *stream)
+{
+    report(FUSE_OK, "");
+    int rc = check_block(b);
+    if (rc)
+        return rc;
+    if (b->pre_weight ? !y : y != nullptr)
+        return report(FUSE_EINVAL, "y goes with pre_weight: both or neither");
+    if (!b->z && h)
+        return report(FUSE_EINVAL, "h needs the block's result z: without one it is x");
+    if (!h && !y)
+        return report(FUSE_EINVAL, "neither h nor y is asked for");
+    if (!x && b->rows > 0)
+        return report(FUSE_EINVAL, "x is NULL");
+    if ((rc = check_ld(b, x, x_ld, "x")) || (rc = check_ld(b, b->z, b->z_ld, "z")) || (rc = check_ld(b, h, h_ld, "h")) ||
+        (rc = check_ld(b, y, y_ld, "y")) || (rc = check_gate_ld(b)))
+        return rc;
+    if (b->rows == 0)
+        return FUSE_OK;
+    FwdArgs a;
+    a.x = x, a.z = b->z, a.post_w = b->post_weight, a.post_b = b->post_bias, a.pre_w = b->pre_weight, a.pre_b = b->pre_bias;
+    a.h = h, a.y = y;
+    a.x_ld = x_ld, a.z_ld = b->z_ld, a.h_ld = h_ld, a.y_ld = y_ld, a.rows = b->rows;
+    a.cols = (int)b->cols, a.group = group_for(b->cols);
+    a.gate = {gate_code(b), b->gate, b->gate_ld};
+    a.eps = b->eps, a.scale = b->scale;
+    const bool vec = block_on_16(b) && rows_on_16(b, x, x_ld) && rows_on_16(b, h, h_ld) && rows_on_16(b, y, y_ld);
+    const int threads = a.group < 256 ? 256 : a.group, per = threads / a.group;
+    const int64_t want = (b->rows + per - 1) / per;
+    const unsigned blocks = (unsigned)(want > 65536 ? 65536 : want);
+    FUSE_BY_DTYPE(b->dtype, launch_fwd, a, b->norm == FUSE_NORM_LAYER, steps_for(b->cols), vec, blocks, threads, (hipStream_t)stream);
+    return launched("block_norm_kernel");
+}
+
+size_t grad_bytes(const fuse_block *b)
+{
+    return (size_t)5 * grad_blocks(b) * b->cols * (b->dtype == FUSE_F64 ? 8 : 4);
+}
+
+int norm_grad_impl(const fuse_block *b, const void *dh, int64_t dh_ld, const void *dy, int64_t dy_ld, const void *h, int64_t h_ld,
+                   const fuse_block_grads *g, void *workspace, size_t workspace_bytes, void *stream)
+{
+    report(FUSE_OK, "");
+    int rc = check_block(b);
+    if (rc)
+        return rc;
+    if (!g)
+        return report(FUSE_EINVAL, "grads is NULL");
+    if (!dh && !dy)
+        return report(FUSE_EINVAL, "neither dh nor dy is given");
+    if (dy && !b->pre_weight)
+        return report(FUSE_EINVAL, "dy needs the norm that made y: pre_weight is NULL");
+    if (dy && !h && b->rows > 0)
+        return report(FUSE_EINVAL, "h is NULL");
+    if (!b->z && g->dz)
+        return report(FUSE_EINVAL, "dz needs z");
+    if ((g->dgate && b->gate_kind == FUSE_GATE_NONE) || (g->dpost_weight && !b->post_weight) || (g->dpre_weight && !b->pre_weight) ||
+        (g->dpost_bias && !b->post_bias) || (g->dpre_bias && !b->pre_bias))
+        return report(FUSE_EINVAL, "a gradient is asked for whose input is not given");
+    if ((rc = check_ld(b, dh, dh_ld, "dh")) || (rc = check_ld(b, dy, dy_ld, "dy")) || (rc = check_ld(b, h, h_ld, "h")) ||
+        (rc = check_ld(b, b->z, b->z_ld, "z")) || (rc = check_ld(b, g->dx, g->dx_ld, "dx")) || (rc = check_ld(b, g->dz, g->dz_ld, "dz")) ||
+        (rc = check_gate_ld(b)) ||
+        (rc = b->gate_kind == FUSE_SIDE_MATRIX ? check_ld(b, g->dgate, g->dgate_ld, "dgate") : FUSE_OK))
+        return rc;
+    if (b->gate_kind == FUSE_SIDE_COLVEC && g->dgate && b->rows > 1 && g->dgate_ld < 1)
+        return report(FUSE_ESHAPE, "dgate: stride < 1");
+    if (!workspace || !on_16_bytes(workspace) || workspace_bytes < grad_bytes(b))
+        return report(FUSE_EINVAL, "workspace: " + std::to_string(grad_bytes(b)) + " bytes on 16 are needed");
+    BwdArgs a;
+    a.dh = dh, a.dy = dy, a.h = h, a.z = b->z, a.post_w = b->post_weight, a.post_b = b->post_bias, a.pre_w = b->pre_weight;
+    a.dx = g->dx, a.dz = g->dz, a.dgate = g->dgate, a.partial = workspace;
+    a.dh_ld = dh_ld, a.dy_ld = dy_ld, a.h_ld = h_ld, a.z_ld = b->z_ld, a.dx_ld = g->dx_ld, a.dz_ld = g->dz_ld, a.dgate_ld = g->dgate_ld;
+    a.rows = b->rows, a.cols = (int)b->cols, a.group = group_for(b->cols);
+    a.gate = {gate_code(b), b->gate, b->gate_ld};
+    a.eps = b->eps, a.scale = b->scale;
+    // (without dy or rows the sums are those of nothing: zeros)
+    a.want_dpre_w = g->dpre_weight != nullptr, a.want_dpre_b = g->dpre_bias != nullptr;
+    a.want_dpost_w = g->dpost_weight != nullptr, a.want_dpost_b = g->dpost_bias != nullptr;
+    const bool vec = block_on_16(b) && rows_on_16(b, dh, dh_ld) && rows_on_16(b, dy, dy_ld) && rows_on_16(b, h, h_ld) &&
+                     rows_on_16(b, g->dx, g->dx_ld) && rows_on_16(b, g->dz, g->dz_ld) &&
+                     (b->gate_kind != FUSE_SIDE_MATRIX || rows_on_16(b, g->dgate, g->dgate_ld));
+    const int blocks = grad_blocks(b);
+    FUSE_BY_DTYPE(b->dtype, launch_bwd, a, b->norm == FUSE_NORM_LAYER, steps_for(b->cols), vec, blocks, kMaxThreads, (hipStream_t)stream);
+    rc = launched("block_norm_grad_kernel");
+    SumArgs sa;
+    sa.partial = workspace, sa.blocks = blocks, sa.cols = (int)b->cols;
+    sa.out[0] = g->dpre_weight, sa.out[1] = g->dpost_weight;
+    sa.out[2] = b->gate_kind == FUSE_SIDE_ROWVEC ? g->dgate : nullptr;
+    sa.out[3] = g->dpre_bias, sa.out[4] = g->dpost_bias;
+    if (rc || (!sa.out[0] && !sa.out[1] && !sa.out[2] && !sa.out[3] && !sa.out[4]))
+        return rc;
+    FUSE_BY_DTYPE(b->dtype, launch_sums, sa, (hipStream_t)stream);
+    rc = launched("block_norm_sums_kernel");
+    if (!rc)
+        set_last_kernel("block_norm_grad_kernel");
+    return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fuse_block_norm(const fuse_block *block, const void *x, int64_t x_ld, void *h, int64_t h_ld, void *y, int64_t y_ld, void *stream)
+{
+    return fuse::guard([&] { return norm_impl(block, x, x_ld, h, h_ld, y, y_ld, stream); });
+}
+
+size_t fuse_block_norm_backward_bytes(const fuse_block *block)
+{
+    if (!block || !known_dtype(block->dtype) || block->rows < 0 || block->cols < 1 || block->cols > kMaxCols)
+        return 0;
+    return grad_bytes(block);
+}
+
+int fuse_block_norm_backward(const fuse_block *block, const void *dh, int64_t dh_ld, const void *dy, int64_t dy_ld, const void *h,
+                             int64_t h_ld, const fuse_block_grads *grads, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return fuse::guard([&] { return norm_grad_impl(block, dh, dh_ld, dy, dy_ld, h, h_ld, grads, workspace, workspace_bytes, stream); });
+}
+
+}  // extern "C"

@@ -1920,6 +1920,14 @@ int guarded(F f)
 
 }  // namespace
 
+namespace fuse {
+
+int report(int code, const std::string &message) { return fail(code, message); }
+
+void set_last_kernel(const char *name) { g_last_kernel = name; }
+
+}  // namespace fuse
+
 // =============================================================================
 extern "C" {
 

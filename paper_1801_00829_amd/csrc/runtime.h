@@ -138,6 +138,10 @@ int transpose_launch(const void *rowptr, int rowptr_is64, const int *colidx, con
 // one (and not inside a group); 0: never.
 long long transpose_row_grain(long long m, long long n, long long nnz);
 
+// The calling thread's fuse_last_error() / fuse_last_kernel() (libfuse.cpp); report returns its code.
+int report(int code, const std::string &message);
+void set_last_kernel(const char *name);
+
 int iota_launch(double *dst, long long n, hipStream_t stream);     // dst[i] = (double)i
 int gather_launch(double *dst, const double *src, const double *perm, long long n, hipStream_t stream);   // dst[i] = src[perm[i]]
 
