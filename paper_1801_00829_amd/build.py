@@ -13,7 +13,7 @@ HOST_SOURCES = ["libfuse.cpp", "expr.cpp", "runtime.cpp"]
 DEVICE_SOURCES = ["probe.hip", "check.hip", "transpose.hip", "noalloc.hip", "block_norm.hip", "grad_clip.hip",
                   "attention.hip", "attention_grad.hip"]
 TEXT_DEPS = ["fuse_args.h", "skel_common.inc", "skel_cell.inc", "skel_row_dense.inc", "skel_row_csr.inc", "skel_row_csr_stream.inc", "skel_row_mfma.inc", "skel_row_mfma_wave.inc", "skel_row_mfma_pipe.inc", "skel_row_stored.inc",
-             "skel_outer.inc", "expr.h", "runtime.h", "block_ops.h", "attention.h"]
+             "skel_outer.inc", "expr.h", "runtime.h", "block_ops.h", "attention.h", "attention_tiles.h"]
 
 
 def _gen_args_text():

@@ -1,23 +1,291 @@
 // Attention over packed sequences, forward (fuse_attention).
-#include "attention.h"
+#include "attention_tiles.h"
 
 namespace {
 
 using namespace fuse;
 
-constexpr int kRows = 128;                 // rows per tile
+constexpr int kRows = 128;                 // rows per tile: 32 per wave
+constexpr int kKeys = 64;                  // keys per step
+constexpr int kMaxSplits = 64;
+constexpr float kLog2e = 1.44269504088896340736f;
 
-// A wave per row.
+// Where a call's keys are split: unnormalised results and statistics of every row and split.
+struct Parts {
+    float *o, *m, *l;                      // (row, split): dim values, maximum, sum
+    int splits;                            // 1: not split
+};
+
+__device__ __forceinline__ long long part_at(const AttnArgs &a, const Parts &p, long long token, int head, int split)
+{
+    return (token * a.heads + head) * p.splits + split;
+}
+
+// Running maximum and sum of a column, and its 32 new scores: rescales the result's DT tiles where the maximum has moved.
+//
+// The maximum that is subtracted is not always the largest score so far: it is moved only when a score is more than 2^8 times
+// larger, so that most steps leave the results as they are.  exp is then at most 2^8, well inside every type's range, and the
+// rounding of a 16 bit type is relative, so nothing is lost.
+template <int DT>
+__device__ __forceinline__ void follow_max(float top, float c, float &m, float &mc, float &l, f32x16 (&o)[DT])
+{
+    if (!__any((top - m) * c > 8.0f))
+        return;
+    const float next = fmaxf(m, top), to = next == -INFINITY ? 0.0f : next * c;
+    const float f = m == -INFINITY ? 0.0f : exp2f(mc - to);
+    m = next;
+    mc = to;
+    l *= f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+        o[d] *= f;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, const Parts parts)
+{
+    using L = Tile<DP>;
+    constexpr int kBytes = kKeys * L::kRowBytes;
+    __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][K, V]
+
+    const int kvh = blockIdx.x % a.kv_heads;
+    const unsigned rest = blockIdx.x / a.kv_heads;
+    const int split = rest % parts.splits;
+    const long long t = rest / parts.splits;
+    const int s = seq_of_tile(a, a.q_off, a.q_tokens, a.group, kRows, t);
+    const Seq x = seq_at(a, s);
+    const long long first = (t - first_tile(x.q0 * a.group, s, kRows)) * kRows, rows = (long long)x.nq * a.group;
+    if (first >= rows)
+        return;
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const long long r = first + wave * 32 + (lane & 31);
+    const bool in = r < rows;
+    const int place = (int)((in ? r : rows - 1) / a.group), head = kvh * a.group + (int)((in ? r : rows - 1) % a.group);
+    const int seen = seen_by(a, x, place);
+    const int seen_lo = __builtin_amdgcn_readfirstlane(seen);              // the wave's first row sees least, its last row most
+    const int seen_hi = first + wave * 32 < rows ? __builtin_amdgcn_readlane(seen, 31) : 0;
+
+    // this split's keys: begin .. end of those that any row of the tile sees
+    int begin = 0, end = seen_by(a, x, (int)((min(first + kRows, rows) - 1) / a.group));
+    if (parts.splits > 1) {
+        const int per = ((end + parts.splits - 1) / parts.splits + kKeys - 1) / kKeys * kKeys;
+        begin = min(split * per, end);
+        end = min(begin + per, end);
+    }
+
+    s16x8 q[L::kSteps];
+    operands<T, DP>(q, row_of<const T>(a.q, x.q0 + place, head), in, a.dim);
+    int row_at[L::kSteps], col_at[L::kCols][2];
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i)
+        row_at[i] = L::row_at(lane, i);
+#pragma unroll
+    for (int i = 0; i < L::kCols; ++i) {
+        col_at[i][0] = L::col_at(lane, i, 0);
+        col_at[i][1] = L::col_at(lane, i, 1);
+    }
+
+    f32x16 o[L::kCols];
+#pragma unroll
+    for (int d = 0; d < L::kCols; ++d)
+        o[d] = f32x16{};
+    float m = -INFINITY, mc = 0.0f, l = 0.0f;
+    const float c = a.scale * kLog2e;
+
+    const T *kbase = row_of<const T>(a.k, x.k0, kvh), *vbase = row_of<const T>(a.v, x.k0, kvh);
+    Stage<T, DP, kKeys> ks, vs;
+    if (begin < end) {
+        ks.load(kbase, a.k.token, begin, x.nk, a.dim);
+        vs.load(vbase, a.v.token, begin, x.nk, a.dim);
+        ks.store(lds[0][0]);
+        vs.store(lds[0][1]);
+    }
+    __syncthreads();
+    for (int j = begin, step = 0; j < end; j += kKeys, ++step) {
+        const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
+        const bool more = j + kKeys < end;
+        if (more) {
+            ks.load(kbase, a.k.token, j + kKeys, x.nk, a.dim);
+            vs.load(vbase, a.v.token, j + kKeys, x.nk, a.dim);
+        }
+        if (j < seen_hi) {
+            f32x16 p[2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                p[n] = f32x16{};
+#pragma unroll
+                for (int i = 0; i < L::kSteps; ++i)
+                    p[n] = product<T>(read_row(kt + n * 32 * L::kRowBytes, row_at[i]), q[i], p[n]);
+            }
+            if (j + kKeys > seen_lo) {
+                const int left = seen - j - 4 * h;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (n * 32 + 8 * (i / 4) + i % 4 >= left)
+                            p[n][i] = -INFINITY;
+            }
+            float top = p[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i)
+                top = fmaxf(top, p[i / 16][i % 16]);
+            follow_max<L::kCols>(both_max(top), c, m, mc, l, o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                p[i / 16][i % 16] = __builtin_amdgcn_exp2f(fmaf(p[i / 16][i % 16], c, -mc));
+                l += p[i / 16][i % 16];
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[i] = p[n / 2][n % 2 * 8 + i];
+                const s16x8 b = rounded<T>(w);
+#pragma unroll
+                for (int d = 0; d < L::kCols; ++d)
+                    o[d] = product<T>(read_col(vt + n * 16 * L::kRowBytes, col_at[d][0], col_at[d][1]), b, o[d]);
+            }
+        }
+        if (more) {
+            ks.store(lds[(step + 1) & 1][0]);
+            vs.store(lds[(step + 1) & 1][1]);
+        }
+        __syncthreads();
+    }
+
+    l = both_sum(l);
+    if (parts.splits > 1) {
+        if (in) {
+            const long long at = part_at(a, parts, x.q0 + place, head, split);
+            if (h == 0) {
+                parts.m[at] = m;
+                parts.l[at] = l;
+            }
+#pragma unroll
+            for (int d = 0; d < L::kCols; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (d * 32 + i * 8 + h * 4 < a.dim)
+                        *reinterpret_cast<f32x4 *>(parts.o + at * a.dim + d * 32 + i * 8 + h * 4) =
+                            f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
+        }
+        return;
+    }
+
+    // A masked score is a weight of 0, which the matrix units still multiply with the value: NaN where that is not finite.
+    // Rows with such a result are done again, key by key.
+    float worst = l - l;
+#pragma unroll
+    for (int d = 0; d < L::kCols; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            worst += o[d][i] - o[d][i];
+    const unsigned long long bad = __ballot(in && worst != 0.0f);
+    const float f = l > 0.0f ? 1.0f / l : 0.0f;
+    if (in && worst == 0.0f) {
+        T *out = row_of<T>(a.out, x.q0 + place, head);
+        typedef T t4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int d = 0; d < L::kCols; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (d * 32 + i * 8 + h * 4 < a.dim)
+                    *reinterpret_cast<t4 *>(out + d * 32 + i * 8 + h * 4) =
+                        t4{(T)(o[d][i * 4] * f), (T)(o[d][i * 4 + 1] * f), (T)(o[d][i * 4 + 2] * f), (T)(o[d][i * 4 + 3] * f)};
+        if (a.lse && h == 0)
+            a.lse[(x.q0 + place) * a.heads + head] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, logf(l));
+    }
+    for (unsigned todo = (unsigned)(bad | (bad >> 32)); todo; todo &= todo - 1) {
+        const long long again = first + wave * 32 + __builtin_ctz(todo);
+        attend_row<T>(a, x, (int)(again / a.group), kvh * a.group + (int)(again % a.group));
+    }
+}
+
+// Joins the splits of every row: a wave per row.
 template <typename T>
-__global__ void __launch_bounds__(256) attention_kernel(const AttnArgs a)
+__global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, const Parts parts, const int tile)
 {
     const int kvh = blockIdx.x % a.kv_heads;
     const long long t = blockIdx.x / a.kv_heads;
-    const int s = seq_of_tile(a, a.q_off, a.q_tokens, a.group, kRows, t);
+    const int s = seq_of_tile(a, a.q_off, a.q_tokens, a.group, tile, t);
     const Seq x = seq_at(a, s);
-    const long long first = (t - first_tile(x.q0 * a.group, s, kRows)) * kRows, end = min(first + kRows, (long long)x.nq * a.group);
-    for (long long r = first + (threadIdx.x >> 6); r < end; r += 4)
-        attend_row<T>(a, x, (int)(r / a.group), kvh * a.group + (int)(r % a.group));
+    const long long first = (t - first_tile(x.q0 * a.group, s, tile)) * tile, rows = min(first + tile, (long long)x.nq * a.group);
+    const int lane = threadIdx.x & 63;
+    for (long long r = first + (threadIdx.x >> 6); r < rows; r += 4) {
+        const int place = (int)(r / a.group), head = kvh * a.group + (int)(r % a.group);
+        const long long at = part_at(a, parts, x.q0 + place, head, 0);
+        const bool mine = lane < parts.splits;
+        const float m = mine ? parts.m[at + lane] : -INFINITY, l = mine ? parts.l[at + lane] : 0.0f;
+        float top = m;
+#pragma unroll
+        for (int i = 32; i > 0; i >>= 1)
+            top = fmaxf(top, __shfl_xor(top, i, 64));
+        const float w = l == 0.0f ? 0.0f : exp2f((m - top) * (a.scale * kLog2e));
+        const float sum = wave_sum(w * l);
+        float o0 = 0.0f, o1 = 0.0f;
+        for (int i = 0; i < parts.splits; ++i) {
+            const float f = __shfl(w, i, 64);
+            if (f == 0.0f)                 // nothing seen, or nothing that counts
+                continue;
+            const float *o = parts.o + (at + i) * a.dim;
+            if (lane < a.dim)
+                o0 = fmaf(f, o[lane], o0);
+            if (lane + 64 < a.dim)
+                o1 = fmaf(f, o[lane + 64], o1);
+        }
+        if (__any(o0 - o0 + (o1 - o1) + (sum - sum) != 0.0f)) {            // as above
+            attend_row<T>(a, x, place, head);
+            continue;
+        }
+        const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
+        T *out = row_of<T>(a.out, x.q0 + place, head);
+        if (lane < a.dim)
+            out[lane] = (T)(o0 * f);
+        if (lane + 64 < a.dim)
+            out[lane + 64] = (T)(o1 * f);
+        if (a.lse && lane == 0)
+            a.lse[(x.q0 + place) * a.heads + head] = top == -INFINITY ? -INFINITY : fmaf(top, a.scale, logf(sum));
+    }
+}
+
+long long tiles_of(const fuse_attn *f) { return first_tile(f->q_tokens * (f->heads / f->kv_heads), (int)f->seqs, kRows); }
+
+// Splits of the keys: as many as it takes to have two blocks for each of 256 compute units, of at least four steps each where all
+// sequences are equally long.
+int splits_of(const fuse_attn *f)
+{
+    const long long blocks = tiles_of(f) * f->kv_heads, keys = f->k_tokens / (f->seqs > 0 ? f->seqs : 1);
+    long long n = blocks > 0 ? 512 / blocks : 1;
+    n = n < keys / (4 * kKeys) ? n : keys / (4 * kKeys);
+    return (int)(n < 1 ? 1 : n > kMaxSplits ? kMaxSplits : n);
+}
+
+size_t parts_floats(const fuse_attn *f, int splits)
+{
+    return splits > 1 ? (size_t)f->q_tokens * f->heads * splits * (f->dim + 2) : 0;
+}
+
+template <typename T>
+int launch(const AttnArgs &a, const Parts &p, unsigned tiles, hipStream_t s)
+{
+    const unsigned blocks = tiles * a.kv_heads * p.splits;
+    if (a.dim <= 64)
+        attention_kernel<T, 64><<<blocks, 256, 0, s>>>(a, p);
+    else if (a.dim <= 96)
+        attention_kernel<T, 96><<<blocks, 256, 0, s>>>(a, p);
+    else
+        attention_kernel<T, 128><<<blocks, 256, 0, s>>>(a, p);
+    int rc = launched("attention_kernel");
+    if (rc || p.splits == 1)
+        return rc;
+    attention_join_kernel<T><<<tiles * a.kv_heads, 256, 0, s>>>(a, p, kRows);
+    rc = launched("attention_join_kernel");
+    if (!rc)
+        set_last_kernel("attention_kernel");
+    return rc;
 }
 
 int attention_impl(const fuse_attn *f, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse, void *workspace,
@@ -31,20 +299,21 @@ int attention_impl(const fuse_attn *f, void *out, int64_t out_token_ld, int64_t 
         return rc;
     if (reinterpret_cast<uintptr_t>(lse) % 4)
         return report(FUSE_EINVAL, "lse is not aligned to its type");
-    (void)workspace;
-    (void)workspace_bytes;
     if (f->q_tokens == 0 || f->seqs == 0)
         return FUSE_OK;
     AttnArgs a = attn_args(f);
     a.out = {out, out_token_ld, out_head_ld};
     a.lse = lse;
-    const long long tiles = first_tile(f->q_tokens * a.group, (int)f->seqs, kRows);
-    const unsigned blocks = (unsigned)(tiles * f->kv_heads);
-    if (f->dtype == FUSE_BF16)
-        attention_kernel<__bf16><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
-    else
-        attention_kernel<_Float16><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
-    return launched("attention_kernel");
+    Parts p = {};
+    p.splits = splits_of(f);
+    const size_t need = parts_floats(f, p.splits) * sizeof(float);
+    if (need && (!workspace || !on_16_bytes(workspace) || workspace_bytes < need))
+        return report(FUSE_EINVAL, "workspace: " + std::to_string(need) + " bytes on 16 are needed");
+    p.o = static_cast<float *>(workspace);
+    p.m = p.o + (size_t)f->q_tokens * f->heads * p.splits * f->dim;
+    p.l = p.m + (size_t)f->q_tokens * f->heads * p.splits;
+    const unsigned tiles = (unsigned)tiles_of(f);
+    return f->dtype == FUSE_BF16 ? launch<__bf16>(a, p, tiles, (hipStream_t)stream) : launch<_Float16>(a, p, tiles, (hipStream_t)stream);
 }
 
 }  // namespace
@@ -121,8 +390,9 @@ extern "C" {
 
 size_t fuse_attention_bytes(const fuse_attn *attn)
 {
-    (void)attn;
-    return 0;
+    if (fuse::check_attn(attn))
+        return 0;
+    return parts_floats(attn, splits_of(attn)) * sizeof(float);
 }
 
 int fuse_attention(const fuse_attn *attn, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse, void *workspace,

@@ -1,0 +1,148 @@
+// Matrix-unit pieces of the attention kernels: operands of the 32 x 32 x 16 product, tiles of rows in LDS.
+//
+// One product D += A B of a wave: A is 32 x 16, B is 16 x 32.  Lane l (half h = l / 32) holds row l % 32 of A and column l % 32 of
+// B, eight neighbours k = 8 h .. 8 h + 7 of each, and of D column l % 32, rows 8 (i / 4) + 4 h + i % 4 for i = 0 .. 15.
+//
+// All products are taken so that what a wave keeps (its 32 queries, or keys) are columns: S = A B with A from a tile in LDS
+// leaves every lane 16 scores of ONE column, so statistics of a column are sums over registers and one exchange between the
+// halves, and the scores, rounded, are the B operand of the next product as they lie: element e of half h stands for row
+// 4 h + e (e < 4) or 8 + 4 h + e - 4 of sixteen, and A is read in that order.  Its A is the transposed tile, eight rows of one
+// column, which the transposing LDS load gives four at a time.
+#pragma once
+#include "attention.h"
+
+namespace fuse {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> __device__ __forceinline__ f32x16 product(s16x8 a, s16x8 b, f32x16 c);
+template <> __device__ __forceinline__ f32x16 product<__bf16>(s16x8 a, s16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x16 product<_Float16>(s16x8 a, s16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Eight values, rounded, as a B operand.
+template <typename T> __device__ __forceinline__ s16x8 rounded(const float *v)
+{
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    t8 x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        x[i] = (T)v[i];
+    return __builtin_bit_cast(s16x8, x);
+}
+
+// The larger, or the sum, of a lane's value and that of the lane 32 away.
+__device__ __forceinline__ float both_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A tile of rows in LDS.  DP: dim rounded up to 64, 96 or 128 (0 behind dim).  Rows of 8 or 16 chunks of 16 bytes; chunk c of row r
+// lies in place c ^ turn(r), so that neither the loads of one chunk of 16 neighbouring rows (the A operand of S) nor those of four
+// neighbouring chunks of four rows (the transposing load) meet in a bank.
+template <int DP>
+struct Tile {
+    static constexpr int kChunks = DP == 64 ? 8 : 16;      // per row in LDS
+    static constexpr int kUsed = DP / 8;
+    static constexpr int kRowBytes = kChunks * 16;
+    static constexpr int kSteps = DP / 16;                 // products over dim
+    static constexpr int kCols = DP / 32;                  // 32 dims each
+
+    static __device__ __forceinline__ int turn(int r)
+    {
+        return kChunks == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    }
+
+    // Byte offsets of this lane's operands within a tile: rows l % 32 of the plain load, and of the transposing load (dims
+    // 32 dt .. of sixteen rows in the order above, first and second four).
+    static __device__ __forceinline__ int row_at(int lane, int step)
+    {
+        const int r = lane & 31, c = step * 2 + (lane >> 5);
+        return r * kRowBytes + ((c ^ turn(r)) << 4);
+    }
+    static __device__ __forceinline__ int col_at(int lane, int dt, int second)
+    {
+        const int i = lane & 15, r = second * 8 + (lane >> 5) * 4 + (i >> 2);
+        const int c = dt * 4 + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+        return r * kRowBytes + ((c ^ turn(r)) << 4) + (i & 1) * 8;
+    }
+};
+
+__device__ __forceinline__ s16x8 read_row(const char *lds, int at)
+{
+    return *reinterpret_cast<const s16x8 *>(lds + at);
+}
+
+__device__ __forceinline__ s16x8 read_col(const char *lds, int first, int second)
+{
+    using P = __attribute__((address_space(3))) s16x4 *;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uint32_t)(uintptr_t)(lds + first));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uint32_t)(uintptr_t)(lds + second));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// ROWS rows of a matrix on their way to LDS by 256 threads: loaded into registers while the tile before is worked on, written
+// when it is done.  Rows from `end` on are zeros and not read.
+template <typename T, int DP, int ROWS>
+struct Stage {
+    using L = Tile<DP>;
+    static constexpr int kPerPass = 256 / L::kChunks, kPasses = ROWS / kPerPass;
+    uint4 v[kPasses];
+
+    static __device__ __forceinline__ int chunk() { return threadIdx.x % L::kChunks; }
+    static __device__ __forceinline__ int row() { return threadIdx.x / L::kChunks; }
+
+    // `base`: row 0 of the matrix, `first`: the tile's first row
+    __device__ __forceinline__ void load(const T *base, long long ld, int first, int end, int dim)
+    {
+        const bool in = chunk() * 8 < dim;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+            const int r = first + row() + i * kPerPass;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (in && r < end)
+                v[i] = *reinterpret_cast<const uint4 *>(base + r * ld + chunk() * 8);
+        }
+    }
+
+    __device__ __forceinline__ void store(char *lds) const
+    {
+        if (chunk() < L::kUsed)
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+                const int r = row() + i * kPerPass;
+                *reinterpret_cast<uint4 *>(lds + r * L::kRowBytes + ((chunk() ^ L::turn(r)) << 4)) = v[i];
+            }
+    }
+};
+
+// A row of 16-bit values as the B operands of the products over dim: row_of the lane's column, 0 behind dim or without a row.
+template <typename T, int DP>
+__device__ __forceinline__ void operands(s16x8 (&b)[DP / 16], const T *row, bool in, int dim)
+{
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+        b[s] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        if (in && (s * 2 + h) * 8 < dim)
+            b[s] = *reinterpret_cast<const s16x8 *>(row + (s * 2 + h) * 8);
+    }
+}
+
+}  // namespace fuse
