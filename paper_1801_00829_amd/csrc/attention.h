@@ -23,6 +23,7 @@ struct AttnArgs {
     long long q_tokens, k_tokens;
     int seqs, heads, kv_heads, group, dim, causal, off64;
     float scale;
+    unsigned div_mul, div_shift;           // rows / group, see place_of
 };
 
 struct Seq {
@@ -77,6 +78,13 @@ __device__ __forceinline__ int seq_of_tile(const AttnArgs &a, const void *off, l
 __device__ __forceinline__ int seen_by(const AttnArgs &a, const Seq &x, int place)
 {
     return a.causal ? min(max(place + x.nk - x.nq + 1, 0), x.nk) : x.nk;
+}
+
+// r / group for r < 2^31, with mul = floor(2^(31 + n) / group) + 1 and 2^n the next power of two: mul * group lies between 2^(31 + n)
+// and 2^(31 + n) + 2^n, so the quotient of any 31 bits is exact.
+__device__ __forceinline__ int place_of(const AttnArgs &a, int r)
+{
+    return a.group == 1 ? r : (int)(__umulhi((unsigned)r, a.div_mul) >> a.div_shift);
 }
 
 // First place whose query sees key j (nq: none).

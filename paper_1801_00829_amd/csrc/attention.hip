@@ -381,6 +381,11 @@ AttnArgs attn_args(const fuse_attn *f)
     a.seqs = (int)f->seqs, a.heads = f->heads, a.kv_heads = f->kv_heads, a.group = f->heads / f->kv_heads, a.dim = f->dim;
     a.causal = f->causal != 0, a.off64 = f->offsets_are_64 != 0;
     a.scale = (float)f->scale;
+    int n = 0;
+    while ((1 << n) < a.group)
+        ++n;
+    a.div_mul = (unsigned)(((unsigned long long)1 << (31 + n)) / (unsigned)a.group + 1);
+    a.div_shift = n > 0 ? n - 1 : 0;
     return a;
 }
 

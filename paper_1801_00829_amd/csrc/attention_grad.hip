@@ -1,52 +1,328 @@
 // Attention over packed sequences, gradients (fuse_attention_backward).
-#include "attention.h"
+#include "attention_tiles.h"
 
 namespace {
 
 using namespace fuse;
 
-constexpr int kRows = 128;                 // rows, or keys, per tile
+constexpr int kRows = 128;                 // rows, or keys, per block: 32 per wave
+constexpr int kStep = 64;                  // keys, or rows, per step
+constexpr float kLog2e = 1.44269504088896340736f;
 
-// A wave per row; leaves delta for the keys' kernel.
-template <typename T>
-__global__ void __launch_bounds__(256) attention_query_grad_kernel(const AttnArgs a)
+// A wave's 32 columns of 32 DT dims, rounded, to rows of a matrix.
+template <typename T, int DT>
+__device__ __forceinline__ void write_columns(const f32x16 (&o)[DT], float f, T *row, int h, int dim)
 {
+    typedef T t4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d * 32 + i * 8 + h * 4 < dim)
+                *reinterpret_cast<t4 *>(row + d * 32 + i * 8 + h * 4) =
+                    t4{(T)(o[d][i * 4] * f), (T)(o[d][i * 4 + 1] * f), (T)(o[d][i * 4 + 2] * f), (T)(o[d][i * 4 + 3] * f)};
+}
+
+// 0 where all of them are finite, NaN otherwise
+template <int DT>
+__device__ __forceinline__ float not_finite(const f32x16 (&o)[DT])
+{
+    float w = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            w += o[d][i] - o[d][i];
+    return w;
+}
+
+// Gradient of the queries, and delta for the keys' kernel.  As the forward kernel: 32 rows per wave as columns, keys and values
+// step by step through LDS; the keys are read twice, as rows for S and transposed for t(K) t(dS).
+template <typename T, int DP>
+__global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const AttnArgs a)
+{
+    using L = Tile<DP>;
+    constexpr int kBytes = kStep * L::kRowBytes;
+    __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][K, V]
+
     const int kvh = blockIdx.x % a.kv_heads;
     const long long t = blockIdx.x / a.kv_heads;
     const int s = seq_of_tile(a, a.q_off, a.q_tokens, a.group, kRows, t);
     const Seq x = seq_at(a, s);
-    const long long first = (t - first_tile(x.q0 * a.group, s, kRows)) * kRows, end = min(first + kRows, (long long)x.nq * a.group);
-    for (long long r = first + (threadIdx.x >> 6); r < end; r += 4)
-        query_grad_row<T>(a, x, (int)(r / a.group), kvh * a.group + (int)(r % a.group));
+    const int first = (int)((t - first_tile(x.q0 * a.group, s, kRows)) * kRows), rows = x.nq * a.group;
+    if (first >= rows)
+        return;
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int r = first + wave * 32 + (lane & 31);
+    const bool in = r < rows;
+    const int place = place_of(a, in ? r : rows - 1), head = kvh * a.group + (in ? r : rows - 1) - place * a.group;
+    const int seen = seen_by(a, x, place);
+    const int seen_lo = __builtin_amdgcn_readfirstlane(seen);
+    const int seen_hi = first + wave * 32 < rows ? __builtin_amdgcn_readlane(seen, 31) : 0;
+    const int end = seen_by(a, x, place_of(a, min(first + kRows, rows) - 1));
+
+    s16x8 q[L::kSteps], g[L::kSteps];
+    operands<T, DP>(q, row_of<const T>(a.q, x.q0 + place, head), in, a.dim);
+    operands<T, DP>(g, row_of<const T>(a.dout, x.q0 + place, head), in, a.dim);
+    float delta = 0.0f, lse2 = 0.0f;
+    {
+        typedef T t8 __attribute__((ext_vector_type(8)));
+        s16x8 o[L::kSteps];
+        operands<T, DP>(o, row_of<const T>(a.out, x.q0 + place, head), in, a.dim);
+#pragma unroll
+        for (int i = 0; i < L::kSteps; ++i) {
+            const t8 u = __builtin_bit_cast(t8, g[i]), v = __builtin_bit_cast(t8, o[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                delta = fmaf((float)u[e], (float)v[e], delta);
+        }
+        delta = both_sum(delta);
+    }
+    if (in) {
+        const long long at = (x.q0 + place) * a.heads + head;
+        lse2 = a.lse[at] * kLog2e;
+        if (h == 0)
+            a.delta[at] = delta;
+    }
+
+    int row_at[L::kSteps], col_at[L::kCols][2];
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i)
+        row_at[i] = L::row_at(lane, i);
+#pragma unroll
+    for (int i = 0; i < L::kCols; ++i) {
+        col_at[i][0] = L::col_at(lane, i, 0);
+        col_at[i][1] = L::col_at(lane, i, 1);
+    }
+    f32x16 o[L::kCols];
+#pragma unroll
+    for (int d = 0; d < L::kCols; ++d)
+        o[d] = f32x16{};
+    const float c = a.scale * kLog2e;
+
+    const T *kbase = row_of<const T>(a.k, x.k0, kvh), *vbase = row_of<const T>(a.v, x.k0, kvh);
+    Stage<T, DP, kStep> ks, vs;
+    if (end > 0) {
+        ks.load(kbase, a.k.token, 0, x.nk, a.dim);
+        vs.load(vbase, a.v.token, 0, x.nk, a.dim);
+        ks.store(lds[0][0]);
+        vs.store(lds[0][1]);
+    }
+    __syncthreads();
+    for (int j = 0, step = 0; j < end; j += kStep, ++step) {
+        const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
+        const bool more = j + kStep < end;
+        if (more) {
+            ks.load(kbase, a.k.token, j + kStep, x.nk, a.dim);
+            vs.load(vbase, a.v.token, j + kStep, x.nk, a.dim);
+        }
+        if (j < seen_hi) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                f32x16 p = {}, dp = {};
+#pragma unroll
+                for (int i = 0; i < L::kSteps; ++i) {
+                    p = product<T>(read_row(kt + n * 32 * L::kRowBytes, row_at[i]), q[i], p);
+                    dp = product<T>(read_row(vt + n * 32 * L::kRowBytes, row_at[i]), g[i], dp);
+                }
+                float w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    w[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -lse2)) * (dp[i] - delta);
+                if (j + kStep > seen_lo) {
+                    const int left = seen - j - n * 32 - 4 * h;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (8 * (i / 4) + i % 4 >= left)
+                            w[i] = 0.0f;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const s16x8 b = rounded<T>(w + u * 8);
+#pragma unroll
+                    for (int d = 0; d < L::kCols; ++d)
+                        o[d] = product<T>(read_col(kt + (n * 2 + u) * 16 * L::kRowBytes, col_at[d][0], col_at[d][1]), b, o[d]);
+                }
+            }
+        }
+        if (more) {
+            ks.store(lds[(step + 1) & 1][0]);
+            vs.store(lds[(step + 1) & 1][1]);
+        }
+        __syncthreads();
+    }
+
+    // as in the forward kernel: 0 for a masked key, times a key that is not finite
+    const float worst = not_finite(o);
+    const unsigned long long bad = __ballot(in && worst != 0.0f);
+    if (in && worst == 0.0f)
+        write_columns<T>(o, a.scale, row_of<T>(a.dq, x.q0 + place, head), h, a.dim);
+    for (unsigned todo = (unsigned)(bad | (bad >> 32)); todo; todo &= todo - 1) {
+        const int again = first + wave * 32 + __builtin_ctz(todo), p = place_of(a, again);
+        query_grad_row<T>(a, x, p, kvh * a.group + again - p * a.group);
+    }
 }
 
-// A wave per key.
-template <typename T>
-__global__ void __launch_bounds__(256) attention_key_grad_kernel(const AttnArgs a)
+// Gradients of the keys and values: 32 keys per wave as columns, the rows that see them step by step through LDS, all query heads
+// of the key head among them.  Both tiles are read twice, as rows (S and dP) and transposed (t(dout) P and t(Q) dS).
+template <typename T, int DP>
+__global__ void __launch_bounds__(256, 1) attention_key_grad_kernel(const AttnArgs a)
 {
+    using L = Tile<DP>;
+    constexpr int kBytes = kStep * L::kRowBytes;
+    __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][Q, dout]
+    __shared__ __attribute__((aligned(16))) float stats[2][2][kStep];      // [step & 1][lse in base 2, delta]
+
     const int kvh = blockIdx.x % a.kv_heads;
     const long long t = blockIdx.x / a.kv_heads;
     const int s = seq_of_tile(a, a.k_off, a.k_tokens, 1, kRows, t);
     const Seq x = seq_at(a, s);
-    const long long first = (t - first_tile(x.k0, s, kRows)) * kRows, end = min(first + kRows, (long long)x.nk);
-    for (long long j = first + (threadIdx.x >> 6); j < end; j += 4)
-        key_grad_row<T>(a, x, (int)j, kvh);
+    const int first = (int)((t - first_tile(x.k0, s, kRows)) * kRows);
+    if (first >= x.nk)
+        return;
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int key = first + wave * 32 + (lane & 31);
+    const bool in = key < x.nk;
+    // the rows that see a key: from row from(key) on
+    const int rows = x.nq * a.group, begin = first_that_sees(a, x, first) * a.group;
+    const int from = first_that_sees(a, x, min(key, x.nk - 1)) * a.group;
+    const int from_lo = first + wave * 32 < x.nk ? __builtin_amdgcn_readfirstlane(from) : rows;
+    const int from_hi = __builtin_amdgcn_readlane(from, 31);
+
+    s16x8 k[L::kSteps], v[L::kSteps];
+    operands<T, DP>(k, row_of<const T>(a.k, x.k0 + min(key, x.nk - 1), kvh), in, a.dim);
+    operands<T, DP>(v, row_of<const T>(a.v, x.k0 + min(key, x.nk - 1), kvh), in, a.dim);
+    int row_at[L::kSteps], col_at[L::kCols][2];
+#pragma unroll
+    for (int i = 0; i < L::kSteps; ++i)
+        row_at[i] = L::row_at(lane, i);
+#pragma unroll
+    for (int i = 0; i < L::kCols; ++i) {
+        col_at[i][0] = L::col_at(lane, i, 0);
+        col_at[i][1] = L::col_at(lane, i, 1);
+    }
+    f32x16 dk[L::kCols], dv[L::kCols];
+#pragma unroll
+    for (int d = 0; d < L::kCols; ++d)
+        dk[d] = dv[d] = f32x16{};
+    const float c = a.scale * kLog2e;
+
+    const T *qbase = row_of<const T>(a.q, x.q0, kvh * a.group), *gbase = row_of<const T>(a.dout, x.q0, kvh * a.group);
+    const long long sbase = x.q0 * a.heads + kvh * a.group;
+    Stage<T, DP, kStep> qs, gs;
+    float stat = 0.0f;
+    auto load = [&](int r0) {
+        qs.load(r0, rows, a.dim, [&](int r) {
+            const int p = place_of(a, r);
+            return qbase + p * a.q.token + (r - p * a.group) * a.q.head;
+        });
+        gs.load(r0, rows, a.dim, [&](int r) {
+            const int p = place_of(a, r);
+            return gbase + p * a.dout.token + (r - p * a.group) * a.dout.head;
+        });
+        if (threadIdx.x < 2 * kStep) {     // rows behind the last one: weights of 0
+            const int r = r0 + threadIdx.x % kStep;
+            const bool is_lse = threadIdx.x < kStep;
+            stat = is_lse ? INFINITY : 0.0f;
+            if (r < rows) {
+                const int p = place_of(a, r);
+                const long long at = sbase + (long long)p * a.heads + (r - p * a.group);
+                stat = is_lse ? a.lse[at] * kLog2e : a.delta[at];
+            }
+        }
+    };
+    auto store = [&](int b) {
+        qs.store(lds[b][0]);
+        gs.store(lds[b][1]);
+        if (threadIdx.x < 2 * kStep)
+            stats[b][threadIdx.x / kStep][threadIdx.x % kStep] = stat;
+    };
+    if (begin < rows) {
+        load(begin);
+        store(0);
+    }
+    __syncthreads();
+    for (int r0 = begin, step = 0; r0 < rows; r0 += kStep, ++step) {
+        const char *qt = lds[step & 1][0], *gt = lds[step & 1][1];
+        const bool more = r0 + kStep < rows;
+        if (more)
+            load(r0 + kStep);
+        if (r0 + kStep > from_lo) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                f32x16 p = {}, dp = {};
+#pragma unroll
+                for (int i = 0; i < L::kSteps; ++i) {
+                    p = product<T>(read_row(qt + n * 32 * L::kRowBytes, row_at[i]), k[i], p);
+                    dp = product<T>(read_row(gt + n * 32 * L::kRowBytes, row_at[i]), v[i], dp);
+                }
+                const float *lse = stats[step & 1][0] + n * 32 + 4 * h, *delta = stats[step & 1][1] + n * 32 + 4 * h;
+                float w[16], ds[16];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 e = *reinterpret_cast<const f32x4 *>(lse + 8 * i), f = *reinterpret_cast<const f32x4 *>(delta + 8 * i);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -e[u]));
+                        ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - f[u]);
+                    }
+                }
+                if (r0 < from_hi) {
+                    const int skip = from - r0 - n * 32 - 4 * h;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (8 * (i / 4) + i % 4 < skip)
+                            w[i] = ds[i] = 0.0f;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const s16x8 bp = rounded<T>(w + u * 8), bs = rounded<T>(ds + u * 8);
+                    const int at = (n * 2 + u) * 16 * L::kRowBytes;
+#pragma unroll
+                    for (int d = 0; d < L::kCols; ++d) {
+                        dv[d] = product<T>(read_col(gt + at, col_at[d][0], col_at[d][1]), bp, dv[d]);
+                        dk[d] = product<T>(read_col(qt + at, col_at[d][0], col_at[d][1]), bs, dk[d]);
+                    }
+                }
+            }
+        }
+        if (more)
+            store((step + 1) & 1);
+        __syncthreads();
+    }
+
+    const float worst = not_finite(dk) + not_finite(dv);
+    const unsigned long long bad = __ballot(in && worst != 0.0f);
+    if (in && worst == 0.0f) {
+        write_columns<T>(dk, a.scale, row_of<T>(a.dk, x.k0 + key, kvh), h, a.dim);
+        write_columns<T>(dv, 1.0f, row_of<T>(a.dv, x.k0 + key, kvh), h, a.dim);
+    }
+    for (unsigned todo = (unsigned)(bad | (bad >> 32)); todo; todo &= todo - 1)
+        key_grad_row<T>(a, x, first + wave * 32 + __builtin_ctz(todo), kvh);
 }
 
 size_t backward_bytes(const fuse_attn *f) { return (size_t)f->q_tokens * f->heads * sizeof(float); }
 
-template <typename T>
-int launch_grads(const AttnArgs &a, hipStream_t s)
+template <typename T, int DP>
+int launch_dim(const AttnArgs &a, hipStream_t s)
 {
     const long long q_tiles = first_tile(a.q_tokens * a.group, a.seqs, kRows), k_tiles = first_tile(a.k_tokens, a.seqs, kRows);
     if (a.q_tokens > 0) {
-        attention_query_grad_kernel<T><<<(unsigned)(q_tiles * a.kv_heads), 256, 0, s>>>(a);
+        attention_query_grad_kernel<T, DP><<<(unsigned)(q_tiles * a.kv_heads), 256, 0, s>>>(a);
         if (const int rc = launched("attention_query_grad_kernel"))
             return rc;
     }
     if (a.k_tokens > 0)
-        attention_key_grad_kernel<T><<<(unsigned)(k_tiles * a.kv_heads), 256, 0, s>>>(a);
+        attention_key_grad_kernel<T, DP><<<(unsigned)(k_tiles * a.kv_heads), 256, 0, s>>>(a);
     return launched("attention_key_grad_kernel");
+}
+
+template <typename T>
+int launch_grads(const AttnArgs &a, hipStream_t s)
+{
+    return a.dim <= 64 ? launch_dim<T, 64>(a, s) : a.dim <= 96 ? launch_dim<T, 96>(a, s) : launch_dim<T, 128>(a, s);
 }
 
 int backward_impl(const fuse_attn *f, const fuse_attn_grads *g, void *workspace, size_t workspace_bytes, void *stream)

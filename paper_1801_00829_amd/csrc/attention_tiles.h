@@ -92,8 +92,8 @@ __device__ __forceinline__ s16x8 read_row(const char *lds, int at)
 __device__ __forceinline__ s16x8 read_col(const char *lds, int first, int second)
 {
     using P = __attribute__((address_space(3))) s16x4 *;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uint32_t)(uintptr_t)(lds + first));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uint32_t)(uintptr_t)(lds + second));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + first));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + second));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
@@ -108,8 +108,9 @@ struct Stage {
     static __device__ __forceinline__ int chunk() { return threadIdx.x % L::kChunks; }
     static __device__ __forceinline__ int row() { return threadIdx.x / L::kChunks; }
 
-    // `base`: row 0 of the matrix, `first`: the tile's first row
-    __device__ __forceinline__ void load(const T *base, long long ld, int first, int end, int dim)
+    // `at(r)`: where row r of the matrix is, `first`: the tile's first row
+    template <typename F>
+    __device__ __forceinline__ void load(int first, int end, int dim, F at)
     {
         const bool in = chunk() * 8 < dim;
 #pragma unroll
@@ -117,8 +118,13 @@ struct Stage {
             const int r = first + row() + i * kPerPass;
             v[i] = make_uint4(0, 0, 0, 0);
             if (in && r < end)
-                v[i] = *reinterpret_cast<const uint4 *>(base + r * ld + chunk() * 8);
+                v[i] = *reinterpret_cast<const uint4 *>(at(r) + chunk() * 8);
         }
+    }
+
+    __device__ __forceinline__ void load(const T *base, long long ld, int first, int end, int dim)
+    {
+        load(first, end, dim, [=](int r) { return base + r * ld; });
     }
 
     __device__ __forceinline__ void store(char *lds) const
