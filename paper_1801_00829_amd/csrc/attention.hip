@@ -94,21 +94,21 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, con
     const float c = a.scale * kLog2e;
 
     const T *kbase = row_of<const T>(a.k, x.k0, kvh), *vbase = row_of<const T>(a.v, x.k0, kvh);
-    Stage<T, DP, kKeys> ks, vs;
+    const Fill<T, DP, kKeys> fill(a.dim);
+    if (a.dim < DP)
+        clear_tiles(lds[0][0], sizeof lds);
     if (begin < end) {
-        ks.load(kbase, a.k.token, begin, x.nk, a.dim);
-        vs.load(vbase, a.v.token, begin, x.nk, a.dim);
-        ks.store(lds[0][0]);
-        vs.store(lds[0][1]);
+        fill.load(lds[0][0], kbase, a.k.token, begin, x.nk);
+        fill.load(lds[0][1], vbase, a.v.token, begin, x.nk);
     }
     __syncthreads();
     for (int j = begin, step = 0; j < end; j += kKeys, ++step) {
         const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
-        const bool more = j + kKeys < end;
-        if (more) {
-            ks.load(kbase, a.k.token, j + kKeys, x.nk, a.dim);
-            vs.load(vbase, a.v.token, j + kKeys, x.nk, a.dim);
+        if (j + kKeys < end) {             // into the tiles that all waves have left behind with the last barrier
+            fill.load(lds[(step + 1) & 1][0], kbase, a.k.token, j + kKeys, x.nk);
+            fill.load(lds[(step + 1) & 1][1], vbase, a.v.token, j + kKeys, x.nk);
         }
+        __builtin_amdgcn_sched_barrier(0); // the loads first, a whole step ahead of the barrier that waits for them
         if (j < seen_hi) {
             f32x16 p[2];
 #pragma unroll
@@ -148,10 +148,6 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, con
                 for (int d = 0; d < L::kCols; ++d)
                     o[d] = product<T>(read_col(vt + n * 16 * L::kRowBytes, col_at[d][0], col_at[d][1]), b, o[d]);
             }
-        }
-        if (more) {
-            ks.store(lds[(step + 1) & 1][0]);
-            vs.store(lds[(step + 1) & 1][1]);
         }
         __syncthreads();
     }

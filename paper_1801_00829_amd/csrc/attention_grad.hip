@@ -5,8 +5,9 @@ namespace {
 
 using namespace fuse;
 
-constexpr int kRows = 128;                 // rows, or keys, per block: 32 per wave
+constexpr int kRows = 128;                 // rows per block: 32 per wave
 constexpr int kStep = 64;                  // keys, or rows, per step
+constexpr int kKeys = 128;                 // keys per block of their kernel
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // A wave's 32 columns of 32 DT dims, rounded, to rows of a matrix.
@@ -102,21 +103,21 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
     const float c = a.scale * kLog2e;
 
     const T *kbase = row_of<const T>(a.k, x.k0, kvh), *vbase = row_of<const T>(a.v, x.k0, kvh);
-    Stage<T, DP, kStep> ks, vs;
+    const Fill<T, DP, kStep> fill(a.dim);
+    if (a.dim < DP)
+        clear_tiles(lds[0][0], sizeof lds);
     if (end > 0) {
-        ks.load(kbase, a.k.token, 0, x.nk, a.dim);
-        vs.load(vbase, a.v.token, 0, x.nk, a.dim);
-        ks.store(lds[0][0]);
-        vs.store(lds[0][1]);
+        fill.load(lds[0][0], kbase, a.k.token, 0, x.nk);
+        fill.load(lds[0][1], vbase, a.v.token, 0, x.nk);
     }
     __syncthreads();
     for (int j = 0, step = 0; j < end; j += kStep, ++step) {
         const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
-        const bool more = j + kStep < end;
-        if (more) {
-            ks.load(kbase, a.k.token, j + kStep, x.nk, a.dim);
-            vs.load(vbase, a.v.token, j + kStep, x.nk, a.dim);
+        if (j + kStep < end) {
+            fill.load(lds[(step + 1) & 1][0], kbase, a.k.token, j + kStep, x.nk);
+            fill.load(lds[(step + 1) & 1][1], vbase, a.v.token, j + kStep, x.nk);
         }
+        __builtin_amdgcn_sched_barrier(0);
         if (j < seen_hi) {
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
@@ -146,10 +147,6 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
                 }
             }
         }
-        if (more) {
-            ks.store(lds[(step + 1) & 1][0]);
-            vs.store(lds[(step + 1) & 1][1]);
-        }
         __syncthreads();
     }
 
@@ -164,61 +161,68 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
     }
 }
 
-// Gradients of the keys and values: 32 keys per wave as columns, the rows that see them step by step through LDS, all query heads
-// of the key head among them.  Both tiles are read twice, as rows (S and dP) and transposed (t(dout) P and t(Q) dS).
+// Gradients of the keys and values: 128 keys per block, the rows that see them step by step through LDS, all query heads of the key
+// head among them.  Both tiles are read twice, as rows (S and dP) and transposed (t(dout) P and t(Q) dS).
+//
+// Two waves share 32 keys, as columns.  Each takes half of a step's rows for S, dP, P and dS, the two exchange P and dS through LDS, and
+// each adds all rows' products to half of the dims of dV and dK.  That is the same work as a wave for itself, but 64 registers of sums
+// instead of 128: with those, next to 64 of keys and values, nothing is left to load operands ahead of the products.
 template <typename T, int DP>
-__global__ void __launch_bounds__(256, 1) attention_key_grad_kernel(const AttnArgs a)
+__global__ void __launch_bounds__(512, 2) attention_key_grad_kernel(const AttnArgs a)
 {
     using L = Tile<DP>;
-    constexpr int kBytes = kStep * L::kRowBytes;
+    constexpr int kBytes = kStep * L::kRowBytes, kHalfCols = (L::kCols + 1) / 2;
     __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][Q, dout]
+    __shared__ s16x8 exchange[4][2][2][2][64];                             // [keys][rows' half][16 rows][P, dS][lane]
     __shared__ __attribute__((aligned(16))) float stats[2][2][kStep];      // [step & 1][lse in base 2, delta]
+    __shared__ unsigned not_numbers[2][4];
 
     const int kvh = blockIdx.x % a.kv_heads;
     const long long t = blockIdx.x / a.kv_heads;
-    const int s = seq_of_tile(a, a.k_off, a.k_tokens, 1, kRows, t);
+    const int s = seq_of_tile(a, a.k_off, a.k_tokens, 1, kKeys, t);
     const Seq x = seq_at(a, s);
-    const int first = (int)((t - first_tile(x.k0, s, kRows)) * kRows);
+    const int first = (int)((t - first_tile(x.k0, s, kKeys)) * kKeys);
     if (first >= x.nk)
         return;
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int key = first + wave * 32 + (lane & 31);
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keys = wave & 3, half = wave >> 2;
+    const int key0 = first + keys * 32, key = key0 + (lane & 31);
     const bool in = key < x.nk;
     // the rows that see a key: from row from(key) on
     const int rows = x.nq * a.group, begin = first_that_sees(a, x, first) * a.group;
     const int from = first_that_sees(a, x, min(key, x.nk - 1)) * a.group;
-    const int from_lo = first + wave * 32 < x.nk ? __builtin_amdgcn_readfirstlane(from) : rows;
+    const int from_lo = key0 < x.nk ? __builtin_amdgcn_readfirstlane(from) : rows;
     const int from_hi = __builtin_amdgcn_readlane(from, 31);
 
     s16x8 k[L::kSteps], v[L::kSteps];
     operands<T, DP>(k, row_of<const T>(a.k, x.k0 + min(key, x.nk - 1), kvh), in, a.dim);
     operands<T, DP>(v, row_of<const T>(a.v, x.k0 + min(key, x.nk - 1), kvh), in, a.dim);
-    int row_at[L::kSteps], col_at[L::kCols][2];
+    int row_at[L::kSteps], col_at[kHalfCols][2];
 #pragma unroll
     for (int i = 0; i < L::kSteps; ++i)
         row_at[i] = L::row_at(lane, i);
 #pragma unroll
-    for (int i = 0; i < L::kCols; ++i) {
-        col_at[i][0] = L::col_at(lane, i, 0);
-        col_at[i][1] = L::col_at(lane, i, 1);
+    for (int i = 0; i < kHalfCols; ++i) {
+        col_at[i][0] = L::col_at(lane, half * kHalfCols + i, 0);
+        col_at[i][1] = L::col_at(lane, half * kHalfCols + i, 1);
     }
-    f32x16 dk[L::kCols], dv[L::kCols];
+    f32x16 dk[kHalfCols], dv[kHalfCols];
 #pragma unroll
-    for (int d = 0; d < L::kCols; ++d)
+    for (int d = 0; d < kHalfCols; ++d)
         dk[d] = dv[d] = f32x16{};
     const float c = a.scale * kLog2e;
 
     const T *qbase = row_of<const T>(a.q, x.q0, kvh * a.group), *gbase = row_of<const T>(a.dout, x.q0, kvh * a.group);
     const long long sbase = x.q0 * a.heads + kvh * a.group;
-    Stage<T, DP, kStep> qs, gs;
+    const Fill<T, DP, kStep, 512> fill(a.dim);
     float stat = 0.0f;
-    auto load = [&](int r0) {
-        qs.load(r0, rows, a.dim, [&](int r) {
+    auto load = [&](int r0, int b) {
+        fill.load(lds[b][0], r0, rows, [&](int r) {
             const int p = place_of(a, r);
             return qbase + p * a.q.token + (r - p * a.group) * a.q.head;
         });
-        gs.load(r0, rows, a.dim, [&](int r) {
+        fill.load(lds[b][1], r0, rows, [&](int r) {
             const int p = place_of(a, r);
             return gbase + p * a.dout.token + (r - p * a.group) * a.dout.head;
         });
@@ -234,13 +238,13 @@ __global__ void __launch_bounds__(256, 1) attention_key_grad_kernel(const AttnAr
         }
     };
     auto store = [&](int b) {
-        qs.store(lds[b][0]);
-        gs.store(lds[b][1]);
         if (threadIdx.x < 2 * kStep)
             stats[b][threadIdx.x / kStep][threadIdx.x % kStep] = stat;
     };
+    if (a.dim < DP)
+        clear_tiles(lds[0][0], sizeof lds);
     if (begin < rows) {
-        load(begin);
+        load(begin, 0);
         store(0);
     }
     __syncthreads();
@@ -248,59 +252,75 @@ __global__ void __launch_bounds__(256, 1) attention_key_grad_kernel(const AttnAr
         const char *qt = lds[step & 1][0], *gt = lds[step & 1][1];
         const bool more = r0 + kStep < rows;
         if (more)
-            load(r0 + kStep);
-        if (r0 + kStep > from_lo) {
+            load(r0 + kStep, (step + 1) & 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (r0 + half * 32 + 32 > from_lo) {
+            f32x16 p = {}, dp = {};
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                f32x16 p = {}, dp = {};
+            for (int i = 0; i < L::kSteps; ++i) {
+                p = product<T>(read_row(qt + half * 32 * L::kRowBytes, row_at[i]), k[i], p);
+                dp = product<T>(read_row(gt + half * 32 * L::kRowBytes, row_at[i]), v[i], dp);
+            }
+            const float *lse = stats[step & 1][0] + half * 32 + 4 * h, *delta = stats[step & 1][1] + half * 32 + 4 * h;
+            float w[16], ds[16];
 #pragma unroll
-                for (int i = 0; i < L::kSteps; ++i) {
-                    p = product<T>(read_row(qt + n * 32 * L::kRowBytes, row_at[i]), k[i], p);
-                    dp = product<T>(read_row(gt + n * 32 * L::kRowBytes, row_at[i]), v[i], dp);
-                }
-                const float *lse = stats[step & 1][0] + n * 32 + 4 * h, *delta = stats[step & 1][1] + n * 32 + 4 * h;
-                float w[16], ds[16];
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 e = *reinterpret_cast<const f32x4 *>(lse + 8 * i), f = *reinterpret_cast<const f32x4 *>(delta + 8 * i);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x4 e = *reinterpret_cast<const f32x4 *>(lse + 8 * i), f = *reinterpret_cast<const f32x4 *>(delta + 8 * i);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -e[u]));
-                        ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - f[u]);
-                    }
-                }
-                if (r0 < from_hi) {
-                    const int skip = from - r0 - n * 32 - 4 * h;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (8 * (i / 4) + i % 4 < skip)
-                            w[i] = ds[i] = 0.0f;
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const s16x8 bp = rounded<T>(w + u * 8), bs = rounded<T>(ds + u * 8);
-                    const int at = (n * 2 + u) * 16 * L::kRowBytes;
-#pragma unroll
-                    for (int d = 0; d < L::kCols; ++d) {
-                        dv[d] = product<T>(read_col(gt + at, col_at[d][0], col_at[d][1]), bp, dv[d]);
-                        dk[d] = product<T>(read_col(qt + at, col_at[d][0], col_at[d][1]), bs, dk[d]);
-                    }
+                for (int u = 0; u < 4; ++u) {
+                    w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -e[u]));
+                    ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - f[u]);
                 }
             }
+            if (r0 + half * 32 < from_hi) {
+                const int skip = from - r0 - half * 32 - 4 * h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i / 4) + i % 4 < skip)
+                        w[i] = ds[i] = 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                exchange[keys][half][u][0][lane] = rounded<T>(w + u * 8);
+                exchange[keys][half][u][1][lane] = rounded<T>(ds + u * 8);
+            }
         }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+            if (r0 + n * 32 + 32 > from_lo) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const s16x8 bp = exchange[keys][n][u][0][lane], bs = exchange[keys][n][u][1][lane];
+                    const int at = (n * 2 + u) * 16 * L::kRowBytes;
+#pragma unroll
+                    for (int d = 0; d < kHalfCols; ++d)
+                        if (half * kHalfCols + d < L::kCols) {
+                            dv[d] = product<T>(read_col(gt + at, col_at[d][0], col_at[d][1]), bp, dv[d]);
+                            dk[d] = product<T>(read_col(qt + at, col_at[d][0], col_at[d][1]), bs, dk[d]);
+                        }
+                }
+            }
         if (more)
             store((step + 1) & 1);
         __syncthreads();
     }
 
+    // keys whose gradient is not finite in either half of the dims: again, by the first of the two waves
     const float worst = not_finite(dk) + not_finite(dv);
-    const unsigned long long bad = __ballot(in && worst != 0.0f);
-    if (in && worst == 0.0f) {
-        write_columns<T>(dk, a.scale, row_of<T>(a.dk, x.k0 + key, kvh), h, a.dim);
-        write_columns<T>(dv, 1.0f, row_of<T>(a.dv, x.k0 + key, kvh), h, a.dim);
+    unsigned long long bad = __ballot(in && worst != 0.0f);
+    if (lane == 0)
+        not_numbers[half][keys] = (unsigned)(bad | (bad >> 32));
+    __syncthreads();
+    unsigned todo = not_numbers[0][keys] | not_numbers[1][keys];
+    if (in && !((todo >> (lane & 31)) & 1)) {
+        const int d0 = half * kHalfCols * 32;
+        write_columns<T>(dk, a.scale, row_of<T>(a.dk, x.k0 + key, kvh) + d0, h, a.dim - d0);
+        write_columns<T>(dv, 1.0f, row_of<T>(a.dv, x.k0 + key, kvh) + d0, h, a.dim - d0);
     }
-    for (unsigned todo = (unsigned)(bad | (bad >> 32)); todo; todo &= todo - 1)
-        key_grad_row<T>(a, x, first + wave * 32 + __builtin_ctz(todo), kvh);
+    if (half == 0)
+        for (; todo; todo &= todo - 1)
+            key_grad_row<T>(a, x, key0 + __builtin_ctz(todo), kvh);
 }
 
 size_t backward_bytes(const fuse_attn *f) { return (size_t)f->q_tokens * f->heads * sizeof(float); }
@@ -308,14 +328,14 @@ size_t backward_bytes(const fuse_attn *f) { return (size_t)f->q_tokens * f->head
 template <typename T, int DP>
 int launch_dim(const AttnArgs &a, hipStream_t s)
 {
-    const long long q_tiles = first_tile(a.q_tokens * a.group, a.seqs, kRows), k_tiles = first_tile(a.k_tokens, a.seqs, kRows);
+    const long long q_tiles = first_tile(a.q_tokens * a.group, a.seqs, kRows), k_tiles = first_tile(a.k_tokens, a.seqs, kKeys);
     if (a.q_tokens > 0) {
         attention_query_grad_kernel<T, DP><<<(unsigned)(q_tiles * a.kv_heads), 256, 0, s>>>(a);
         if (const int rc = launched("attention_query_grad_kernel"))
             return rc;
     }
     if (a.k_tokens > 0)
-        attention_key_grad_kernel<T, DP><<<(unsigned)(k_tiles * a.kv_heads), 256, 0, s>>>(a);
+        attention_key_grad_kernel<T, DP><<<(unsigned)(k_tiles * a.kv_heads), 512, 0, s>>>(a);
     return launched("attention_key_grad_kernel");
 }
 

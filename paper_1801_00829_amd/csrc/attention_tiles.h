@@ -97,46 +97,52 @@ __device__ __forceinline__ s16x8 read_col(const char *lds, int first, int second
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// ROWS rows of a matrix on their way to LDS by 256 threads: loaded into registers while the tile before is worked on, written
-// when it is done.  Rows from `end` on are zeros and not read.
-template <typename T, int DP, int ROWS>
-struct Stage {
+// Brings ROWS rows of a matrix to LDS by THREADS threads, straight from memory: a wave's load writes 64 chunks one behind the other, so
+// each lane asks for the chunk that belongs in its place.  Nothing waits here; the barrier that ends a step waits for the loads.
+// Rows from `end` on hold the last row instead: their scores are masked, and what a weight of 0 makes of a value that is not finite
+// is looked for where the results are written.  Chunks behind dim are left as they are (clear_tiles).
+template <typename T, int DP, int ROWS, int THREADS = 256>
+struct Fill {
     using L = Tile<DP>;
-    static constexpr int kPerPass = 256 / L::kChunks, kPasses = ROWS / kPerPass;
-    uint4 v[kPasses];
+    static constexpr int kPerPass = THREADS / L::kChunks, kPasses = ROWS / kPerPass;
+    static_assert(kPerPass % 16 == 0 && ROWS % kPerPass == 0, "all rows of a lane have one turn");
 
-    static __device__ __forceinline__ int chunk() { return threadIdx.x % L::kChunks; }
-    static __device__ __forceinline__ int row() { return threadIdx.x / L::kChunks; }
+    int row, chunk, wave;
+    bool in;
 
-    // `at(r)`: where row r of the matrix is, `first`: the tile's first row
+    __device__ __forceinline__ explicit Fill(int dim)
+    {
+        row = threadIdx.x / L::kChunks;
+        chunk = (threadIdx.x % L::kChunks) ^ L::turn(row);
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        in = chunk * 8 < dim;
+    }
+
+    // `at(r)`: where row r of the matrix is; `first`: the tile's first row, `end` > first
     template <typename F>
-    __device__ __forceinline__ void load(int first, int end, int dim, F at)
+    __device__ __forceinline__ void load(char *lds, int first, int end, F at) const
     {
-        const bool in = chunk() * 8 < dim;
+        if (in)
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int r = first + row() + i * kPerPass;
-            v[i] = make_uint4(0, 0, 0, 0);
-            if (in && r < end)
-                v[i] = *reinterpret_cast<const uint4 *>(at(r) + chunk() * 8);
-        }
+            for (int i = 0; i < kPasses; ++i)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)(at(min(first + row + i * kPerPass, end - 1)) + chunk * 8),
+                    (__attribute__((address_space(3))) void *)(lds + i * kPerPass * L::kRowBytes + wave * 1024), 16, 0, 0);
     }
 
-    __device__ __forceinline__ void load(const T *base, long long ld, int first, int end, int dim)
+    __device__ __forceinline__ void load(char *lds, const T *base, long long ld, int first, int end) const
     {
-        load(first, end, dim, [=](int r) { return base + r * ld; });
-    }
-
-    __device__ __forceinline__ void store(char *lds) const
-    {
-        if (chunk() < L::kUsed)
-#pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                const int r = row() + i * kPerPass;
-                *reinterpret_cast<uint4 *>(lds + r * L::kRowBytes + ((chunk() ^ L::turn(r)) << 4)) = v[i];
-            }
+        load(lds, first, end, [=](int r) { return base + r * ld; });
     }
 };
+
+// Zeros in all places of a kernel's tiles, where some stand for dims behind dim; ends with a barrier.
+__device__ __forceinline__ void clear_tiles(char *lds, int bytes)
+{
+    for (int i = threadIdx.x * 16; i < bytes; i += blockDim.x * 16)
+        *reinterpret_cast<uint4 *>(lds + i) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+}
 
 // A row of 16-bit values as the B operands of the products over dim: row_of the lane's column, 0 behind dim or without a row.
 template <typename T, int DP>
