@@ -18,7 +18,8 @@ struct Mat {
 
 struct AttnArgs {
     Mat q, k, v, out, dout, dq, dk, dv;
-    float *lse, *delta;                    // q_tokens x heads
+    float *lse;                            // q_tokens x heads
+    float *delta, *lse2;                   // gradients: sum of dout o out, and lse in base 2; see stat_at
     const void *q_off, *k_off, *k_len;     // k_len NULL: the distances of k_off
     long long q_tokens, k_tokens;
     int seqs, heads, kv_heads, group, dim, causal, off64;
@@ -159,6 +160,12 @@ __device__ void attend_row(const AttnArgs &a, const Seq &x, int place, int head)
         a.lse[(x.q0 + place) * a.heads + head] = base + logf(sum);
 }
 
+// Place of a row's delta and lse2: key heads x rows, so that the rows of one problem follow each other.
+__device__ __forceinline__ long long stat_at(const AttnArgs &a, long long token, int head)
+{
+    return (head / a.group * a.q_tokens + token) * a.group + head % a.group;
+}
+
 template <typename T>
 __device__ __forceinline__ float delta_of(const AttnArgs &a, long long token, int head)
 {
@@ -195,7 +202,7 @@ __device__ void query_grad_row(const AttnArgs &a, const Seq &x, int place, int h
     if (lane + 64 < a.dim)
         out[lane + 64] = (T)o1;
     if (lane == 0)
-        a.delta[token * a.heads + head] = delta;
+        a.delta[stat_at(a, token, head)] = delta;
 }
 
 // One key's and value's gradients by one wave, query by query over all heads of the group.
@@ -212,7 +219,7 @@ __device__ void key_grad_row(const AttnArgs &a, const Seq &x, int j, int kvh)
             const long long token = x.q0 + (r0 + lane) / a.group;
             const int head = kvh * a.group + (int)((r0 + lane) % a.group);
             p = expf(a.scale * dot_rows(row_of<const T>(a.q, token, head), k, a.dim) - a.lse[token * a.heads + head]);
-            ds = a.scale * p * (dot_rows(row_of<const T>(a.dout, token, head), v, a.dim) - a.delta[token * a.heads + head]);
+            ds = a.scale * p * (dot_rows(row_of<const T>(a.dout, token, head), v, a.dim) - a.delta[stat_at(a, token, head)]);
         }
         for (int i = 0; i < 64 && r0 + i < end; ++i) {
             const float wp = __shfl(p, i, 64), ws = __shfl(ds, i, 64);

@@ -7,7 +7,7 @@ using namespace fuse;
 
 constexpr int kRows = 128;                 // rows per block: 32 per wave
 constexpr int kStep = 64;                  // keys, or rows, per step
-constexpr int kKeys = 128;                 // keys per block of their kernel
+constexpr int kKeys = 64;                  // keys per block of their kernel
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // A wave's 32 columns of 32 DT dims, rounded, to rows of a matrix.
@@ -37,7 +37,7 @@ __device__ __forceinline__ float not_finite(const f32x16 (&o)[DT])
     return w;
 }
 
-// Gradient of the queries, and delta for the keys' kernel.  As the forward kernel: 32 rows per wave as columns, keys and values
+// Gradient of the queries, and delta and lse, in the order of the rows, for the keys' kernel.  As the forward kernel: 32 rows per wave as columns, keys and values
 // step by step through LDS; the keys are read twice, as rows for S and transposed for t(K) t(dS).
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const AttnArgs a)
@@ -81,10 +81,12 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
         delta = both_sum(delta);
     }
     if (in) {
-        const long long at = (x.q0 + place) * a.heads + head;
-        lse2 = a.lse[at] * kLog2e;
-        if (h == 0)
+        const long long at = stat_at(a, x.q0 + place, head);
+        lse2 = a.lse[(x.q0 + place) * a.heads + head] * kLog2e;
+        if (h == 0) {
             a.delta[at] = delta;
+            a.lse2[at] = lse2;
+        }
     }
 
     int row_at[L::kSteps], col_at[L::kCols][2];
@@ -161,21 +163,20 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
     }
 }
 
-// Gradients of the keys and values: 128 keys per block, the rows that see them step by step through LDS, all query heads of the key
+// Gradients of the keys and values: 64 keys per block, the rows that see them step by step through LDS, all query heads of the key
 // head among them.  Both tiles are read twice, as rows (S and dP) and transposed (t(dout) P and t(Q) dS).
 //
 // Two waves share 32 keys, as columns.  Each takes half of a step's rows for S, dP, P and dS, the two exchange P and dS through LDS, and
 // each adds all rows' products to half of the dims of dV and dK.  That is the same work as a wave for itself, but 64 registers of sums
 // instead of 128: with those, next to 64 of keys and values, nothing is left to load operands ahead of the products.
 template <typename T, int DP>
-__global__ void __launch_bounds__(512, 2) attention_key_grad_kernel(const AttnArgs a)
+__global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnArgs a)
 {
     using L = Tile<DP>;
     constexpr int kBytes = kStep * L::kRowBytes, kHalfCols = (L::kCols + 1) / 2;
     __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][Q, dout]
-    __shared__ s16x8 exchange[4][2][2][2][64];                             // [keys][rows' half][16 rows][P, dS][lane]
-    __shared__ __attribute__((aligned(16))) float stats[2][2][kStep];      // [step & 1][lse in base 2, delta]
-    __shared__ unsigned not_numbers[2][4];
+    __shared__ s16x8 exchange[2][2][2][2][64];                             // [keys][rows' half][16 rows][P, dS][lane]
+    // (80 KB for a dim of 128: two blocks per compute unit, whose steps overlap)
 
     const int kvh = blockIdx.x % a.kv_heads;
     const long long t = blockIdx.x / a.kv_heads;
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(512, 2) attention_key_grad_kernel(const AttnAr
         return;
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keys = wave & 3, half = wave >> 2;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keys = wave & 1, half = wave >> 1;
     const int key0 = first + keys * 32, key = key0 + (lane & 31);
     const bool in = key < x.nk;
     // the rows that see a key: from row from(key) on
@@ -214,9 +215,8 @@ __global__ void __launch_bounds__(512, 2) attention_key_grad_kernel(const AttnAr
     const float c = a.scale * kLog2e;
 
     const T *qbase = row_of<const T>(a.q, x.q0, kvh * a.group), *gbase = row_of<const T>(a.dout, x.q0, kvh * a.group);
-    const long long sbase = x.q0 * a.heads + kvh * a.group;
-    const Fill<T, DP, kStep, 512> fill(a.dim);
-    float stat = 0.0f;
+    const long long sbase = stat_at(a, x.q0, kvh * a.group);
+    const Fill<T, DP, kStep> fill(a.dim);
     auto load = [&](int r0, int b) {
         fill.load(lds[b][0], r0, rows, [&](int r) {
             const int p = place_of(a, r);
@@ -226,57 +226,50 @@ __global__ void __launch_bounds__(512, 2) attention_key_grad_kernel(const AttnAr
             const int p = place_of(a, r);
             return gbase + p * a.dout.token + (r - p * a.group) * a.dout.head;
         });
-        if (threadIdx.x < 2 * kStep) {     // rows behind the last one: weights of 0
-            const int r = r0 + threadIdx.x % kStep;
-            const bool is_lse = threadIdx.x < kStep;
-            stat = is_lse ? INFINITY : 0.0f;
-            if (r < rows) {
-                const int p = place_of(a, r);
-                const long long at = sbase + (long long)p * a.heads + (r - p * a.group);
-                stat = is_lse ? a.lse[at] * kLog2e : a.delta[at];
-            }
-        }
-    };
-    auto store = [&](int b) {
-        if (threadIdx.x < 2 * kStep)
-            stats[b][threadIdx.x / kStep][threadIdx.x % kStep] = stat;
     };
     if (a.dim < DP)
         clear_tiles(lds[0][0], sizeof lds);
-    if (begin < rows) {
+    if (begin < rows)
         load(begin, 0);
-        store(0);
-    }
     __syncthreads();
     for (int r0 = begin, step = 0; r0 < rows; r0 += kStep, ++step) {
         const char *qt = lds[step & 1][0], *gt = lds[step & 1][1];
-        const bool more = r0 + kStep < rows;
-        if (more)
+        const bool work = r0 + half * 32 + 32 > from_lo;
+        f32x4u lse[4], delta[4];           // of rows 8 i + 4 h ..; behind the last row they are anything, and masked
+        if (work) {
+            const long long at = sbase + r0 + half * 32 + 4 * h;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lse[i] = *reinterpret_cast<const f32x4u *>(a.lse2 + at + 8 * i);
+                delta[i] = *reinterpret_cast<const f32x4u *>(a.delta + at + 8 * i);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (r0 + kStep < rows)
             load(r0 + kStep, (step + 1) & 1);
         __builtin_amdgcn_sched_barrier(0);
-        if (r0 + half * 32 + 32 > from_lo) {
+        if (work) {
             f32x16 p = {}, dp = {};
 #pragma unroll
             for (int i = 0; i < L::kSteps; ++i) {
                 p = product<T>(read_row(qt + half * 32 * L::kRowBytes, row_at[i]), k[i], p);
                 dp = product<T>(read_row(gt + half * 32 * L::kRowBytes, row_at[i]), v[i], dp);
             }
-            const float *lse = stats[step & 1][0] + half * 32 + 4 * h, *delta = stats[step & 1][1] + half * 32 + 4 * h;
+            ahead<L::kSteps * 2, 6>();
             float w[16], ds[16];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f32x4 e = *reinterpret_cast<const f32x4 *>(lse + 8 * i), f = *reinterpret_cast<const f32x4 *>(delta + 8 * i);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -e[u]));
-                    ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - f[u]);
+                    w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -lse[i][u]));
+                    ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - delta[i][u]);
                 }
             }
-            if (r0 + half * 32 < from_hi) {
-                const int skip = from - r0 - half * 32 - 4 * h;
+            if (r0 + half * 32 < from_hi || r0 + half * 32 + 32 > rows) {
+                const int skip = from - r0 - half * 32 - 4 * h, left = rows - r0 - half * 32 - 4 * h;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (8 * (i / 4) + i % 4 < skip)
+                    if (8 * (i / 4) + i % 4 < skip || 8 * (i / 4) + i % 4 >= left)
                         w[i] = ds[i] = 0.0f;
             }
 #pragma unroll
@@ -295,20 +288,19 @@ __global__ void __launch_bounds__(512, 2) attention_key_grad_kernel(const AttnAr
                     const int at = (n * 2 + u) * 16 * L::kRowBytes;
 #pragma unroll
                     for (int d = 0; d < kHalfCols; ++d)
-                        if (half * kHalfCols + d < L::kCols) {
+                        if (L::kCols % 2 == 0 || half * kHalfCols + d < L::kCols) {
                             dv[d] = product<T>(read_col(gt + at, col_at[d][0], col_at[d][1]), bp, dv[d]);
                             dk[d] = product<T>(read_col(qt + at, col_at[d][0], col_at[d][1]), bs, dk[d]);
                         }
                 }
             }
-        if (more)
-            store((step + 1) & 1);
         __syncthreads();
     }
 
     // keys whose gradient is not finite in either half of the dims: again, by the first of the two waves
     const float worst = not_finite(dk) + not_finite(dv);
     unsigned long long bad = __ballot(in && worst != 0.0f);
+    unsigned (*not_numbers)[2] = reinterpret_cast<unsigned (*)[2]>(lds[0][0]);     // (all waves are behind the last barrier)
     if (lane == 0)
         not_numbers[half][keys] = (unsigned)(bad | (bad >> 32));
     __syncthreads();
@@ -323,7 +315,8 @@ __global__ void __launch_bounds__(512, 2) attention_key_grad_kernel(const AttnAr
             key_grad_row<T>(a, x, key0 + __builtin_ctz(todo), kvh);
 }
 
-size_t backward_bytes(const fuse_attn *f) { return (size_t)f->q_tokens * f->heads * sizeof(float); }
+// delta and lse2, each with room for a last step's rows behind the last row
+size_t backward_bytes(const fuse_attn *f) { return ((size_t)f->q_tokens * f->heads + kStep) * 2 * sizeof(float); }
 
 template <typename T, int DP>
 int launch_dim(const AttnArgs &a, hipStream_t s)
@@ -335,7 +328,7 @@ int launch_dim(const AttnArgs &a, hipStream_t s)
             return rc;
     }
     if (a.k_tokens > 0)
-        attention_key_grad_kernel<T, DP><<<(unsigned)(k_tiles * a.kv_heads), 512, 0, s>>>(a);
+        attention_key_grad_kernel<T, DP><<<(unsigned)(k_tiles * a.kv_heads), 256, 0, s>>>(a);
     return launched("attention_key_grad_kernel");
 }
 
@@ -373,6 +366,7 @@ int backward_impl(const fuse_attn *f, const fuse_attn_grads *g, void *workspace,
     a.dv = {g->dv, g->dv_token_ld, g->dv_head_ld};
     a.lse = const_cast<float *>(g->lse);
     a.delta = static_cast<float *>(workspace);
+    a.lse2 = a.delta + f->q_tokens * f->heads + kStep;
     return f->dtype == FUSE_BF16 ? launch_grads<__bf16>(a, (hipStream_t)stream) : launch_grads<_Float16>(a, (hipStream_t)stream);
 }
 

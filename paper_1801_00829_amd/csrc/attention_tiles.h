@@ -15,6 +15,7 @@ namespace fuse {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -28,6 +29,19 @@ template <> __device__ __forceinline__ f32x16 product<__bf16>(s16x8 a, s16x8 b, 
 template <> __device__ __forceinline__ f32x16 product<_Float16>(s16x8 a, s16x8 b, f32x16 c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// For the scheduler: N products with an LDS load each, DEPTH loads ahead of the first product.
+template <int N, int DEPTH>
+__device__ __forceinline__ void ahead()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, DEPTH, 0);
+#pragma unroll
+    for (int i = 0; i < N - DEPTH; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x8, DEPTH, 0);
 }
 
 // Eight values, rounded, as a B operand.
