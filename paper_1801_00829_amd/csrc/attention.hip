@@ -51,23 +51,22 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, con
     const int kvh = blockIdx.x % a.kv_heads;
     const unsigned rest = blockIdx.x / a.kv_heads;
     const int split = rest % parts.splits;
-    const long long t = rest / parts.splits;
-    const int s = seq_of_tile(a, a.q_off, a.q_tokens, a.group, kRows, t);
-    const Seq x = seq_at(a, s);
-    const long long first = (t - first_tile(x.q0 * a.group, s, kRows)) * kRows, rows = (long long)x.nq * a.group;
-    if (first >= rows)
+    const Work work = work_of<false>(a, kRows, rest / parts.splits);
+    if (!work.any)
         return;
+    const Seq &x = work.x;
+    const int first = work.first, rows = x.nq * a.group;
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const long long r = first + wave * 32 + (lane & 31);
+    const int r = first + wave * 32 + (lane & 31);
     const bool in = r < rows;
-    const int place = (int)((in ? r : rows - 1) / a.group), head = kvh * a.group + (int)((in ? r : rows - 1) % a.group);
+    const int place = place_of(a, in ? r : rows - 1), head = kvh * a.group + (in ? r : rows - 1) - place * a.group;
     const int seen = seen_by(a, x, place);
     const int seen_lo = __builtin_amdgcn_readfirstlane(seen);              // the wave's first row sees least, its last row most
     const int seen_hi = first + wave * 32 < rows ? __builtin_amdgcn_readlane(seen, 31) : 0;
 
     // this split's keys: begin .. end of those that any row of the tile sees
-    int begin = 0, end = seen_by(a, x, (int)((min(first + kRows, rows) - 1) / a.group));
+    int begin = 0, end = seen_by(a, x, place_of(a, min(first + kRows, rows) - 1));
     if (parts.splits > 1) {
         const int per = ((end + parts.splits - 1) / parts.splits + kKeys - 1) / kKeys * kKeys;
         begin = min(split * per, end);
@@ -195,8 +194,8 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, con
             a.lse[(x.q0 + place) * a.heads + head] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, logf(l));
     }
     for (unsigned todo = (unsigned)(bad | (bad >> 32)); todo; todo &= todo - 1) {
-        const long long again = first + wave * 32 + __builtin_ctz(todo);
-        attend_row<T>(a, x, (int)(again / a.group), kvh * a.group + (int)(again % a.group));
+        const int again = first + wave * 32 + __builtin_ctz(todo), p = place_of(a, again);
+        attend_row<T>(a, x, p, kvh * a.group + again - p * a.group);
     }
 }
 

@@ -47,12 +47,11 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
     __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][K, V]
 
     const int kvh = blockIdx.x % a.kv_heads;
-    const long long t = blockIdx.x / a.kv_heads;
-    const int s = seq_of_tile(a, a.q_off, a.q_tokens, a.group, kRows, t);
-    const Seq x = seq_at(a, s);
-    const int first = (int)((t - first_tile(x.q0 * a.group, s, kRows)) * kRows), rows = x.nq * a.group;
-    if (first >= rows)
+    const Work work = work_of<false>(a, kRows, blockIdx.x / a.kv_heads);
+    if (!work.any)
         return;
+    const Seq &x = work.x;
+    const int first = work.first, rows = x.nq * a.group;
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     const int r = first + wave * 32 + (lane & 31);
@@ -179,12 +178,11 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
     // (80 KB for a dim of 128: two blocks per compute unit, whose steps overlap)
 
     const int kvh = blockIdx.x % a.kv_heads;
-    const long long t = blockIdx.x / a.kv_heads;
-    const int s = seq_of_tile(a, a.k_off, a.k_tokens, 1, kKeys, t);
-    const Seq x = seq_at(a, s);
-    const int first = (int)((t - first_tile(x.k0, s, kKeys)) * kKeys);
-    if (first >= x.nk)
+    const Work tile = work_of<true>(a, kKeys, blockIdx.x / a.kv_heads);
+    if (!tile.any)
         return;
+    const Seq &x = tile.x;
+    const int first = tile.first;
 
     const int lane = threadIdx.x & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keys = wave & 1, half = wave >> 1;
