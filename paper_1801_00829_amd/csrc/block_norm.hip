@@ -21,7 +21,7 @@ using namespace fuse;
 constexpr int V = 8;                       // columns per thread and step
 constexpr int kMaxCols = 32768;            // 1024 threads x 4 steps
 constexpr int kMaxThreads = 1024;
-constexpr int kGradBlocks = 256;           // blocks of a gradient call: each leaves one partial row of every column sum
+constexpr int kGradBlocks = 512;           // blocks of a gradient call: each leaves one partial row of every column sum
 
 struct Gate {
     int kind;                              // 0: none, 1: per column, 2: per row, 3: per cell
@@ -63,67 +63,88 @@ __device__ __forceinline__ int col_of(int k, int j, int lane, int group)
     return VEC ? (k * group + lane) * V + j : (k * V + j) * group + lane;
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_row(const T *__restrict__ p, int k, int lane, int group, int cols,
-                                         typename acc_of<T>::type (&v)[V])
-{
+// A thread's part of a row as it lies in memory: what is loaded ahead of its use stays in the row's own type.
+template <typename T, int K>
+struct Part {
+    struct alignas(16) Pack { T t[16 / sizeof(T)]; };
+    static constexpr int N = 16 / sizeof(T);
     using A = typename acc_of<T>::type;
-    if (VEC) {
-        const int c = col_of<true>(k, 0, lane, group);
-        if (c < cols) {
-            struct alignas(16) Pack { T t[16 / sizeof(T)]; };
-            constexpr int N = 16 / sizeof(T);
+    Pack v[K][V / N];
+
+    __device__ __forceinline__ A at(int k, int j) const { return (A)v[k][j / N].t[j % N]; }
+
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-            for (int i = 0; i < V / N; ++i) {
-                const Pack q = *reinterpret_cast<const Pack *>(p + c + i * N);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    v[i * N + j] = (A)q.t[j];
-            }
-        } else {
+        for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                v[j] = (A)0;
-        }
-    } else {
+                v[k][j / N].t[j % N] = (T)0;
+    }
+
+    // 0 behind the row's end
+    template <bool VEC>
+    __device__ __forceinline__ void load(const void *p_, int lane, int group, int cols)
+    {
+        const T *__restrict__ p = static_cast<const T *>(p_);
+        clear();
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = col_of<false>(k, j, lane, group);
-            v[j] = c < cols ? (A)p[c] : (A)0;
+        for (int k = 0; k < K; ++k) {
+            if (VEC) {
+                const int c = col_of<true>(k, 0, lane, group);
+                if (c < cols)
+#pragma unroll
+                    for (int i = 0; i < V / N; ++i)
+                        v[k][i] = *reinterpret_cast<const Pack *>(p + c + i * N);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const int c = col_of<false>(k, j, lane, group);
+                    if (c < cols)
+                        v[k][j / N].t[j % N] = p[c];
+                }
+            }
+        }
+    }
+};
+
+template <typename T, int K, bool VEC>
+__device__ __forceinline__ void store_row(void *p_, int lane, int group, int cols, const typename acc_of<T>::type (&v)[K][V])
+{
+    T *__restrict__ p = static_cast<T *>(p_);
+    using P = Part<T, K>;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (VEC) {
+            const int c = col_of<true>(k, 0, lane, group);
+            if (c < cols)
+#pragma unroll
+                for (int i = 0; i < V / P::N; ++i) {
+                    typename P::Pack q;
+#pragma unroll
+                    for (int j = 0; j < P::N; ++j)
+                        q.t[j] = (T)v[k][i * P::N + j];
+                    *reinterpret_cast<typename P::Pack *>(p + c + i * P::N) = q;
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = col_of<false>(k, j, lane, group);
+                if (c < cols)
+                    p[c] = (T)v[k][j];
+            }
         }
     }
 }
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_row(T *__restrict__ p, int k, int lane, int group, int cols,
-                                          const typename acc_of<T>::type (&v)[V])
+template <typename T>
+__device__ __forceinline__ const T *row_at(const void *p, long long row, long long ld)
 {
-    if (VEC) {
-        const int c = col_of<true>(k, 0, lane, group);
-        if (c < cols) {
-            struct alignas(16) Pack { T t[16 / sizeof(T)]; };
-            constexpr int N = 16 / sizeof(T);
-#pragma unroll
-            for (int i = 0; i < V / N; ++i) {
-                Pack q;
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    q.t[j] = (T)v[i * N + j];
-                *reinterpret_cast<Pack *>(p + c + i * N) = q;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = col_of<false>(k, j, lane, group);
-            if (c < cols)
-                p[c] = (T)v[j];
-        }
-    }
+    return static_cast<const T *>(p) + row * ld;
 }
 
 // Sums over a row's group of threads of N values at once; every thread of the block calls it (rows behind the last one with
-// zeros), and two calls in a row take different `buf`s, so that one barrier per sum is enough.
+// zeros).  Each sum of a row has its own buffer, and rows take two sets of them in turn, so one barrier per sum is enough.
 template <typename A, int N>
 __device__ __forceinline__ void group_sum(A (&v)[N], int group, A *buf)
 {
@@ -138,190 +159,169 @@ __device__ __forceinline__ void group_sum(A (&v)[N], int group, A *buf)
         for (int i = 0; i < N; ++i)
             buf[wave * N + i] = v[i];
     __syncthreads();
-    const int per = group >> 6, first = wave / per * per;
+    // one load: every sixteen lanes take a sum of each of the group's waves, sixteen at most
+    const int per = group >> 6, first = wave / per * per, other = threadIdx.x & 15;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        v[i] = buf[first * N + i];
-    for (int w = 1; w < per; ++w)
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            v[i] += buf[(first + w) * N + i];
+    for (int i = 0; i < N; ++i) {
+        v[i] = other < per ? buf[(first + other) * N + i] : (A)0;
+        v[i] = sum_of_16(v[i]);
+    }
 }
 
-template <typename A> struct Stats {
-    A mean, r;
-};
+constexpr int kWaves = kMaxThreads / 64;
 
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
 
-template <typename A, int K, bool VEC, bool LAYER>
-__device__ __forceinline__ Stats<A> stats_of(const A (&v)[K][V], int lane, int group, int cols, A eps, A *buf)
+// v[k][j] - mean, 0 behind the row's end
+template <bool VEC, bool LAYER, typename A>
+__device__ __forceinline__ A centred(A v, A mean, int k, int j, int lane, int group, int cols)
 {
-    Stats<A> st;
-    st.mean = (A)0;
-    A s[1] = {(A)0};
-    if (LAYER) {
+    return LAYER ? (col_of<VEC>(k, j, lane, group) < cols ? v - mean : (A)0) : v;
+}
+
+// Rows are taken by persistent blocks, a group's next row loaded while this one is worked on; weights stay in registers.
+template <typename T, int K, bool VEC, bool LAYER>
+__global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads) block_norm_kernel(const FwdArgs a)
+{
+    using A = typename acc_of<T>::type;
+    __shared__ A buf[2][4][kWaves];
+    const int group = a.group, per_block = blockDim.x / group, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / group);
+    const int lane = threadIdx.x - mine * group;               // (groups are whole waves: rows are the same for all lanes of one)
+    const int cols = a.cols;
+    const A scale = (A)a.scale, eps = (A)a.eps;
+    Part<T, K> post_w, pre_w, post_b, pre_b, gate, x, z;
+    if (a.post_w)
+        post_w.template load<VEC>(a.post_w, lane, group, cols);
+    if (a.pre_w)
+        pre_w.template load<VEC>(a.pre_w, lane, group, cols);
+    if (LAYER && a.post_b)
+        post_b.template load<VEC>(a.post_b, lane, group, cols);
+    if (LAYER && a.pre_b)
+        pre_b.template load<VEC>(a.pre_b, lane, group, cols);
+    if (a.gate.kind == 1)
+        gate.template load<VEC>(a.gate.p, lane, group, cols);
+    const long long stride = (long long)gridDim.x * per_block;
+    auto load = [&](long long row) {
+        if (row < a.rows) {
+            x.template load<VEC>(row_at<T>(a.x, row, a.x_ld), lane, group, cols);
+            if (a.z)
+                z.template load<VEC>(row_at<T>(a.z, row, a.z_ld), lane, group, cols);
+        } else {
+            x.clear();
+            z.clear();
+        }
+    };
+    long long row = (long long)blockIdx.x * per_block + mine;
+    load(row);
+    for (int turn = 0; row - mine < a.rows; row += stride, turn ^= 1) {
+        const bool in = row < a.rows;
+        A h[K][V];
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                s[0] += v[k][j];
-        group_sum<A, 1>(s, group, buf);
-        st.mean = s[0] / (A)cols;
-        s[0] = (A)0;
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const A d = LAYER ? (col_of<VEC>(k, j, lane, group) < cols ? v[k][j] - st.mean : (A)0) : v[k][j];
-            s[0] += d * d;
-        }
-    group_sum<A, 1>(s, group, buf + 32);
-    st.r = inv_sqrt(s[0] / (A)cols + eps);
-    return st;
-}
-
-template <typename T, bool VEC>
-__device__ __forceinline__ void gate_of(const Gate &gate, long long row, int k, int lane, int group, int cols,
-                                        typename acc_of<T>::type (&g)[V])
-{
-    using A = typename acc_of<T>::type;
-    const T *p = static_cast<const T *>(gate.p);
-    if (gate.kind == 1 || gate.kind == 3) {
-        load_row<T, VEC>(gate.kind == 1 ? p : p + row * gate.ld, k, lane, group, cols, g);
-    } else {
-        const A s = gate.kind == 2 ? (A)p[row * gate.ld] : (A)1;
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            g[j] = s;
-    }
-}
-
-template <typename T, int K, bool VEC, bool LAYER>
-__global__ void __launch_bounds__(kMaxThreads) block_norm_kernel(const FwdArgs a)
-{
-    using A = typename acc_of<T>::type;
-    __shared__ A buf[2][64];               // one half per norm
-    const int group = a.group, per_block = blockDim.x / group, lane = threadIdx.x % group;
-    for (long long first = (long long)blockIdx.x * per_block; first < a.rows; first += (long long)gridDim.x * per_block) {
-        const long long row = first + threadIdx.x / group;
-        const bool in = row < a.rows;
-        A h[K][V], u[K][V];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (in) {
-                load_row<T, VEC>(static_cast<const T *>(a.x) + row * a.x_ld, k, lane, group, a.cols, h[k]);
-                if (a.z)
-                    load_row<T, VEC>(static_cast<const T *>(a.z) + row * a.z_ld, k, lane, group, a.cols, u[k]);
-            }
-            if (!in || !a.z)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    u[k][j] = (A)0;
-                    if (!in)
-                        h[k][j] = (A)0;
-                }
-        }
+                h[k][j] = x.at(k, j);
         if (a.z) {
-            if (a.post_w) {
-                const Stats<A> st = stats_of<A, K, VEC, LAYER>(u, lane, group, a.cols, (A)a.eps, buf[0]);
+            A u[K][V];
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    A w[V], b[V];
-                    load_row<T, VEC>(static_cast<const T *>(a.post_w), k, lane, group, a.cols, w);
-                    if (LAYER && a.post_b)
-                        load_row<T, VEC>(static_cast<const T *>(a.post_b), k, lane, group, a.cols, b);
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    u[k][j] = z.at(k, j);
+            if (a.gate.kind == 3 && in)
+                gate.template load<VEC>(row_at<T>(a.gate.p, row, a.gate.ld), lane, group, cols);
+            A each = scale;
+            if (a.gate.kind == 2 && in)
+                each *= (A)*row_at<T>(a.gate.p, row, a.gate.ld);
+            load(row + stride);
+            if (a.post_w) {
+                A mean = (A)0, s[1] = {(A)0};
+                if (LAYER) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+#pragma unroll
+                        for (int j = 0; j < V; ++j)
+                            s[0] += u[k][j];
+                    group_sum<A, 1>(s, group, buf[turn][0]);
+                    mean = s[0] / (A)cols;
+                    s[0] = (A)0;
+                }
+#pragma unroll
+                for (int k = 0; k < K; ++k)
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        u[k][j] = (u[k][j] - st.mean) * st.r * w[j];
-                        if (LAYER && a.post_b)
-                            u[k][j] += b[j];
+                        u[k][j] = centred<VEC, LAYER>(u[k][j], mean, k, j, lane, group, cols);
+                        s[0] += u[k][j] * u[k][j];
                     }
-                }
-            }
+                group_sum<A, 1>(s, group, buf[turn][1]);
+                const A r = inv_sqrt(s[0] / (A)cols + eps);
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                if (in) {
-                    A g[V];
-                    gate_of<T, VEC>(a.gate, row, k, lane, group, a.cols, g);
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        u[k][j] = u[k][j] * r * post_w.at(k, j);
+                        if (LAYER && a.post_b)
+                            u[k][j] += post_b.at(k, j);
+                    }
+            }
+            if (a.gate.kind == 1 || a.gate.kind == 3)
+#pragma unroll
+                for (int k = 0; k < K; ++k)
 #pragma unroll
                     for (int j = 0; j < V; ++j)
-                        if (col_of<VEC>(k, j, lane, group) < a.cols)
-                            h[k][j] += (A)a.scale * g[j] * u[k][j];
-                    if (a.h)
-                        store_row<T, VEC>(static_cast<T *>(a.h) + row * a.h_ld, k, lane, group, a.cols, h[k]);
-                }
-            }
+                        u[k][j] *= gate.at(k, j);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    h[k][j] += each * u[k][j];
+            if (a.h && in)
+                store_row<T, K, VEC>(static_cast<T *>(a.h) + row * a.h_ld, lane, group, cols, h);
+        } else {
+            load(row + stride);
         }
         if (a.y) {
             // the norm is that of h before its rounding: it is in registers, and y is rounded once
-            const Stats<A> st = stats_of<A, K, VEC, LAYER>(h, lane, group, a.cols, (A)a.eps, buf[1]);
+            A mean = (A)0, s[1] = {(A)0};
+            if (LAYER) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                A w[V], b[V], y[V];
-                load_row<T, VEC>(static_cast<const T *>(a.pre_w), k, lane, group, a.cols, w);
-                if (LAYER && a.pre_b)
-                    load_row<T, VEC>(static_cast<const T *>(a.pre_b), k, lane, group, a.cols, b);
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        s[0] += col_of<VEC>(k, j, lane, group) < cols ? h[k][j] : (A)0;
+                group_sum<A, 1>(s, group, buf[turn][2]);
+                mean = s[0] / (A)cols;
+                s[0] = (A)0;
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    y[j] = (h[k][j] - st.mean) * st.r * w[j];
-                    if (LAYER && a.pre_b)
-                        y[j] += b[j];
+                    h[k][j] = col_of<VEC>(k, j, lane, group) < cols ? h[k][j] - mean : (A)0;
+                    s[0] += h[k][j] * h[k][j];
                 }
-                if (in)
-                    store_row<T, VEC>(static_cast<T *>(a.y) + row * a.y_ld, k, lane, group, a.cols, y);
-            }
-        }
-        if (group > 64)
-            __syncthreads();               // the next rows' sums take the same buffers
-    }
-}
-
-// d = r (g - n mean(g n) [- mean(g)]) with g = dy o w, and the terms of the two column sums.
-template <typename T, int K, bool VEC, bool LAYER>
-__device__ __forceinline__ void norm_back(const typename acc_of<T>::type (&v)[K][V], typename acc_of<T>::type (&dy)[K][V],
-                                          const T *w_, bool in, int lane, int group, int cols, double eps,
-                                          typename acc_of<T>::type (&sum_w)[K][V], typename acc_of<T>::type (&sum_b)[LAYER ? K : 1][V],
-                                          typename acc_of<T>::type *buf)
-{
-    using A = typename acc_of<T>::type;
-    Stats<A> st = stats_of<A, K, VEC, LAYER>(v, lane, group, cols, (A)eps, buf);
-    if (!in)
-        st.r = (A)0;                       // a row behind the last one adds 0 to the column sums, eps = 0 included
-    A s[2] = {(A)0, (A)0};
+            group_sum<A, 1>(s, group, buf[turn][3]);
+            const A r = inv_sqrt(s[0] / (A)cols + eps);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        A w[V];
-        load_row<T, VEC>(w_, k, lane, group, cols, w);
+            for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const A n = (v[k][j] - st.mean) * st.r;
-            if (LAYER)
-                sum_b[LAYER ? k : 0][j] += dy[k][j];
-            sum_w[k][j] += dy[k][j] * n;
-            dy[k][j] *= w[j];
-            s[0] += dy[k][j] * n;          // (0 behind the row's end: dy is)
-            if (LAYER)
-                s[1] += dy[k][j];
+                for (int j = 0; j < V; ++j) {
+                    h[k][j] = h[k][j] * r * pre_w.at(k, j);
+                    if (LAYER && a.pre_b)
+                        h[k][j] += pre_b.at(k, j);
+                }
+            if (in)
+                store_row<T, K, VEC>(static_cast<T *>(a.y) + row * a.y_ld, lane, group, cols, h);
         }
     }
-    group_sum<A, 2>(s, group, buf + 64);
-    s[0] /= (A)cols;
-    s[1] = LAYER ? s[1] / (A)cols : (A)0;
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            dy[k][j] = st.r * (dy[k][j] - (v[k][j] - st.mean) * st.r * s[0] - s[1]);
 }
 
 // One block's rows of a column sum: the groups of a block are added in order, then the block's partial row is written.
 template <typename A, int K, bool VEC>
-__device__ __forceinline__ void leave_sum(const A (&v)[K][V], int lane, int group, int cols, A *out, A *add)
+__device__ __forceinline__ void leave_sum(const A (&v)[K][V], int lane, int mine, int group, int cols, A *out, A *add)
 {
-    const int per_block = blockDim.x / group, mine = threadIdx.x / group;
+    const int per_block = blockDim.x / group;
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -341,125 +341,183 @@ __device__ __forceinline__ void leave_sum(const A (&v)[K][V], int lane, int grou
         }
 }
 
+// Three sums per row at most: means (layer norms only); squares of h and z and what dy needs of h; what du needs of z.  The row after
+// this one is loaded meanwhile.
 template <typename T, int K, bool VEC, bool LAYER>
-__global__ void __launch_bounds__(kMaxThreads) block_norm_grad_kernel(const BwdArgs a)
+__global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads) block_norm_grad_kernel(const BwdArgs a)
 {
     using A = typename acc_of<T>::type;
-    __shared__ A buf[2][96];
+    __shared__ A buf[2][3][kWaves * 4];
     __shared__ A add[kMaxThreads];
-    const int group = a.group, per_block = blockDim.x / group, lane = threadIdx.x % group;
+    const int group = a.group, per_block = blockDim.x / group, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / group);
+    const int lane = threadIdx.x - mine * group;               // (groups are whole waves: rows are the same for all lanes of one)
+    const int cols = a.cols;
+    const A scale = (A)a.scale, eps = (A)a.eps, inv = (A)1 / (A)cols;
     A sum_pre[K][V] = {}, sum_post[K][V] = {}, sum_gate[K][V] = {};
     A sum_pre_b[LAYER ? K : 1][V] = {}, sum_post_b[LAYER ? K : 1][V] = {};
-    for (long long first = (long long)blockIdx.x * per_block; first < a.rows; first += (long long)gridDim.x * per_block) {
-        const long long row = first + threadIdx.x / group;
+    Part<T, K> post_w, post_b, pre_w, gate, ph, pdy, pdh, pz;
+    if (a.post_w)
+        post_w.template load<VEC>(a.post_w, lane, group, cols);
+    if (LAYER && a.post_b)
+        post_b.template load<VEC>(a.post_b, lane, group, cols);
+    if (a.pre_w)
+        pre_w.template load<VEC>(a.pre_w, lane, group, cols);
+    if (a.gate.kind == 1)
+        gate.template load<VEC>(a.gate.p, lane, group, cols);
+    const long long stride = (long long)gridDim.x * per_block;
+    auto load = [&](long long row) {
         const bool in = row < a.rows;
-        A v[K][V], d[K][V];                // h and dy, then z and dx
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (in && a.dy) {
-                load_row<T, VEC>(static_cast<const T *>(a.h) + row * a.h_ld, k, lane, group, a.cols, v[k]);
-                load_row<T, VEC>(static_cast<const T *>(a.dy) + row * a.dy_ld, k, lane, group, a.cols, d[k]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    v[k][j] = d[k][j] = (A)0;
-            }
+        if (in && a.dy) {
+            ph.template load<VEC>(row_at<T>(a.h, row, a.h_ld), lane, group, cols);
+            pdy.template load<VEC>(row_at<T>(a.dy, row, a.dy_ld), lane, group, cols);
+        } else {
+            ph.clear();
+            pdy.clear();
         }
-        if (a.dy)
-            norm_back<T, K, VEC, LAYER>(v, d, static_cast<const T *>(a.pre_w), in, lane, group, a.cols, a.eps, sum_pre, sum_pre_b, buf[0]);
+        if (in && a.dh)
+            pdh.template load<VEC>(row_at<T>(a.dh, row, a.dh_ld), lane, group, cols);
+        else
+            pdh.clear();
+        if (in && a.z)
+            pz.template load<VEC>(row_at<T>(a.z, row, a.z_ld), lane, group, cols);
+        else
+            pz.clear();
+    };
+    long long row = (long long)blockIdx.x * per_block + mine;
+    load(row);
+    for (int turn = 0; row - mine < a.rows; row += stride, turn ^= 1) {
+        const bool in = row < a.rows;
+        A n[K][V], d[K][V], z[K][V];       // h, then normalised; dy o w, then dx, then the gradient of u; z
+        if (a.gate.kind == 3 && in)
+            gate.template load<VEC>(row_at<T>(a.gate.p, row, a.gate.ld), lane, group, cols);
+        A each = (A)1;
+        if (a.gate.kind == 2 && in)
+            each = (A)*row_at<T>(a.gate.p, row, a.gate.ld);
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (in && a.dh) {
-                A t[V];
-                load_row<T, VEC>(static_cast<const T *>(a.dh) + row * a.dh_ld, k, lane, group, a.cols, t);
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    d[k][j] += t[j];
+            for (int j = 0; j < V; ++j) {
+                n[k][j] = ph.at(k, j);
+                z[k][j] = pz.at(k, j);
+                d[k][j] = pdy.at(k, j);
             }
-            if (in && a.dx)
-                store_row<T, VEC>(static_cast<T *>(a.dx) + row * a.dx_ld, k, lane, group, a.cols, d[k]);
+        if (LAYER) {
+            A s[2] = {(A)0, (A)0};
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                d[k][j] = in && col_of<VEC>(k, j, lane, group) < a.cols ? d[k][j] * (A)a.scale : (A)0;
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    s[0] += n[k][j];
+                    s[1] += z[k][j];
+                }
+            group_sum<A, 2>(s, group, buf[turn][0]);
+            const A mh = s[0] / (A)cols, mz = a.post_w ? s[1] / (A)cols : (A)0;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    n[k][j] = centred<VEC, true>(n[k][j], mh, k, j, lane, group, cols);
+                    z[k][j] = centred<VEC, true>(z[k][j], mz, k, j, lane, group, cols);
+                }
         }
+        A s[4] = {(A)0, (A)0, (A)0, (A)0}; // squares of h, squares of z, sum of dy o w o h, sum of dy o w
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                s[0] += n[k][j] * n[k][j];
+                s[1] += z[k][j] * z[k][j];
+                const A g = d[k][j] * (a.dy ? pre_w.at(k, j) : (A)0);
+                s[2] += g * n[k][j];
+                s[3] += g;
+            }
+        group_sum<A, 4>(s, group, buf[turn][1]);
+        // (a row behind the last one adds 0 to the column sums, eps = 0 included)
+        const A rh = in ? inv_sqrt(s[0] / (A)cols + eps) : (A)0, rz = in ? inv_sqrt(s[1] / (A)cols + eps) : (A)0;
+        const A with_h = s[2] * rh * inv, with_1 = LAYER ? s[3] * inv : (A)0;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const A dy = d[k][j];
+                d[k][j] = pdh.at(k, j);
+                if (a.dy) {
+                    n[k][j] *= rh;
+                    sum_pre[k][j] += dy * n[k][j];
+                    if (LAYER)
+                        sum_pre_b[LAYER ? k : 0][j] += dy;
+                    d[k][j] += rh * (dy * pre_w.at(k, j) - n[k][j] * with_h - with_1);
+                }
+            }
+        if (K == 1)
+            load(row + stride);            // (the registers of longer rows do not hold two of them)
+        if (in && a.dx)
+            store_row<T, K, VEC>(static_cast<T *>(a.dx) + row * a.dx_ld, lane, group, cols, d);
         if (a.z) {
+            // d: gradient of u o gate, then of u
+            A sz[3] = {(A)0, (A)0, (A)0};  // sum of du o w o z, sum of du o w, sum of the gate's gradient
+            A t[K][V];
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                if (in)
-                    load_row<T, VEC>(static_cast<const T *>(a.z) + row * a.z_ld, k, lane, group, a.cols, v[k]);
-                else
+            for (int k = 0; k < K; ++k)
 #pragma unroll
-                    for (int j = 0; j < V; ++j)
-                        v[k][j] = (A)0;
-            }
-            if (a.gate.kind != 0) {
-                // dgate needs u, the gate's other factor; then d becomes the gradient of u
-                Stats<A> st;
-                st.mean = (A)0;
-                st.r = (A)1;
-                if (a.post_w)
-                    st = stats_of<A, K, VEC, LAYER>(v, lane, group, a.cols, (A)a.eps, buf[1]);
-                A s[1] = {(A)0};
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    A w[V], b[V], g[V], t[V];
+                for (int j = 0; j < V; ++j) {
+                    d[k][j] = in && col_of<VEC>(k, j, lane, group) < cols ? d[k][j] * scale : (A)0;
                     if (a.post_w)
-                        load_row<T, VEC>(static_cast<const T *>(a.post_w), k, lane, group, a.cols, w);
-                    if (LAYER && a.post_b)
-                        load_row<T, VEC>(static_cast<const T *>(a.post_b), k, lane, group, a.cols, b);
-                    if (in)
-                        gate_of<T, VEC>(a.gate, row, k, lane, group, a.cols, g);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        A u = (v[k][j] - st.mean) * st.r;
+                        z[k][j] *= rz;
+                    if (a.gate.kind != 0) {
+                        A u = z[k][j];
                         if (a.post_w)
-                            u *= w[j];
+                            u *= post_w.at(k, j);
                         if (LAYER && a.post_b)
-                            u += b[j];
-                        t[j] = in ? d[k][j] * u : (A)0;
-                        s[0] += t[j];
-                        d[k][j] = in ? d[k][j] * g[j] : (A)0;
+                            u += post_b.at(k, j);
+                        t[k][j] = in ? d[k][j] * u : (A)0;
+                        sz[2] += t[k][j];
+                        if (a.gate.kind == 1)
+                            sum_gate[k][j] += t[k][j];
+                        d[k][j] *= a.gate.kind == 2 ? each : in ? gate.at(k, j) : (A)0;
                     }
-                    if (a.gate.kind == 1)
-#pragma unroll
-                        for (int j = 0; j < V; ++j)
-                            sum_gate[k][j] += t[j];
-                    else if (a.gate.kind == 3 && in && a.dgate)
-                        store_row<T, VEC>(static_cast<T *>(a.dgate) + row * a.dgate_ld, k, lane, group, a.cols, t);
+                    if (a.post_w) {
+                        sum_post[k][j] += d[k][j] * z[k][j];
+                        if (LAYER)
+                            sum_post_b[LAYER ? k : 0][j] += d[k][j];
+                        d[k][j] *= post_w.at(k, j);
+                        sz[0] += d[k][j] * z[k][j];
+                        sz[1] += d[k][j];
+                    }
                 }
-                if (a.gate.kind == 2 && a.dgate) {
-                    if (group > 64)
-                        __syncthreads();   // (the sums of the statistics have been read)
-                    group_sum<A, 1>(s, group, buf[1] + 64);
-                    if (in && lane == 0)
-                        static_cast<T *>(a.dgate)[row * a.dgate_ld] = (T)s[0];
-                }
-                if (group > 64)
-                    __syncthreads();
-            }
-            if (a.post_w)
-                norm_back<T, K, VEC, LAYER>(v, d, static_cast<const T *>(a.post_w), in, lane, group, a.cols, a.eps, sum_post, sum_post_b, buf[1]);
-            if (in && a.dz)
+            if (a.gate.kind == 3 && in && a.dgate)
+                store_row<T, K, VEC>(static_cast<T *>(a.dgate) + row * a.dgate_ld, lane, group, cols, t);
+            if (a.post_w || a.gate.kind == 2)
+                group_sum<A, 3>(sz, group, buf[turn][2]);
+            if (a.gate.kind == 2 && a.dgate && in && lane == 0)
+                static_cast<T *>(a.dgate)[row * a.dgate_ld] = (T)sz[2];
+            if (a.post_w) {
+                const A with_z = sz[0] * inv, with_one = LAYER ? sz[1] * inv : (A)0;
 #pragma unroll
                 for (int k = 0; k < K; ++k)
-                    store_row<T, VEC>(static_cast<T *>(a.dz) + row * a.dz_ld, k, lane, group, a.cols, d[k]);
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        d[k][j] = rz * (d[k][j] - z[k][j] * with_z - with_one);
+            }
+            if (in && a.dz)
+                store_row<T, K, VEC>(static_cast<T *>(a.dz) + row * a.dz_ld, lane, group, cols, d);
         }
-        if (group > 64)
-            __syncthreads();
+        if (K > 1)
+            load(row + stride);
     }
-    A *out = static_cast<A *>(a.partial) + (long long)blockIdx.x * a.cols;
-    const long long step = (long long)gridDim.x * a.cols;
+    A *out = static_cast<A *>(a.partial) + (long long)blockIdx.x * cols;
+    const long long step = (long long)gridDim.x * cols;
     if (a.want_dpre_w)
-        leave_sum<A, K, VEC>(sum_pre, lane, group, a.cols, out, add);
+        leave_sum<A, K, VEC>(sum_pre, lane, mine, group, cols, out, add);
     if (a.want_dpost_w)
-        leave_sum<A, K, VEC>(sum_post, lane, group, a.cols, out + step, add);
+        leave_sum<A, K, VEC>(sum_post, lane, mine, group, cols, out + step, add);
     if (a.gate.kind == 1 && a.dgate)
-        leave_sum<A, K, VEC>(sum_gate, lane, group, a.cols, out + 2 * step, add);
+        leave_sum<A, K, VEC>(sum_gate, lane, mine, group, cols, out + 2 * step, add);
     if (LAYER) {
         if (a.want_dpre_b)
-            leave_sum<A, LAYER ? K : 1, VEC>(sum_pre_b, lane, group, a.cols, out + 3 * step, add);
+            leave_sum<A, LAYER ? K : 1, VEC>(sum_pre_b, lane, mine, group, cols, out + 3 * step, add);
         if (a.want_dpost_b)
-            leave_sum<A, LAYER ? K : 1, VEC>(sum_post_b, lane, group, a.cols, out + 4 * step, add);
+            leave_sum<A, LAYER ? K : 1, VEC>(sum_post_b, lane, mine, group, cols, out + 4 * step, add);
     }
 }
 
@@ -476,6 +534,7 @@ __global__ void __launch_bounds__(1024) block_norm_sums_kernel(const SumArgs a)
     const int per = (a.blocks + 15) / 16, end = min(a.blocks, (slice + 1) * per);
     A s = (A)0;
     if (c < a.cols)
+#pragma unroll 8
         for (int b = slice * per; b < end; ++b)
             s += p[(long long)b * a.cols + c];
     part[slice][threadIdx.x & 63] = s;
@@ -488,24 +547,26 @@ __global__ void __launch_bounds__(1024) block_norm_sums_kernel(const SumArgs a)
     }
 }
 
-// Threads per row: a wave or a power of two of them, so that a row of up to 8192 columns is one step.
+// Steps of eight columns per thread, and threads per row: whole waves, as few as that takes.  Blocks of 512 threads leave a thread 256
+// registers, which hold a gradient call's sums and two rows of one step each; the longest rows take 1024.
+int steps_for(int64_t cols) { return cols <= 512 * V ? 1 : cols <= 1024 * V ? 2 : 4; }
+
 int group_for(int64_t cols)
 {
-    int g = 64;
-    while (g < kMaxThreads && (int64_t)g * V < cols)
-        g *= 2;
-    return g;
+    const int64_t per = 64 * V * steps_for(cols);
+    return (int)((cols + per - 1) / per) * 64;
 }
 
-int steps_for(int64_t cols)
+// Threads per block: as many groups as 512 hold, at least one.
+int threads_for(int64_t cols)
 {
-    const int64_t k = (cols + (int64_t)V * kMaxThreads - 1) / ((int64_t)V * kMaxThreads);
-    return k <= 1 ? 1 : k <= 2 ? 2 : 4;
+    const int g = group_for(cols);
+    return g >= 512 ? g : 512 / g * g;
 }
 
 int grad_blocks(const fuse_block *b)
 {
-    const int64_t per = kMaxThreads / group_for(b->cols), want = (b->rows + per - 1) / per;
+    const int64_t per = threads_for(b->cols) / group_for(b->cols), want = (b->rows + per - 1) / per;
     return (int)(want < 1 ? 1 : want > kGradBlocks ? kGradBlocks : want);
 }
 
@@ -654,9 +715,9 @@ int norm_impl(const fuse_block *b, const void *x, int64_t x_ld, void *h, int64_t
     a.gate = {gate_code(b), b->gate, b->gate_ld};
     a.eps = b->eps, a.scale = b->scale;
     const bool vec = block_on_16(b) && rows_on_16(b, x, x_ld) && rows_on_16(b, h, h_ld) && rows_on_16(b, y, y_ld);
-    const int threads = a.group < 256 ? 256 : a.group, per = threads / a.group;
-    const int64_t want = (b->rows + per - 1) / per;
-    const unsigned blocks = (unsigned)(want > 65536 ? 65536 : want);
+    const int threads = threads_for(b->cols), per = threads / a.group;
+    const int64_t want = (b->rows + per - 1) / per, most = 256 * (2048 / threads);
+    const unsigned blocks = (unsigned)(want > most ? most : want);
     FUSE_BY_DTYPE(b->dtype, launch_fwd, a, b->norm == FUSE_NORM_LAYER, steps_for(b->cols), vec, blocks, threads, (hipStream_t)stream);
     return launched("block_norm_kernel");
 }
@@ -709,7 +770,7 @@ int norm_grad_impl(const fuse_block *b, const void *dh, int64_t dh_ld, const voi
                      rows_on_16(b, g->dx, g->dx_ld) && rows_on_16(b, g->dz, g->dz_ld) &&
                      (b->gate_kind != FUSE_SIDE_MATRIX || rows_on_16(b, g->dgate, g->dgate_ld));
     const int blocks = grad_blocks(b);
-    FUSE_BY_DTYPE(b->dtype, launch_bwd, a, b->norm == FUSE_NORM_LAYER, steps_for(b->cols), vec, blocks, kMaxThreads, (hipStream_t)stream);
+    FUSE_BY_DTYPE(b->dtype, launch_bwd, a, b->norm == FUSE_NORM_LAYER, steps_for(b->cols), vec, blocks, threads_for(b->cols), (hipStream_t)stream);
     rc = launched("block_norm_grad_kernel");
     SumArgs sa;
     sa.partial = workspace, sa.blocks = blocks, sa.cols = (int)b->cols;

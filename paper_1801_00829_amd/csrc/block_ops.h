@@ -48,13 +48,51 @@ int guard(F f)
     }
 }
 
+// v of another lane of the same sixteen, by the pattern CTRL (a move within the registers: no LDS latency).
+template <int CTRL>
+__device__ __forceinline__ float moved(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double moved(double v)
+{
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, true),
+                            __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sum over each sixteen lanes, in all of them: neighbours, pairs, halves of eight and of sixteen.
+template <typename A>
+__device__ __forceinline__ A sum_of_16(A v)
+{
+    v += moved<0xB1>(v);                   // lanes 1 0 3 2
+    v += moved<0x4E>(v);                   // lanes 2 3 0 1
+    v += moved<0x141>(v);                  // mirrored within eight
+    v += moved<0x140>(v);                  // mirrored within sixteen
+    return v;
+}
+
+// Sum of the two values that a swap of v with itself leaves: v of lane l and of the lane 16, or 32, away.
+template <int WIDTH>
+__device__ __forceinline__ float swapped_sum(float v)
+{
+    const unsigned u = __float_as_uint(v);
+    const auto r = WIDTH == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <int WIDTH>
+__device__ __forceinline__ double swapped_sum(double v)
+{
+    const unsigned lo = (unsigned)__double2loint(v), hi = (unsigned)__double2hiint(v);
+    const auto l = WIDTH == 16 ? __builtin_amdgcn_permlane16_swap(lo, lo, false, false) : __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+    const auto h = WIDTH == 16 ? __builtin_amdgcn_permlane16_swap(hi, hi, false, false) : __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+    return __hiloint2double((int)h[0], (int)l[0]) + __hiloint2double((int)h[1], (int)l[1]);
+}
+
 template <typename A>
 __device__ __forceinline__ A wave_sum(A v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-        v += __shfl_xor(v, o, 64);
-    return v;
+    return swapped_sum<32>(swapped_sum<16>(sum_of_16(v)));
 }
 
 }  // namespace fuse
