@@ -82,6 +82,20 @@ struct Part {
                 v[k][j / N].t[j % N] = (T)0;
     }
 
+    // Kept as it is: its values are converted where they are used, not once and for all in twice as many registers.
+    __device__ __forceinline__ void stay()
+    {
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V / N; ++i) {
+                u4 u = __builtin_bit_cast(u4, v[k][i]);
+                asm volatile("" : "+v"(u));
+                v[k][i] = __builtin_bit_cast(Pack, u);
+            }
+    }
+
     // 0 behind the row's end
     template <bool VEC>
     __device__ __forceinline__ void load(const void *p_, int lane, int group, int cols)
@@ -169,6 +183,12 @@ __device__ __forceinline__ void group_sum(A (&v)[N], int group, A *buf)
 }
 
 constexpr int kWaves = kMaxThreads / 64;
+
+// for all of a thread's columns
+#define FUSE_EACH(...)                                                                                                    \
+    do {                                                                                                                  \
+        _Pragma("unroll") for (int k = 0; k < K; ++k) _Pragma("unroll") for (int j = 0; j < V; ++j) { __VA_ARGS__; }      \
+    } while (0)
 
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
@@ -344,7 +364,7 @@ __device__ __forceinline__ void leave_sum(const A (&v)[K][V], int lane, int mine
 // Three sums per row at most: means (layer norms only); squares of h and z and what dy needs of h; what du needs of z.  The row after
 // this one is loaded meanwhile.
 template <typename T, int K, bool VEC, bool LAYER>
-__global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads) block_norm_grad_kernel(const BwdArgs a)
+__global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads, sizeof(T) == 2 && VEC && K == 1 ? 4 : 1) block_norm_grad_kernel(const BwdArgs a)
 {
     using A = typename acc_of<T>::type;
     __shared__ A buf[2][3][kWaves * 4];
@@ -387,6 +407,13 @@ __global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads) block_norm_grad_ker
     load(row);
     for (int turn = 0; row - mine < a.rows; row += stride, turn ^= 1) {
         const bool in = row < a.rows;
+        if (sizeof(T) == 2) {
+            post_w.stay();
+            pre_w.stay();
+            if (LAYER)
+                post_b.stay();
+            gate.stay();
+        }
         A n[K][V], d[K][V], z[K][V];       // h, then normalised; dy o w, then dx, then the gradient of u; z
         if (a.gate.kind == 3 && in)
             gate.template load<VEC>(row_at<T>(a.gate.p, row, a.gate.ld), lane, group, cols);
@@ -427,28 +454,24 @@ __global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads) block_norm_grad_ker
             for (int j = 0; j < V; ++j) {
                 s[0] += n[k][j] * n[k][j];
                 s[1] += z[k][j] * z[k][j];
-                const A g = d[k][j] * (a.dy ? pre_w.at(k, j) : (A)0);
-                s[2] += g * n[k][j];
-                s[3] += g;
             }
+        if (a.dy) {
+            FUSE_EACH(s[2] += d[k][j] * pre_w.at(k, j) * n[k][j]);
+            if (LAYER)
+                FUSE_EACH(s[3] += d[k][j] * pre_w.at(k, j));
+        }
         group_sum<A, 4>(s, group, buf[turn][1]);
         // (a row behind the last one adds 0 to the column sums, eps = 0 included)
         const A rh = in ? inv_sqrt(s[0] / (A)cols + eps) : (A)0, rz = in ? inv_sqrt(s[1] / (A)cols + eps) : (A)0;
         const A with_h = s[2] * rh * inv, with_1 = LAYER ? s[3] * inv : (A)0;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const A dy = d[k][j];
-                d[k][j] = pdh.at(k, j);
-                if (a.dy) {
-                    n[k][j] *= rh;
-                    sum_pre[k][j] += dy * n[k][j];
-                    if (LAYER)
-                        sum_pre_b[LAYER ? k : 0][j] += dy;
-                    d[k][j] += rh * (dy * pre_w.at(k, j) - n[k][j] * with_h - with_1);
-                }
-            }
+        if (a.dy) {
+            FUSE_EACH(n[k][j] *= rh);
+            FUSE_EACH(sum_pre[k][j] += d[k][j] * n[k][j]);
+            if (LAYER)
+                FUSE_EACH(sum_pre_b[LAYER ? k : 0][j] += d[k][j]);
+            FUSE_EACH(d[k][j] = rh * (d[k][j] * pre_w.at(k, j) - n[k][j] * with_h - with_1));
+        }
+        FUSE_EACH(d[k][j] += pdh.at(k, j));
         if (K == 1)
             load(row + stride);            // (the registers of longer rows do not hold two of them)
         if (in && a.dx)
@@ -456,35 +479,37 @@ __global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads) block_norm_grad_ker
         if (a.z) {
             // d: gradient of u o gate, then of u
             A sz[3] = {(A)0, (A)0, (A)0};  // sum of du o w o z, sum of du o w, sum of the gate's gradient
+            const A zs = a.post_w ? rz : (A)1, ds = in ? scale : (A)0;
+            FUSE_EACH(d[k][j] = col_of<VEC>(k, j, lane, group) < cols ? d[k][j] * ds : (A)0);
+            FUSE_EACH(z[k][j] *= zs);
             A t[K][V];
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    d[k][j] = in && col_of<VEC>(k, j, lane, group) < cols ? d[k][j] * scale : (A)0;
-                    if (a.post_w)
-                        z[k][j] *= rz;
-                    if (a.gate.kind != 0) {
-                        A u = z[k][j];
-                        if (a.post_w)
-                            u *= post_w.at(k, j);
-                        if (LAYER && a.post_b)
-                            u += post_b.at(k, j);
-                        t[k][j] = in ? d[k][j] * u : (A)0;
-                        sz[2] += t[k][j];
-                        if (a.gate.kind == 1)
-                            sum_gate[k][j] += t[k][j];
-                        d[k][j] *= a.gate.kind == 2 ? each : in ? gate.at(k, j) : (A)0;
-                    }
-                    if (a.post_w) {
-                        sum_post[k][j] += d[k][j] * z[k][j];
-                        if (LAYER)
-                            sum_post_b[LAYER ? k : 0][j] += d[k][j];
-                        d[k][j] *= post_w.at(k, j);
-                        sz[0] += d[k][j] * z[k][j];
-                        sz[1] += d[k][j];
-                    }
+            if (a.gate.kind != 0) {        // (branches are around the loops, not in them: the same for the whole call)
+                FUSE_EACH(t[k][j] = z[k][j]);
+                if (a.post_w)
+                    FUSE_EACH(t[k][j] *= post_w.at(k, j));
+                if (LAYER && a.post_b)
+                    FUSE_EACH(t[k][j] += post_b.at(k, j));
+                FUSE_EACH(t[k][j] *= d[k][j]);
+                if (!in)
+                    FUSE_EACH(t[k][j] = (A)0);
+                if (a.gate.kind == 1)
+                    FUSE_EACH(sum_gate[k][j] += t[k][j]);
+                if (a.gate.kind == 2) {
+                    FUSE_EACH(sz[2] += t[k][j]);
+                    FUSE_EACH(d[k][j] *= each);
+                } else if (in) {
+                    FUSE_EACH(d[k][j] *= gate.at(k, j));
                 }
+            }
+            if (a.post_w) {
+                FUSE_EACH(sum_post[k][j] += d[k][j] * z[k][j]);
+                if (LAYER)
+                    FUSE_EACH(sum_post_b[LAYER ? k : 0][j] += d[k][j]);
+                FUSE_EACH(d[k][j] *= post_w.at(k, j));
+                FUSE_EACH(sz[0] += d[k][j] * z[k][j]);
+                if (LAYER)
+                    FUSE_EACH(sz[1] += d[k][j]);
+            }
             if (a.gate.kind == 3 && in && a.dgate)
                 store_row<T, K, VEC>(static_cast<T *>(a.dgate) + row * a.dgate_ld, lane, group, cols, t);
             if (a.post_w || a.gate.kind == 2)
