@@ -428,6 +428,9 @@ __global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads, sizeof(T) == 2 && V
                 z[k][j] = pz.at(k, j);
                 d[k][j] = pdy.at(k, j);
             }
+        const Part<T, K> dh = pdh;
+        if (K == 1)
+            load(row + stride);            // (the registers of longer rows do not hold two of them)
         if (LAYER) {
             A s[2] = {(A)0, (A)0};
 #pragma unroll
@@ -471,9 +474,7 @@ __global__ void __launch_bounds__(K < 4 ? 512 : kMaxThreads, sizeof(T) == 2 && V
                 FUSE_EACH(sum_pre_b[LAYER ? k : 0][j] += d[k][j]);
             FUSE_EACH(d[k][j] = rh * (d[k][j] * pre_w.at(k, j) - n[k][j] * with_h - with_1));
         }
-        FUSE_EACH(d[k][j] += pdh.at(k, j));
-        if (K == 1)
-            load(row + stride);            // (the registers of longer rows do not hold two of them)
+        FUSE_EACH(d[k][j] += dh.at(k, j));
         if (in && a.dx)
             store_row<T, K, VEC>(static_cast<T *>(a.dx) + row * a.dx_ld, lane, group, cols, d);
         if (a.z) {
