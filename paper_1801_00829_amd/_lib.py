@@ -121,11 +121,11 @@ def load():
                        ("fuse_block_norm_backward", [P(Block), vp, i64, vp, i64, vp, i64, P(BlockGrads), vp, size, vp]),
                        ("fuse_attention", [P(Attn), vp, i64, i64, vp, vp, size, vp]),
                        ("fuse_attention_backward", [P(Attn), P(AttnGrads), vp, size, vp]),
-                       ("fuse_grad_norm", [P(Tensor), i64, vp, vp, size, vp]),
-                       ("fuse_grad_clip", [P(Tensor), i64, f64, f64, vp, vp, vp, size, vp])):
+                       ("fuse_grad_norm", [vp, i64, vp, vp, size, vp]),
+                       ("fuse_grad_clip", [vp, i64, f64, f64, vp, vp, vp, size, vp])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, ci
     for name, args in (("fuse_block_norm_backward_bytes", [P(Block)]), ("fuse_attention_bytes", [P(Attn)]),
-                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_grad_norm_bytes", [P(Tensor), i64])):
+                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_grad_norm_bytes", [vp, i64])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, size
     lib.fuse_last_error.restype = ctypes.c_char_p
     lib.fuse_last_kernel.restype = ctypes.c_char_p

@@ -10,7 +10,7 @@ from contextlib import contextmanager
 import torch
 
 from . import _lib as L
-from .api import SIDE, _check
+from .api import SIDE, _check, _raw_stream
 
 NORM = {"rms": 0, "layer": 1}
 DTYPE = {torch.float64: 0, torch.float32: 1, torch.bfloat16: 2, torch.float16: 3}
@@ -19,24 +19,37 @@ BlockGrads = namedtuple("BlockGrads", "dx dz dgate dpost dpost_bias dpre dpre_bi
 """Gradients of fuse_block_norm; None where the call had no such input."""
 
 
+def _handle(device, stream):
+    """The stream's handle where a call runs as things are: on the current device and its current stream.  None: see _on."""
+    if device.type != "cuda":
+        raise ValueError("tensors must be CUDA (HIP) tensors, got device %s" % device)
+    if stream is None and _raw_stream is not None and device.index == torch.cuda.current_device():
+        return _raw_stream(device.index)
+    return None
+
+
 @contextmanager
 def _on(device, stream):
     """The device, and the stream on it (default: its current one), that a call runs on; yields the stream's handle.
     Allocations inside belong to that stream."""
-    if device.type != "cuda":
-        raise ValueError("tensors must be CUDA (HIP) tensors, got device %s" % device)
     if stream is not None and not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     if stream is not None and stream.device != device:
         raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, device))
-    if stream is None and device.index == torch.cuda.current_device():
-        yield ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
-        return
     with torch.cuda.device(device):
         if stream is None:
             stream = torch.cuda.current_stream(device)
         with torch.cuda.stream(stream):
-            yield ctypes.c_void_p(stream.cuda_stream)
+            yield stream.cuda_stream
+
+
+def _run(device, stream, call):
+    """call(handle) on the device and stream."""
+    handle = _handle(device, stream)
+    if handle is not None:
+        return call(handle)
+    with _on(device, stream) as handle:
+        return call(handle)
 
 
 def _workspace(nbytes, device):
@@ -46,10 +59,10 @@ def _workspace(nbytes, device):
 def _like(t, x, what):
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a tensor" % what)
+    if t.dtype is not x.dtype:
+        raise TypeError("%s is %s, not %s" % (what, t.dtype, x.dtype))
     if t.device != x.device:
         raise ValueError("%s is on %s, not on %s" % (what, t.device, x.device))
-    if t.dtype != x.dtype:
-        raise TypeError("%s is %s, not %s" % (what, t.dtype, x.dtype))
     return t
 
 
@@ -63,13 +76,15 @@ def _dtype(x, what):
 
 def _rows_of(t, x, what):
     """Pointer and leading dimension of a matrix of x's shape with unit column stride."""
-    _like(t, x, what)
-    if t.shape != x.shape:
-        raise ValueError("%s has shape %s, not %s" % (what, tuple(t.shape), tuple(x.shape)))
+    if t is not x:
+        _like(t, x, what)
+        if t.shape != x.shape:
+            raise ValueError("%s has shape %s, not %s" % (what, tuple(t.shape), tuple(x.shape)))
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s needs unit column stride" % what)
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), ld if rows > 1 else cols
 
 
 def _vector(t, x, count, what):
@@ -131,16 +146,17 @@ def fuse_block_norm(x, z=None, gate=None, scale=1.0, post=None, pre=None, kind="
     if pre is None and y is not None:
         raise ValueError("y needs the norm that makes it: pre is None")
     xp, x_ld = _rows_of(x, x, "x")
-    with _on(x.device, stream) as handle:
-        if z is not None and h is None:
-            h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if pre is not None and y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        hp, h_ld = _rows_of(h, x, "h") if h is not None else (None, 0)
-        yp, y_ld = _rows_of(y, x, "y") if y is not None else (None, 0)
+
+    def call(handle):
+        rh = torch.empty_like(x, memory_format=torch.contiguous_format) if z is not None and h is None else h
+        ry = torch.empty_like(x, memory_format=torch.contiguous_format) if pre is not None and y is None else y
+        hp, h_ld = _rows_of(rh, x, "h") if rh is not None else (None, 0)
+        yp, y_ld = _rows_of(ry, x, "y") if ry is not None else (None, 0)
         if x.numel():
-            _check(L.load().fuse_block_norm(ctypes.byref(b), xp, x_ld, hp, h_ld, yp, y_ld, handle))
-    return (x if h is None else h), y
+            _check(L.load().fuse_block_norm(b, xp, x_ld, hp, h_ld, yp, y_ld, handle))
+        return x if rh is None else rh, ry
+
+    return _run(x.device, stream, call)
 
 
 def fuse_block_norm_backward(dh, dy, h, z=None, gate=None, scale=1.0, post=None, pre=None, kind="rms", eps=1e-6, stream=None):
@@ -150,75 +166,78 @@ def fuse_block_norm_backward(dh, dy, h, z=None, gate=None, scale=1.0, post=None,
     b, gk, gt = _block(like, z, gate, scale, post, pre, kind, eps, "h")
     (post_w, post_b), (pre_w, pre_b) = _weights(post), _weights(pre)
     lib = L.load()
-    with _on(like.device, stream) as handle:
-        def new(t):
-            return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
+    def new(t):
+        return None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format)
+
+    def call(handle):
         got = BlockGrads(new(like), new(z), new(gt), new(post_w), new(post_b), new(pre_w), new(pre_b))
         if like.numel() == 0:
             for t in got:
                 if t is not None:
                     t.zero_()
             return got
-        g = L.BlockGrads(dx=got.dx.data_ptr(), dx_ld=like.shape[1], dgate_ld=like.shape[1] if gk == "matrix" else 1)
-        if z is not None:
-            g.dz, g.dz_ld = got.dz.data_ptr(), like.shape[1]
-        for name, t in (("dgate", got.dgate), ("dpost_weight", got.dpost), ("dpost_bias", got.dpost_bias),
-                        ("dpre_weight", got.dpre), ("dpre_bias", got.dpre_bias)):
-            if t is not None:
-                setattr(g, name, t.data_ptr())
-        nbytes = lib.fuse_block_norm_backward_bytes(ctypes.byref(b))
-        ws = _workspace(nbytes, like.device)
+        cols = like.shape[1]
+        dx, dz, dgate, dpost, dpost_bias, dpre, dpre_bias = [t.data_ptr() if t is not None else None for t in got]
+        g = L.BlockGrads(dx, cols, dz, cols, dgate, cols if gk == "matrix" else 1, dpost, dpost_bias, dpre, dpre_bias)
+        ws = _workspace(lib.fuse_block_norm_backward_bytes(b), like.device)
         args = []
         for t, what in ((dh, "dh"), (dy, "dy"), (h, "h")):
             args += _rows_of(t, like, what) if t is not None else (None, 0)
-        _check(lib.fuse_block_norm_backward(ctypes.byref(b), *args, ctypes.byref(g), ws.data_ptr(), ws.numel(), handle))
-    return got
+        _check(lib.fuse_block_norm_backward(b, *args, g, ws.data_ptr(), ws.numel(), handle))
+        return got
+
+    return _run(like.device, stream, call)
 
 
 # -------------------------------------------------------------------------- attention ---
 
 def _heads_of(t, like, what, tokens=None, heads=None):
     """(pointer, stride between tokens, stride between heads) of a (tokens, heads, dim) tensor with unit stride along dim."""
-    _like(t, like, what)
-    if t.dim() != 3 or t.shape[2] != like.shape[2]:
-        raise ValueError("%s must be (tokens, heads, %d)" % (what, like.shape[2]))
-    if (tokens is not None and t.shape[0] != tokens) or (heads is not None and t.shape[1] != heads):
-        raise ValueError("%s has shape %s, not (%s, %s, %d)" % (what, tuple(t.shape), tokens, heads, like.shape[2]))
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    if t is not like:
+        _like(t, like, what)
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != like.shape[2]:
+        raise ValueError("%s must be (tokens, heads, %d)" % (what, like.shape[-1]))
+    n, h, dim = shape
+    if (tokens is not None and n != tokens) or (heads is not None and h != heads):
+        raise ValueError("%s has shape %s, not (%s, %s, %d)" % (what, tuple(shape), tokens, heads, dim))
+    token, head, step = t.stride()
+    if step != 1 and dim > 1:
         raise ValueError("%s needs unit stride along dim" % what)
-    dim = t.shape[2]
-    return (t.data_ptr(), t.stride(0) if t.shape[0] > 1 else dim * max(t.shape[1], 1), t.stride(1) if t.shape[1] > 1 else dim)
+    return t.data_ptr(), token if n > 1 else dim * h, head if h > 1 else dim
+
+
+def _places(t, like, device, count, what):
+    if t.dtype is not like.dtype:
+        raise TypeError("%s must be int32 or int64, like offsets" % what)
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (what, t.device, device))
+    if t.dim() != 1 or t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous vector of %d values" % (what, count))
+    return t.data_ptr()
 
 
 def _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale):
     dtype = _dtype(q, "q")
-    if q.dim() != 3 or k.dim() != 3 or q.shape[1] < 1 or k.shape[1] < 1 or q.shape[2] < 1:
+    qs, ks = q.shape, k.shape
+    if len(qs) != 3 or len(ks) != 3 or qs[1] < 1 or ks[1] < 1 or qs[2] < 1:
         raise ValueError("q, k and v must be (tokens, heads, dim)")
-    f = L.Attn(dtype=dtype, heads=q.shape[1], kv_heads=k.shape[1], dim=q.shape[2], causal=int(bool(causal)),
-               q_tokens=q.shape[0], k_tokens=k.shape[0], scale=float(scale) if scale is not None else q.shape[2] ** -0.5)
-    f.q, f.q_token_ld, f.q_head_ld = _heads_of(q, q, "q")
-    f.k, f.k_token_ld, f.k_head_ld = _heads_of(k, q, "k")
-    f.v, f.v_token_ld, f.v_head_ld = _heads_of(v, q, "v", k.shape[0], k.shape[1])
+    qp, q_token, q_head = _heads_of(q, q, "q")
+    kp, k_token, k_head = _heads_of(k, q, "k")
+    vp, v_token, v_head = _heads_of(v, q, "v", ks[0], ks[1])
     if offsets is None or offsets.dim() != 1 or offsets.numel() < 1:
         raise ValueError("offsets must be a vector of the number of sequences + 1 values")
-    f.seqs = offsets.numel() - 1
+    if offsets.dtype is not torch.int32 and offsets.dtype is not torch.int64:
+        raise TypeError("offsets must be int32 or int64")
     if key_lengths is not None and key_offsets is None:
         raise ValueError("key_lengths needs key_offsets")
-    for t, what, count in ((offsets, "offsets", f.seqs + 1), (key_offsets, "key_offsets", f.seqs + 1), (key_lengths, "key_lengths", f.seqs)):
-        if t is None:
-            continue
-        if t.dtype not in (torch.int32, torch.int64) or t.dtype != offsets.dtype:
-            raise TypeError("%s must be int32 or int64, like offsets" % what)
-        if t.device != q.device:
-            raise ValueError("%s is on %s, not on %s" % (what, t.device, q.device))
-        if t.dim() != 1 or t.numel() != count or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous vector of %d values" % (what, count))
-    f.offsets_are_64 = int(offsets.dtype == torch.int64)
-    f.q_offsets = offsets.data_ptr()
-    f.k_offsets = key_offsets.data_ptr() if key_offsets is not None else None
-    f.k_lengths = key_lengths.data_ptr() if key_lengths is not None else None
-    return f
+    device, seqs = q.device, offsets.numel() - 1
+    qo = _places(offsets, offsets, device, seqs + 1, "offsets")
+    ko = None if key_offsets is None else _places(key_offsets, offsets, device, seqs + 1, "key_offsets")
+    kl = None if key_lengths is None else _places(key_lengths, offsets, device, seqs, "key_lengths")
+    return L.Attn(dtype, qs[1], ks[1], qs[2], 1 if causal else 0, 1 if offsets.dtype is torch.int64 else 0, qs[0], ks[0], seqs, qo, ko, kl,
+                  qs[2] ** -0.5 if scale is None else scale, qp, kp, vp, q_token, q_head, k_token, k_head, v_token, v_head)
 
 
 def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=True, scale=None, out=None, lse=None, stream=None):
@@ -230,19 +249,20 @@ def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=
     causal: the last query sees all keys, the one before it all but the last, and so on.  scale: None is 1 / sqrt(dim).  lse:
     (tokens, heads) float32.  Rows that belong to no sequence are not written: in results made here they hold anything."""
     f = _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != q.device):
+        raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % (tuple(q.shape[:2]), q.device))
     lib = L.load()
-    with _on(q.device, stream) as handle:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if lse is None:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        elif lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != q.device:
-            raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % (tuple(q.shape[:2]), q.device))
-        op, o_token, o_head = _heads_of(out, q, "out", q.shape[0], q.shape[1])
-        nbytes = lib.fuse_attention_bytes(ctypes.byref(f))
+
+    def call(handle):
+        o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
+        l = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
+        op, o_token, o_head = _heads_of(o, q, "out", q.shape[0], q.shape[1])
+        nbytes = lib.fuse_attention_bytes(f)
         ws = _workspace(nbytes, q.device) if nbytes else None
-        _check(lib.fuse_attention(ctypes.byref(f), op, o_token, o_head, lse.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, handle))
-    return out, lse
+        _check(lib.fuse_attention(f, op, o_token, o_head, l.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, handle))
+        return o, l
+
+    return _run(q.device, stream, call)
 
 
 def fuse_attention_backward(dout, q, k, v, out, lse, offsets, key_offsets=None, key_lengths=None, causal=True, scale=None,
@@ -252,20 +272,18 @@ def fuse_attention_backward(dout, q, k, v, out, lse, offsets, key_offsets=None, 
     if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != q.device:
         raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % (tuple(q.shape[:2]), q.device))
     lib = L.load()
-    with _on(q.device, stream) as handle:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
-        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
-        g = L.AttnGrads(lse=lse.data_ptr())
-        for name, t, like in (("dout", dout, q), ("out", out, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
-            p, token, head = _heads_of(t, q, name, like.shape[0], like.shape[1])
-            setattr(g, name, p)
-            setattr(g, name + "_token_ld", token)
-            setattr(g, name + "_head_ld", head)
-        nbytes = lib.fuse_attention_backward_bytes(ctypes.byref(f))
-        ws = _workspace(nbytes, q.device)
-        _check(lib.fuse_attention_backward(ctypes.byref(f), ctypes.byref(g), ws.data_ptr(), ws.numel(), handle))
-    return dq, dk, dv
+
+    def call(handle):
+        got = [torch.empty_like(like, memory_format=torch.contiguous_format) if t is None else t for t, like in ((dq, q), (dk, k), (dv, v))]
+        at = [_heads_of(t, q, name, like.shape[0], like.shape[1]) for name, t, like in
+              (("dout", dout, q), ("out", out, q), ("dq", got[0], q), ("dk", got[1], k), ("dv", got[2], v))]
+        g = L.AttnGrads(at[0][0], at[1][0], lse.data_ptr(), *at[0][1:], *at[1][1:], at[2][0], at[3][0], at[4][0], *at[2][1:], *at[3][1:],
+                        *at[4][1:])
+        ws = _workspace(lib.fuse_attention_backward_bytes(f), q.device)
+        _check(lib.fuse_attention_backward(f, g, ws.data_ptr(), ws.numel(), handle))
+        return tuple(got)
+
+    return _run(q.device, stream, call)
 
 
 # -------------------------------------------------------------------------- gradients ---
@@ -290,52 +308,64 @@ def _list(tensors, out):
         out = list(out)
         if len(out) != len(tensors):
             raise ValueError("%d results for %d tensors" % (len(out), len(tensors)))
-    arr = (L.Tensor * len(tensors))()
+    cells = []                             # (data, out, count, dtype) of each, as L.Tensor has them
     for i, t in enumerate(tensors):
-        if not t.is_contiguous():
+        flat = t.is_contiguous()
+        if not flat:
             _dense_cells(t, "tensor %d" % i)
         dtype = DTYPE.get(t.dtype)
         if dtype is None or t.device != device:
             _dtype(t, "tensor %d" % i)
             raise ValueError("tensor %d is on %s, not on %s" % (i, t.device, device))
-        a = arr[i]
-        a.data, a.count, a.dtype = t.data_ptr(), t.numel(), dtype
+        at = 0
         if out is not None:
             o = out[i]
             _like(o, t, "result %d" % i)
-            if o.shape != t.shape or (o.stride() != t.stride() and not (o.is_contiguous() and t.is_contiguous())):
+            if o.shape != t.shape or not (flat and o.is_contiguous() or o.stride() == t.stride()):
                 raise ValueError("result %d is not laid out like its tensor" % i)
-            a.out = o.data_ptr()
-    return arr, device
+            at = o.data_ptr()
+        cells += (t.data_ptr(), at, t.numel(), dtype)
+    return (ctypes.c_int64 * len(cells))(*cells), len(tensors), device
+
+
+def _one_value(t, device, what):
+    if t.dtype != torch.float64 or t.numel() != 1 or t.device != device:
+        raise ValueError("%s must be one float64 value on %s" % (what, device))
+    return t
 
 
 def fuse_grad_norm(tensors, out=None, stream=None):
     """C: fuse_grad_norm.  The 2-norm over all cells of all tensors: one float64 value on the device."""
-    arr, device = _list(tensors, None)
+    arr, n, device = _list(tensors, None)
+    if out is not None:
+        _one_value(out, device, "out")
     lib = L.load()
-    with _on(device, stream) as handle:
-        if out is None:
-            out = torch.empty(1, dtype=torch.float64, device=device)
-        elif out.dtype != torch.float64 or out.numel() != 1 or out.device != device:
-            raise ValueError("out must be one float64 value on %s" % device)
-        ws = _workspace(lib.fuse_grad_norm_bytes(arr, len(arr)), device)
-        _check(lib.fuse_grad_norm(arr, len(arr), out.data_ptr(), ws.data_ptr(), ws.numel(), handle))
-    return out
+
+    def call(handle):
+        norm = torch.empty(1, dtype=torch.float64, device=device) if out is None else out
+        ws = _workspace(lib.fuse_grad_norm_bytes(arr, n), device)
+        _check(lib.fuse_grad_norm(arr, n, norm.data_ptr(), ws.data_ptr(), ws.numel(), handle))
+        return norm
+
+    return _run(device, stream, call)
 
 
 def fuse_grad_clip(tensors, max_norm, eps=1e-6, norm=None, out=None, stream=None):
     """C: fuse_grad_clip.  Scales all tensors by min(1, max_norm / (norm + eps)), in place or into the tensors `out`; returns the
     norm (float64, on the device).  norm: None computes it; or one float64 value on the device that the program has already (such as the
     root of a sum over several processes)."""
-    arr, device = _list(tensors, out)
+    arr, n, device = _list(tensors, out)
+    if norm is not None:
+        _one_value(norm, device, "norm")
     lib = L.load()
-    with _on(device, stream) as handle:
+
+    def call(handle):
         if norm is not None:
-            if norm.dtype != torch.float64 or norm.numel() != 1 or norm.device != device:
-                raise ValueError("norm must be one float64 value on %s" % device)
-            _check(lib.fuse_grad_clip(arr, len(arr), float(max_norm), float(eps), norm.data_ptr(), None, None, 0, handle))
+            _check(lib.fuse_grad_clip(arr, n, max_norm, eps, norm.data_ptr(), None, None, 0, handle))
             return norm
-        norm = torch.empty(1, dtype=torch.float64, device=device)
-        ws = _workspace(lib.fuse_grad_norm_bytes(arr, len(arr)), device)
-        _check(lib.fuse_grad_clip(arr, len(arr), float(max_norm), float(eps), None, norm.data_ptr(), ws.data_ptr(), ws.numel(), handle))
-    return norm
+        found = torch.empty(1, dtype=torch.float64, device=device)
+        ws = _workspace(lib.fuse_grad_norm_bytes(arr, n), device)
+        _check(lib.fuse_grad_clip(arr, n, max_norm, eps, None, found.data_ptr(), ws.data_ptr(), ws.numel(), handle))
+        return found
+
+    return _run(device, stream, call)
