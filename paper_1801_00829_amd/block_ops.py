@@ -308,23 +308,24 @@ def _list(tensors, out):
         out = list(out)
         if len(out) != len(tensors):
             raise ValueError("%d results for %d tensors" % (len(out), len(tensors)))
+    index = device.index if device.type == "cuda" else -1
     cells = []                             # (data, out, count, dtype) of each, as L.Tensor has them
     for i, t in enumerate(tensors):
-        flat = t.is_contiguous()
-        if not flat:
-            _dense_cells(t, "tensor %d" % i)
-        dtype = DTYPE.get(t.dtype)
-        if dtype is None or t.device != device:
+        flat, dtype, count = t.is_contiguous(), DTYPE.get(t.dtype), t.numel()
+        if dtype is None or t.get_device() != index:
             _dtype(t, "tensor %d" % i)
             raise ValueError("tensor %d is on %s, not on %s" % (i, t.device, device))
-        at = 0
-        if out is not None:
-            o = out[i]
+        if not flat:
+            _dense_cells(t, "tensor %d" % i)
+        if out is None:
+            cells += (t.data_ptr(), 0, count, dtype)
+            continue
+        o = out[i]
+        if o.dtype is not t.dtype or o.get_device() != index:
             _like(o, t, "result %d" % i)
-            if o.shape != t.shape or not (flat and o.is_contiguous() or o.stride() == t.stride()):
-                raise ValueError("result %d is not laid out like its tensor" % i)
-            at = o.data_ptr()
-        cells += (t.data_ptr(), at, t.numel(), dtype)
+        if o.numel() != count or not (flat and o.is_contiguous() or o.shape == t.shape and o.stride() == t.stride()):
+            raise ValueError("result %d is not laid out like its tensor" % i)
+        cells += (t.data_ptr(), o.data_ptr(), count, dtype)
     return (ctypes.c_int64 * len(cells))(*cells), len(tensors), device
 
 

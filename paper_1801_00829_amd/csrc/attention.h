@@ -53,6 +53,22 @@ __device__ __forceinline__ Seq seq_at(const AttnArgs &a, int s)
     return x;
 }
 
+// The same in scalar registers, for a sequence that is the same for the whole wave.
+__device__ __forceinline__ long long uniform(long long v)
+{
+    return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)v) |
+                       (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+}
+__device__ __forceinline__ Seq uniform(const Seq &v)
+{
+    Seq x;
+    x.q0 = uniform(v.q0);
+    x.k0 = uniform(v.k0);
+    x.nq = __builtin_amdgcn_readfirstlane(v.nq);
+    x.nk = __builtin_amdgcn_readfirstlane(v.nk);
+    return x;
+}
+
 // Tiles of `tile` rows over all sequences without their lengths on the host: sequence s starts at tile
 // floor(offset / tile) + s, which leaves it at least as many tiles as it needs (some stay empty).
 __host__ __device__ inline long long first_tile(long long rows_before, int s, int tile) { return rows_before / tile + s; }
@@ -95,7 +111,7 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
     Work w;
     if (a.seqs > kSorted) {
         const int s = KEYS ? seq_of_tile(a, a.k_off, a.k_tokens, 1, tile, b) : seq_of_tile(a, a.q_off, a.q_tokens, a.group, tile, b);
-        w.x = seq_at(a, s);
+        w.x = uniform(seq_at(a, s));
         const long long at = (b - first_tile(KEYS ? w.x.k0 : w.x.q0 * a.group, s, tile)) * tile;
         w.any = at < (KEYS ? (long long)w.x.nk : (long long)w.x.nq * a.group);
         w.first = (int)at;
@@ -137,7 +153,7 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
     for (int i = (int)b - before; i > 0; --i)
         have &= have - 1;
     const int s = __builtin_ctzll(have);
-    w.x = seq_at(a, s);
+    w.x = uniform(seq_at(a, s));
     w.first = (KEYS ? __builtin_amdgcn_readlane(n, s) - low : low - 1) * tile;
     return w;
 }

@@ -132,6 +132,12 @@ struct Fill {
         in = chunk * 8 < dim;
     }
 
+    __device__ __forceinline__ void pass(char *lds, int i, const T *from) const
+    {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                         (__attribute__((address_space(3))) void *)(lds + i * kPerPass * L::kRowBytes + wave * 1024), 16, 0, 0);
+    }
+
     // `at(r)`: where row r of the matrix is; `first`: the tile's first row, `end` > first
     template <typename F>
     __device__ __forceinline__ void load(char *lds, int first, int end, F at) const
@@ -139,10 +145,20 @@ struct Fill {
         if (in)
 #pragma unroll
             for (int i = 0; i < kPasses; ++i)
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void *)(at(min(first + row + i * kPerPass, end - 1)) + chunk * 8),
-                    (__attribute__((address_space(3))) void *)(lds + i * kPerPass * L::kRowBytes + wave * 1024), 16, 0, 0);
+                pass(lds, i, at(min(first + row + i * kPerPass, end - 1)) + chunk * 8);
     }
+
+    // A whole tile whose rows lie so that those of one pass are the same distance from the next one's: `tile` its first row, the
+    // same for all lanes, `lane` this lane's first element from there (lane_of), `step` the distance.  The addresses are then scalars
+    // with one offset per lane, and cost the vector unit nothing.
+    __device__ __forceinline__ void load_whole(char *lds, const T *tile, unsigned lane, long long step) const
+    {
+        if (in)
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i)
+                pass(lds, i, reinterpret_cast<const T *>(reinterpret_cast<const char *>(tile + i * step) + lane));
+    }
+    __device__ __forceinline__ unsigned lane_of(long long row_at) const { return (unsigned)((row_at + chunk * 8) * (long long)sizeof(T)); }
 
     __device__ __forceinline__ void load(char *lds, const T *base, long long ld, int first, int end) const
     {

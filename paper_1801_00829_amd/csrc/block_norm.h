@@ -13,6 +13,9 @@
 // of a layer norm are taken in two passes over the registers (mean, then squares of the differences): one pass of sums of
 // squares would lose the digits that a large mean has.
 #pragma once
+#include <algorithm>
+#include <atomic>
+
 #include "block_ops.h"
 
 namespace fuse {
@@ -577,33 +580,68 @@ __global__ void __launch_bounds__(1024) block_norm_sums_kernel(const SumArgs a)
     }
 }
 
-// A type's kernels by steps per row and alignment (see steps_for).
-#define FUSE_BY_STEPS(kernel, a, layer, k, vec, ...)                                                                       \
-    do {                                                                                                                  \
-        if (vec) {                                                                                                        \
-            if (layer) FUSE_STEPS(kernel, k, true, true, a, __VA_ARGS__); else FUSE_STEPS(kernel, k, true, false, a, __VA_ARGS__);     \
-        } else {                                                                                                          \
-            if (layer) FUSE_STEPS(kernel, k, false, true, a, __VA_ARGS__); else FUSE_STEPS(kernel, k, false, false, a, __VA_ARGS__);   \
-        }                                                                                                                 \
-    } while (0)
-#define FUSE_STEPS(kernel, k, vec, layer, a, ...)                                                                          \
-    do {                                                                                                                  \
-        if (k == 1) kernel<T, 1, vec, layer><<<__VA_ARGS__>>>(a);                                                         \
-        else if (k == 2) kernel<T, 2, vec, layer><<<__VA_ARGS__>>>(a);                                                    \
-        else if (k == 4) kernel<T, 4, vec, layer><<<__VA_ARGS__>>>(a);                                                    \
-        else kernel<T, 32 / kEach<T>, vec, layer><<<__VA_ARGS__>>>(a);                                                    \
-    } while (0)
-
-template <typename T>
-void launch_fwd(const FwdArgs &a, bool layer, int k, bool vec, unsigned blocks, unsigned threads, hipStream_t s)
+// Persistent blocks: as many as the device holds at once (asked for once per kernel and block size), so that all of them run from
+// start to end; a few more would run when the others are done.
+template <auto KERNEL>
+unsigned resident_blocks(unsigned threads)
 {
-    FUSE_BY_STEPS(block_norm_kernel, a, layer, k, vec, blocks, threads, 0, s);
+    static std::atomic<int> known[kMaxThreads / 64 + 1];
+    std::atomic<int> &n = known[threads / 64];
+    if (!n.load(std::memory_order_relaxed)) {
+        int per = 0;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per, KERNEL, (int)threads, 0) != hipSuccess || per < 1) {
+            (void)hipGetLastError();
+            per = 1;
+        }
+        n.store(per, std::memory_order_relaxed);
+    }
+    return (unsigned)(n.load(std::memory_order_relaxed) * Runtime::get().num_cus());
 }
 
+// A type's kernels by steps per row and alignment (see steps_for); `most` blocks where all of them are resident.
+#define FUSE_BY_STEPS(kernel, a, layer, k, vec, most, threads, s)                                                          \
+    do {                                                                                                                  \
+        if (vec) {                                                                                                        \
+            if (layer) FUSE_STEPS(kernel, k, true, true, a, most, threads, s); else FUSE_STEPS(kernel, k, true, false, a, most, threads, s);     \
+        } else {                                                                                                          \
+            if (layer) FUSE_STEPS(kernel, k, false, true, a, most, threads, s); else FUSE_STEPS(kernel, k, false, false, a, most, threads, s);   \
+        }                                                                                                                 \
+    } while (0)
+#define FUSE_STEPS(kernel, k, vec, layer, a, most, threads, s)                                                             \
+    do {                                                                                                                  \
+        if (k == 1) FUSE_PERSISTENT((kernel<T, 1, vec, layer>), a, most, threads, s);                                     \
+        else if (k == 2) FUSE_PERSISTENT((kernel<T, 2, vec, layer>), a, most, threads, s);                                \
+        else if (k == 4) FUSE_PERSISTENT((kernel<T, 4, vec, layer>), a, most, threads, s);                                \
+        else FUSE_PERSISTENT((kernel<T, 32 / kEach<T>, vec, layer>), a, most, threads, s);                                \
+    } while (0)
+#define FUSE_PERSISTENT(kernel, a, most, threads, s)                                                                       \
+    kernel<<<std::min(most, resident_blocks<kernel>(threads)), threads, 0, s>>>(a)
+
+template <typename T>
+void launch_fwd(const FwdArgs &a, bool layer, int k, bool vec, unsigned most, unsigned threads, hipStream_t s)
+{
+    FUSE_BY_STEPS(block_norm_kernel, a, layer, k, vec, most, threads, s);
+}
+
+// (a gradient call's blocks are those that its workspace has room for)
 template <typename T>
 void launch_bwd(const BwdArgs &a, bool layer, int k, bool vec, unsigned blocks, unsigned threads, hipStream_t s)
 {
-    FUSE_BY_STEPS(block_norm_grad_kernel, a, layer, k, vec, blocks, threads, 0, s);
+#define FUSE_GRAD(k_, vec_, layer_) block_norm_grad_kernel<T, k_, vec_, layer_><<<blocks, threads, 0, s>>>(a)
+#define FUSE_GRAD_STEPS(vec_, layer_)                                                                                      \
+    do {                                                                                                                  \
+        if (k == 1) FUSE_GRAD(1, vec_, layer_);                                                                           \
+        else if (k == 2) FUSE_GRAD(2, vec_, layer_);                                                                      \
+        else if (k == 4) FUSE_GRAD(4, vec_, layer_);                                                                      \
+        else FUSE_GRAD(32 / kEach<T>, vec_, layer_);                                                                      \
+    } while (0)
+    if (vec) {
+        if (layer) FUSE_GRAD_STEPS(true, true); else FUSE_GRAD_STEPS(true, false);
+    } else {
+        if (layer) FUSE_GRAD_STEPS(false, true); else FUSE_GRAD_STEPS(false, false);
+    }
+#undef FUSE_GRAD
+#undef FUSE_GRAD_STEPS
 }
 
 template <typename T>

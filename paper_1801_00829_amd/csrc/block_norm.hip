@@ -142,8 +142,8 @@ int norm_impl(const fuse_block *b, const void *x, int64_t x_ld, void *h, int64_t
     a.eps = b->eps, a.scale = b->scale;
     const bool vec = block_on_16(b) && rows_on_16(b, x, x_ld) && rows_on_16(b, h, h_ld) && rows_on_16(b, y, y_ld);
     const int threads = threads_for(b), per = threads / a.group;
-    const int64_t want = (b->rows + per - 1) / per, most = 256 * (2048 / threads);
-    const unsigned blocks = (unsigned)(want > most ? most : want);
+    const int64_t want = (b->rows + per - 1) / per;
+    const unsigned blocks = (unsigned)(want > 65536 ? 65536 : want);
     FUSE_BY_DTYPE(b->dtype, launch_fwd, a, b->norm == FUSE_NORM_LAYER, steps_for(b), vec, blocks, threads, (hipStream_t)stream);
     return launched("block_norm_kernel");
 }
