@@ -183,151 +183,10 @@ __device__ __forceinline__ T *row_of(const Mat &m, long long token, int head)
     return static_cast<T *>(m.p) + token * m.token + head * m.head;
 }
 
-// dot(a, b) over dim, a multiple of 8, in fp32
-template <typename T>
-__device__ __forceinline__ float dot_rows(const T *__restrict__ a, const T *__restrict__ b, int dim)
-{
-    struct alignas(16) Pack { T t[8]; };
-    float s = 0.0f;
-    for (int d = 0; d < dim; d += 8) {
-        const Pack x = *reinterpret_cast<const Pack *>(a + d), y = *reinterpret_cast<const Pack *>(b + d);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            s = fmaf((float)x.t[j], (float)y.t[j], s);
-    }
-    return s;
-}
-
-// One query's output by one wave, key by key: nothing but the keys that it sees is touched.  Lane l holds dims l and l + 64.
-template <typename T>
-__device__ void attend_row(const AttnArgs &a, const Seq &x, int place, int head)
-{
-    const int lane = threadIdx.x & 63, kvh = head / a.group, n = seen_by(a, x, place);
-    const T *q = row_of<const T>(a.q, x.q0 + place, head);
-    float top = -INFINITY;
-    bool nan = false;
-    for (int j = lane; j < n; j += 64) {
-        const float s = a.scale * dot_rows(q, row_of<const T>(a.k, x.k0 + j, kvh), a.dim);
-        nan |= s != s;
-        top = fmaxf(top, s);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
-        top = fmaxf(top, __shfl_xor(top, o, 64));
-    if (__any(nan))
-        top = NAN;
-    const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        float p = 0.0f;
-        if (j0 + lane < n)
-            p = expf(a.scale * dot_rows(q, row_of<const T>(a.k, x.k0 + j0 + lane, kvh), a.dim) - base);
-        sum += p;
-        for (int j = 0; j < 64 && j0 + j < n; ++j) {
-            const float w = __shfl(p, j, 64);
-            const T *v = row_of<const T>(a.v, x.k0 + j0 + j, kvh);
-            if (lane < a.dim)
-                o0 = fmaf(w, (float)v[lane], o0);
-            if (lane + 64 < a.dim)
-                o1 = fmaf(w, (float)v[lane + 64], o1);
-        }
-    }
-    sum = wave_sum(sum);
-    const float r = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-    T *out = row_of<T>(a.out, x.q0 + place, head);
-    if (lane < a.dim)
-        out[lane] = (T)(o0 * r);
-    if (lane + 64 < a.dim)
-        out[lane + 64] = (T)(o1 * r);
-    if (a.lse && lane == 0)
-        a.lse[(x.q0 + place) * a.heads + head] = base + logf(sum);
-}
-
 // Place of a row's delta and lse2: key heads x rows, so that the rows of one problem follow each other.
 __device__ __forceinline__ long long stat_at(const AttnArgs &a, long long token, int head)
 {
     return (head / a.group * a.q_tokens + token) * a.group + head % a.group;
-}
-
-template <typename T>
-__device__ __forceinline__ float delta_of(const AttnArgs &a, long long token, int head)
-{
-    return dot_rows(row_of<const T>(a.dout, token, head), row_of<const T>(a.out, token, head), a.dim);
-}
-
-// One query's gradient by one wave, key by key.
-template <typename T>
-__device__ void query_grad_row(const AttnArgs &a, const Seq &x, int place, int head)
-{
-    const int lane = threadIdx.x & 63, kvh = head / a.group, n = seen_by(a, x, place);
-    const long long token = x.q0 + place;
-    const T *q = row_of<const T>(a.q, token, head), *g = row_of<const T>(a.dout, token, head);
-    const float delta = delta_of<T>(a, token, head), lse = a.lse[token * a.heads + head];
-    float o0 = 0.0f, o1 = 0.0f;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        float ds = 0.0f;
-        if (j0 + lane < n) {
-            const float p = expf(a.scale * dot_rows(q, row_of<const T>(a.k, x.k0 + j0 + lane, kvh), a.dim) - lse);
-            ds = a.scale * p * (dot_rows(g, row_of<const T>(a.v, x.k0 + j0 + lane, kvh), a.dim) - delta);
-        }
-        for (int j = 0; j < 64 && j0 + j < n; ++j) {
-            const float w = __shfl(ds, j, 64);
-            const T *k = row_of<const T>(a.k, x.k0 + j0 + j, kvh);
-            if (lane < a.dim)
-                o0 = fmaf(w, (float)k[lane], o0);
-            if (lane + 64 < a.dim)
-                o1 = fmaf(w, (float)k[lane + 64], o1);
-        }
-    }
-    T *out = row_of<T>(a.dq, token, head);
-    if (lane < a.dim)
-        out[lane] = (T)o0;
-    if (lane + 64 < a.dim)
-        out[lane + 64] = (T)o1;
-    if (lane == 0)
-        a.delta[stat_at(a, token, head)] = delta;
-}
-
-// One key's and value's gradients by one wave, query by query over all heads of the group.
-template <typename T>
-__device__ void key_grad_row(const AttnArgs &a, const Seq &x, int j, int kvh)
-{
-    const int lane = threadIdx.x & 63;
-    const T *k = row_of<const T>(a.k, x.k0 + j, kvh), *v = row_of<const T>(a.v, x.k0 + j, kvh);
-    float k0 = 0.0f, k1 = 0.0f, v0 = 0.0f, v1 = 0.0f;
-    const long long end = (long long)x.nq * a.group;
-    for (long long r0 = (long long)first_that_sees(a, x, j) * a.group; r0 < end; r0 += 64) {
-        float p = 0.0f, ds = 0.0f;
-        if (r0 + lane < end) {
-            const long long token = x.q0 + (r0 + lane) / a.group;
-            const int head = kvh * a.group + (int)((r0 + lane) % a.group);
-            p = expf(a.scale * dot_rows(row_of<const T>(a.q, token, head), k, a.dim) - a.lse[token * a.heads + head]);
-            ds = a.scale * p * (dot_rows(row_of<const T>(a.dout, token, head), v, a.dim) - a.delta[stat_at(a, token, head)]);
-        }
-        for (int i = 0; i < 64 && r0 + i < end; ++i) {
-            const float wp = __shfl(p, i, 64), ws = __shfl(ds, i, 64);
-            const long long token = x.q0 + (r0 + i) / a.group;
-            const int head = kvh * a.group + (int)((r0 + i) % a.group);
-            const T *q = row_of<const T>(a.q, token, head), *g = row_of<const T>(a.dout, token, head);
-            if (lane < a.dim) {
-                k0 = fmaf(ws, (float)q[lane], k0);
-                v0 = fmaf(wp, (float)g[lane], v0);
-            }
-            if (lane + 64 < a.dim) {
-                k1 = fmaf(ws, (float)q[lane + 64], k1);
-                v1 = fmaf(wp, (float)g[lane + 64], v1);
-            }
-        }
-    }
-    T *dk = row_of<T>(a.dk, x.k0 + j, kvh), *dv = row_of<T>(a.dv, x.k0 + j, kvh);
-    if (lane < a.dim) {
-        dk[lane] = (T)k0;
-        dv[lane] = (T)v0;
-    }
-    if (lane + 64 < a.dim) {
-        dk[lane + 64] = (T)k1;
-        dv[lane + 64] = (T)v1;
-    }
 }
 
 // Checks of both directions, and the arguments that both have (host).

@@ -1,4 +1,6 @@
 // Attention over packed sequences, forward (fuse_attention).
+#include <type_traits>
+
 #include "attention_tiles.h"
 
 namespace {
@@ -42,11 +44,12 @@ __device__ __forceinline__ void follow_max(float top, float c, float &m, float &
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, const Parts parts)
+__global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const AttnArgs a, const Parts parts)
 {
     using L = Tile<DP>;
     constexpr int kBytes = kKeys * L::kRowBytes;
     __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][K, V]
+    __shared__ s16x8 spare[4][2][64];                                      // weights, see add_seen
 
     const int kvh = blockIdx.x % a.kv_heads;
     const unsigned rest = blockIdx.x / a.kv_heads;
@@ -86,70 +89,94 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, con
     }
 
     f32x16 o[L::kCols];
-#pragma unroll
-    for (int d = 0; d < L::kCols; ++d)
-        o[d] = f32x16{};
-    float m = -INFINITY, mc = 0.0f, l = 0.0f;
+    float m, mc, l;
     const float c = a.scale * kLog2e;
 
     const T *kbase = row_of<const T>(a.k, x.k0, kvh), *vbase = row_of<const T>(a.v, x.k0, kvh);
     const Fill<T, DP, kKeys> fill(a.dim);
     if (a.dim < DP)
         clear_tiles(lds[0][0], sizeof lds);
-    if (begin < end) {
-        fill.load(lds[0][0], kbase, a.k.token, begin, x.nk);
-        fill.load(lds[0][1], vbase, a.v.token, begin, x.nk);
-    }
-    __syncthreads();
-    for (int j = begin, step = 0; j < end; j += kKeys, ++step) {
-        const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
-        if (j + kKeys < end) {             // into the tiles that all waves have left behind with the last barrier
-            fill.load(lds[(step + 1) & 1][0], kbase, a.k.token, j + kKeys, x.nk);
-            fill.load(lds[(step + 1) & 1][1], vbase, a.v.token, j + kKeys, x.nk);
-        }
-        __builtin_amdgcn_sched_barrier(0); // the loads first, a whole step ahead of the barrier that waits for them
-        if (j < seen_hi) {
-            f32x16 p[2];
+    auto attend = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        m = -INFINITY, mc = 0.0f, l = 0.0f;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                p[n] = f32x16{};
-#pragma unroll
-                for (int i = 0; i < L::kSteps; ++i)
-                    p[n] = product<T>(read_row(kt + n * 32 * L::kRowBytes, row_at[i]), q[i], p[n]);
-            }
-            if (j + kKeys > seen_lo) {
-                const int left = seen - j - 4 * h;
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (n * 32 + 8 * (i / 4) + i % 4 >= left)
-                            p[n][i] = -INFINITY;
-            }
-            float top = p[0][0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i)
-                top = fmaxf(top, p[i / 16][i % 16]);
-            follow_max<L::kCols>(both_max(top), c, m, mc, l, o);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                p[i / 16][i % 16] = __builtin_amdgcn_exp2f(fmaf(p[i / 16][i % 16], c, -mc));
-                l += p[i / 16][i % 16];
-            }
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                float w[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    w[i] = p[n / 2][n % 2 * 8 + i];
-                const s16x8 b = rounded<T>(w);
-#pragma unroll
-                for (int d = 0; d < L::kCols; ++d)
-                    o[d] = product<T>(read_col(vt + n * 16 * L::kRowBytes, col_at[d][0], col_at[d][1]), b, o[d]);
-            }
+        for (int d = 0; d < L::kCols; ++d)
+            o[d] = f32x16{};
+        if (begin < end) {
+            fill.load(lds[0][0], kbase, a.k.token, begin, x.nk);
+            fill.load(lds[0][1], vbase, a.v.token, begin, x.nk);
         }
         __syncthreads();
-    }
+        for (int j = begin, step = 0; j < end; j += kKeys, ++step) {
+            const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
+            if (j + kKeys < end) {             // into the tiles that all waves have left behind with the last barrier
+                fill.load(lds[(step + 1) & 1][0], kbase, a.k.token, j + kKeys, x.nk);
+                fill.load(lds[(step + 1) & 1][1], vbase, a.v.token, j + kKeys, x.nk);
+            }
+            __builtin_amdgcn_sched_barrier(0); // the loads first, a whole step ahead of the barrier that waits for them
+            if (j < seen_hi) {
+                f32x16 p[2];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    p[n] = f32x16{};
+#pragma unroll
+                    for (int i = 0; i < L::kSteps; ++i)
+                        p[n] = product<T>(read_row(kt + n * 32 * L::kRowBytes, row_at[i]), q[i], p[n]);
+                }
+                const bool masked = j + kKeys > seen_lo;
+                if (masked) {
+                    const int left = seen - j - 4 * h;
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (n * 32 + 8 * (i / 4) + i % 4 >= left)
+                                p[n][i] = -INFINITY;
+                }
+                float top = p[0][0];
+#pragma unroll
+                for (int i = 1; i < 32; ++i)
+                    top = fmaxf(top, p[i / 16][i % 16]);
+                follow_max<L::kCols>(both_max(top), c, m, mc, l, o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    p[i / 16][i % 16] = __builtin_amdgcn_exp2f(fmaf(p[i / 16][i % 16], c, -mc));
+                    l += p[i / 16][i % 16];
+                }
+                s16x8 w[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    float e[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        e[i] = p[n / 2][n % 2 * 8 + i];
+                    w[n] = rounded<T>(e);
+                }
+                if (CAREFUL && masked && holds_no_number<T, DP>(vt, kKeys)) {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        spare[wave][0][lane] = w[n * 2];
+                        spare[wave][1][lane] = w[n * 2 + 1];
+                        wave_sees();
+                        add_seen<T, DP>(o, vt + n * 32 * L::kRowBytes, spare[wave][0], 64, 32, 0, seen - j - n * 32, 0);
+                        wave_sees();
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int d = 0; d < L::kCols; ++d)
+                            o[d] = product<T>(read_col(vt + n * 16 * L::kRowBytes, col_at[d][0], col_at[d][1]), w[n], o[d]);
+                }
+            }
+            __syncthreads();
+        }
+    };
+    attend(std::false_type());
+    // A masked score is a weight of 0, which the matrix units still multiply with the value: no number where that is not finite.  A
+    // block with such a result is done again, with an eye on the values of the steps that have a mask.
+    if (any_wave(in && not_finite(o) != 0.0f, lds[0][0]))
+        attend(std::true_type());
 
     l = both_sum(l);
     if (parts.splits > 1) {
@@ -170,32 +197,11 @@ __global__ void __launch_bounds__(256, 2) attention_kernel(const AttnArgs a, con
         return;
     }
 
-    // A masked score is a weight of 0, which the matrix units still multiply with the value: NaN where that is not finite.
-    // Rows with such a result are done again, key by key.
-    float worst = l - l;
-#pragma unroll
-    for (int d = 0; d < L::kCols; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            worst += o[d][i] - o[d][i];
-    const unsigned long long bad = __ballot(in && worst != 0.0f);
-    const float f = l > 0.0f ? 1.0f / l : 0.0f;
-    if (in && worst == 0.0f) {
-        T *out = row_of<T>(a.out, x.q0 + place, head);
-        typedef T t4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-        for (int d = 0; d < L::kCols; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (d * 32 + i * 8 + h * 4 < a.dim)
-                    *reinterpret_cast<t4 *>(out + d * 32 + i * 8 + h * 4) =
-                        t4{(T)(o[d][i * 4] * f), (T)(o[d][i * 4 + 1] * f), (T)(o[d][i * 4 + 2] * f), (T)(o[d][i * 4 + 3] * f)};
+    const float f = l > 0.0f ? 1.0f / l : 0.0f;        // (no key seen: 0; a score that is no number: o holds none either)
+    if (in) {
+        write_columns<T>(o, f, row_of<T>(a.out, x.q0 + place, head), h, a.dim);
         if (a.lse && h == 0)
-            a.lse[(x.q0 + place) * a.heads + head] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, logf(l));
-    }
-    for (unsigned todo = (unsigned)(bad | (bad >> 32)); todo; todo &= todo - 1) {
-        const int again = first + wave * 32 + __builtin_ctz(todo), p = place_of(a, again);
-        attend_row<T>(a, x, p, kvh * a.group + again - p * a.group);
+            a.lse[(x.q0 + place) * a.heads + head] = l == 0.0f ? -INFINITY : fmaf(m, a.scale, logf(l));
     }
 }
 
@@ -223,17 +229,11 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
         float o0 = 0.0f, o1 = 0.0f;
         for (int i = 0; i < parts.splits; ++i) {
             const float f = __shfl(w, i, 64);
-            if (f == 0.0f)                 // nothing seen, or nothing that counts
-                continue;
             const float *o = parts.o + (at + i) * a.dim;
             if (lane < a.dim)
                 o0 = fmaf(f, o[lane], o0);
             if (lane + 64 < a.dim)
                 o1 = fmaf(f, o[lane + 64], o1);
-        }
-        if (__any(o0 - o0 + (o1 - o1) + (sum - sum) != 0.0f)) {            // as above
-            attend_row<T>(a, x, place, head);
-            continue;
         }
         const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
         T *out = row_of<T>(a.out, x.q0 + place, head);
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
         if (lane + 64 < a.dim)
             out[lane + 64] = (T)(o1 * f);
         if (a.lse && lane == 0)
-            a.lse[(x.q0 + place) * a.heads + head] = top == -INFINITY ? -INFINITY : fmaf(top, a.scale, logf(sum));
+            a.lse[(x.q0 + place) * a.heads + head] = sum == 0.0f ? -INFINITY : fmaf(top, a.scale, logf(sum));
     }
 }
 

@@ -1,4 +1,6 @@
 // Attention over packed sequences, gradients (fuse_attention_backward).
+#include <type_traits>
+
 #include "attention_tiles.h"
 
 namespace {
@@ -10,33 +12,6 @@ constexpr int kStep = 64;                  // keys, or rows, per step
 constexpr int kKeys = 64;                  // keys per block of their kernel
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// A wave's 32 columns of 32 DT dims, rounded, to rows of a matrix.
-template <typename T, int DT>
-__device__ __forceinline__ void write_columns(const f32x16 (&o)[DT], float f, T *row, int h, int dim)
-{
-    typedef T t4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (d * 32 + i * 8 + h * 4 < dim)
-                *reinterpret_cast<t4 *>(row + d * 32 + i * 8 + h * 4) =
-                    t4{(T)(o[d][i * 4] * f), (T)(o[d][i * 4 + 1] * f), (T)(o[d][i * 4 + 2] * f), (T)(o[d][i * 4 + 3] * f)};
-}
-
-// 0 where all of them are finite, NaN otherwise
-template <int DT>
-__device__ __forceinline__ float not_finite(const f32x16 (&o)[DT])
-{
-    float w = 0.0f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            w += o[d][i] - o[d][i];
-    return w;
-}
-
 // Gradient of the queries, and delta and lse, in the order of the rows, for the keys' kernel.  As the forward kernel: 32 rows per wave as columns, keys and values
 // step by step through LDS; the keys are read twice, as rows for S and transposed for t(K) t(dS).
 template <typename T, int DP>
@@ -45,6 +20,7 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
     using L = Tile<DP>;
     constexpr int kBytes = kStep * L::kRowBytes;
     __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][K, V]
+    __shared__ s16x8 spare[4][2][64];                                      // weights, see add_seen
 
     const int kvh = blockIdx.x % a.kv_heads;
     const Work work = work_of<false>(a, kRows, blockIdx.x / a.kv_heads);
@@ -98,68 +74,75 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
         col_at[i][1] = L::col_at(lane, i, 1);
     }
     f32x16 o[L::kCols];
-#pragma unroll
-    for (int d = 0; d < L::kCols; ++d)
-        o[d] = f32x16{};
     const float c = a.scale * kLog2e;
 
     const T *kbase = row_of<const T>(a.k, x.k0, kvh), *vbase = row_of<const T>(a.v, x.k0, kvh);
     const Fill<T, DP, kStep> fill(a.dim);
     if (a.dim < DP)
         clear_tiles(lds[0][0], sizeof lds);
-    if (end > 0) {
-        fill.load(lds[0][0], kbase, a.k.token, 0, x.nk);
-        fill.load(lds[0][1], vbase, a.v.token, 0, x.nk);
-    }
-    __syncthreads();
-    for (int j = 0, step = 0; j < end; j += kStep, ++step) {
-        const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
-        if (j + kStep < end) {
-            fill.load(lds[(step + 1) & 1][0], kbase, a.k.token, j + kStep, x.nk);
-            fill.load(lds[(step + 1) & 1][1], vbase, a.v.token, j + kStep, x.nk);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (j < seen_hi) {
+    auto sum_up = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                f32x16 p = {}, dp = {};
-#pragma unroll
-                for (int i = 0; i < L::kSteps; ++i) {
-                    p = product<T>(read_row(kt + n * 32 * L::kRowBytes, row_at[i]), q[i], p);
-                    dp = product<T>(read_row(vt + n * 32 * L::kRowBytes, row_at[i]), g[i], dp);
-                }
-                float w[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    w[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -lse2)) * (dp[i] - delta);
-                if (j + kStep > seen_lo) {
-                    const int left = seen - j - n * 32 - 4 * h;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (8 * (i / 4) + i % 4 >= left)
-                            w[i] = 0.0f;
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const s16x8 b = rounded<T>(w + u * 8);
-#pragma unroll
-                    for (int d = 0; d < L::kCols; ++d)
-                        o[d] = product<T>(read_col(kt + (n * 2 + u) * 16 * L::kRowBytes, col_at[d][0], col_at[d][1]), b, o[d]);
-                }
-            }
+        for (int d = 0; d < L::kCols; ++d)
+            o[d] = f32x16{};
+        if (end > 0) {
+            fill.load(lds[0][0], kbase, a.k.token, 0, x.nk);
+            fill.load(lds[0][1], vbase, a.v.token, 0, x.nk);
         }
         __syncthreads();
-    }
+        for (int j = 0, step = 0; j < end; j += kStep, ++step) {
+            const char *kt = lds[step & 1][0], *vt = lds[step & 1][1];
+            if (j + kStep < end) {
+                fill.load(lds[(step + 1) & 1][0], kbase, a.k.token, j + kStep, x.nk);
+                fill.load(lds[(step + 1) & 1][1], vbase, a.v.token, j + kStep, x.nk);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (j < seen_hi) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    f32x16 p = {}, dp = {};
+#pragma unroll
+                    for (int i = 0; i < L::kSteps; ++i) {
+                        p = product<T>(read_row(kt + n * 32 * L::kRowBytes, row_at[i]), q[i], p);
+                        dp = product<T>(read_row(vt + n * 32 * L::kRowBytes, row_at[i]), g[i], dp);
+                    }
+                    float w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        w[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -lse2)) * (dp[i] - delta);
+                    const bool masked = j + kStep > seen_lo;
+                    if (masked) {
+                        const int left = seen - j - n * 32 - 4 * h;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (8 * (i / 4) + i % 4 >= left)
+                                w[i] = 0.0f;
+                    }
+                    const s16x8 ds[2] = {rounded<T>(w), rounded<T>(w + 8)};
+                    if (CAREFUL && masked && holds_no_number<T, DP>(kt + n * 32 * L::kRowBytes, 32)) {
+                        spare[wave][0][lane] = ds[0];
+                        spare[wave][1][lane] = ds[1];
+                        wave_sees();
+                        add_seen<T, DP>(o, kt + n * 32 * L::kRowBytes, spare[wave][0], 64, 32, 0, seen - j - n * 32, 0);
+                        wave_sees();
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int d = 0; d < L::kCols; ++d)
+                                o[d] = product<T>(read_col(kt + (n * 2 + u) * 16 * L::kRowBytes, col_at[d][0], col_at[d][1]), ds[u], o[d]);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    };
+    sum_up(std::false_type());
+    if (any_wave(in && not_finite(o) != 0.0f, lds[0][0]))     // as in the forward kernel: 0 for a masked key, times a key that is not finite
+        sum_up(std::true_type());
 
-    // as in the forward kernel: 0 for a masked key, times a key that is not finite
-    const float worst = not_finite(o);
-    const unsigned long long bad = __ballot(in && worst != 0.0f);
-    if (in && worst == 0.0f)
+    if (in)
         write_columns<T>(o, a.scale, row_of<T>(a.dq, x.q0 + place, head), h, a.dim);
-    for (unsigned todo = (unsigned)(bad | (bad >> 32)); todo; todo &= todo - 1) {
-        const int again = first + wave * 32 + __builtin_ctz(todo), p = place_of(a, again);
-        query_grad_row<T>(a, x, p, kvh * a.group + again - p * a.group);
-    }
 }
 
 // Gradients of the keys and values: 64 keys per block, the rows that see them step by step through LDS, all query heads of the key
@@ -210,9 +193,6 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
         col_at[i][1] = L::col_at(lane, half * kHalfCols + i, 1);
     }
     f32x16 dk[kHalfCols], dv[kHalfCols];
-#pragma unroll
-    for (int d = 0; d < kHalfCols; ++d)
-        dk[d] = dv[d] = f32x16{};
     const float c = a.scale * kLog2e;
 
     const T *qbase = row_of<const T>(a.q, x.q0, kvh * a.group), *gbase = row_of<const T>(a.dout, x.q0, kvh * a.group);
@@ -239,90 +219,96 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
     };
     if (a.dim < DP)
         clear_tiles(lds[0][0], sizeof lds);
-    if (begin < rows)
-        load(0, begin);
-    __syncthreads();
-    for (int r0 = begin, B = 0; r0 < rows; r0 += kStep, B ^= 1) {
-        const char *qt = lds[B][0], *gt = lds[B][1];
-        const bool work = r0 + half * 32 + 32 > from_lo;
-        f32x4u lse[4], delta[4];           // of rows 8 i + 4 h ..; behind the last row they are anything, and masked
-        if (work) {
-            const long long at = sbase + r0 + half * 32 + 4 * h;
+    auto sum_up = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                lse[i] = *reinterpret_cast<const f32x4u *>(a.lse2 + at + 8 * i);
-                delta[i] = *reinterpret_cast<const f32x4u *>(a.delta + at + 8 * i);
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (r0 + kStep < rows)
-            load(B ^ 1, r0 + kStep);
-        __builtin_amdgcn_sched_barrier(0);
-        if (work) {
-            f32x16 p = {}, dp = {};
+        for (int d = 0; d < kHalfCols; ++d)
+            dk[d] = dv[d] = f32x16{};
+        if (begin < rows)
+            load(0, begin);
+        __syncthreads();
+        for (int r0 = begin, B = 0; r0 < rows; r0 += kStep, B ^= 1) {
+            const char *qt = lds[B][0], *gt = lds[B][1];
+            const bool work = r0 + half * 32 + 32 > from_lo;
+            f32x4u lse[4], delta[4];           // of rows 8 i + 4 h ..; behind the last row they are anything, and masked
+            if (work) {
+                const long long at = sbase + r0 + half * 32 + 4 * h;
 #pragma unroll
-            for (int i = 0; i < L::kSteps; ++i) {
-                p = product<T>(read_row(qt + half * 32 * L::kRowBytes, row_at[i]), k[i], p);
-                dp = product<T>(read_row(gt + half * 32 * L::kRowBytes, row_at[i]), v[i], dp);
-            }
-            ahead<L::kSteps * 2, 6>();
-            float w[16], ds[16];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -lse[i][u]));
-                    ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - delta[i][u]);
+                for (int i = 0; i < 4; ++i) {
+                    lse[i] = *reinterpret_cast<const f32x4u *>(a.lse2 + at + 8 * i);
+                    delta[i] = *reinterpret_cast<const f32x4u *>(a.delta + at + 8 * i);
                 }
             }
-            if (r0 + half * 32 < from_hi || r0 + half * 32 + 32 > rows) {
-                const int skip = from - r0 - half * 32 - 4 * h, left = rows - r0 - half * 32 - 4 * h;
+            __builtin_amdgcn_sched_barrier(0);
+            if (r0 + kStep < rows)
+                load(B ^ 1, r0 + kStep);
+            __builtin_amdgcn_sched_barrier(0);
+            if (work) {
+                f32x16 p = {}, dp = {};
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (8 * (i / 4) + i % 4 < skip || 8 * (i / 4) + i % 4 >= left)
-                        w[i] = ds[i] = 0.0f;
-            }
+                for (int i = 0; i < L::kSteps; ++i) {
+                    p = product<T>(read_row(qt + half * 32 * L::kRowBytes, row_at[i]), k[i], p);
+                    dp = product<T>(read_row(gt + half * 32 * L::kRowBytes, row_at[i]), v[i], dp);
+                }
+                ahead<L::kSteps * 2, 6>();
+                float w[16], ds[16];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                exchange[keys][half][u][0][lane] = rounded<T>(w + u * 8);
-                exchange[keys][half][u][1][lane] = rounded<T>(ds + u * 8);
-            }
-        }
-        __syncthreads();
+                for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-            if (r0 + n * 32 + 32 > from_lo) {
+                    for (int u = 0; u < 4; ++u) {
+                        w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -lse[i][u]));
+                        ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - delta[i][u]);
+                    }
+                }
+                if (r0 + half * 32 < from_hi || r0 + half * 32 + 32 > rows) {
+                    const int skip = from - r0 - half * 32 - 4 * h, left = rows - r0 - half * 32 - 4 * h;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (8 * (i / 4) + i % 4 < skip || 8 * (i / 4) + i % 4 >= left)
+                            w[i] = ds[i] = 0.0f;
+                }
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const s16x8 bp = exchange[keys][n][u][0][lane], bs = exchange[keys][n][u][1][lane];
-                    const int at = (n * 2 + u) * 16 * L::kRowBytes;
-#pragma unroll
-                    for (int d = 0; d < kHalfCols; ++d)
-                        if (L::kCols % 2 == 0 || half * kHalfCols + d < L::kCols) {
-                            dv[d] = product<T>(read_col(gt + at, col_at[d][0], col_at[d][1]), bp, dv[d]);
-                            dk[d] = product<T>(read_col(qt + at, col_at[d][0], col_at[d][1]), bs, dk[d]);
-                        }
+                    exchange[keys][half][u][0][lane] = rounded<T>(w + u * 8);
+                    exchange[keys][half][u][1][lane] = rounded<T>(ds + u * 8);
                 }
             }
-        __syncthreads();
-    }
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+                if (r0 + n * 32 + 32 > from_lo) {
+                    const char *qn = qt + n * 32 * L::kRowBytes, *gn = gt + n * 32 * L::kRowBytes;
+                    const bool masked = r0 + n * 32 < from_hi || r0 + n * 32 + 32 > rows;
+                    if (CAREFUL && masked && (holds_no_number<T, DP>(qn, 32) || holds_no_number<T, DP>(gn, 32))) {
+                        const int low = from - r0 - n * 32, high = rows - r0 - n * 32;
+                        add_seen<T, DP>(dv, gn, exchange[keys][n][0][0], 2 * 64, 32, low, high, half * kHalfCols);
+                        add_seen<T, DP>(dk, qn, exchange[keys][n][0][1], 2 * 64, 32, low, high, half * kHalfCols);
+                        continue;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const s16x8 bp = exchange[keys][n][u][0][lane], bs = exchange[keys][n][u][1][lane];
+                        const int at = u * 16 * L::kRowBytes;
+#pragma unroll
+                        for (int d = 0; d < kHalfCols; ++d)
+                            if (L::kCols % 2 == 0 || half * kHalfCols + d < L::kCols) {
+                                dv[d] = product<T>(read_col(gn + at, col_at[d][0], col_at[d][1]), bp, dv[d]);
+                                dk[d] = product<T>(read_col(qn + at, col_at[d][0], col_at[d][1]), bs, dk[d]);
+                            }
+                    }
+                }
+            __syncthreads();
+        }
+    };
+    sum_up(std::false_type());
+    if (any_wave(in && not_finite(dk) + not_finite(dv) != 0.0f, lds[0][0]))   // 0 for a masked row, times a row that is not finite
+        sum_up(std::true_type());
 
-    // keys whose gradient is not finite in either half of the dims: again, by the first of the two waves
-    const float worst = not_finite(dk) + not_finite(dv);
-    unsigned long long bad = __ballot(in && worst != 0.0f);
-    unsigned (*not_numbers)[2] = reinterpret_cast<unsigned (*)[2]>(lds[0][0]);     // (all waves are behind the last barrier)
-    if (lane == 0)
-        not_numbers[half][keys] = (unsigned)(bad | (bad >> 32));
-    __syncthreads();
-    unsigned todo = not_numbers[0][keys] | not_numbers[1][keys];
-    if (in && !((todo >> (lane & 31)) & 1)) {
+    if (in) {
         const int d0 = half * kHalfCols * 32;
         write_columns<T>(dk, a.scale, row_of<T>(a.dk, x.k0 + key, kvh) + d0, h, a.dim - d0);
         write_columns<T>(dv, 1.0f, row_of<T>(a.dv, x.k0 + key, kvh) + d0, h, a.dim - d0);
     }
-    if (half == 0)
-        for (; todo; todo &= todo - 1)
-            key_grad_row<T>(a, x, key0 + __builtin_ctz(todo), kvh);
 }
 
 // delta and lse2, each with room for a last step's rows behind the last row

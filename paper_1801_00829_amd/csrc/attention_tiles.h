@@ -113,8 +113,7 @@ __device__ __forceinline__ s16x8 read_col(const char *lds, int first, int second
 
 // Brings ROWS rows of a matrix to LDS by THREADS threads, straight from memory: a wave's load writes 64 chunks one behind the other, so
 // each lane asks for the chunk that belongs in its place.  Nothing waits here; the barrier that ends a step waits for the loads.
-// Rows from `end` on hold the last row instead: their scores are masked, and what a weight of 0 makes of a value that is not finite
-// is looked for where the results are written.  Chunks behind dim are left as they are (clear_tiles).
+// Rows from `end` on hold the last row instead: they are masked.  Chunks behind dim are left as they are (clear_tiles).
 template <typename T, int DP, int ROWS, int THREADS = 256>
 struct Fill {
     using L = Tile<DP>;
@@ -166,6 +165,80 @@ struct Fill {
     }
 };
 
+// Whether any of `rows` rows of a tile in LDS holds a value that is not finite (0 times it is no number), for a whole wave.
+template <typename T, int DP>
+__device__ __forceinline__ bool holds_no_number(const char *tile, int rows)
+{
+    float s = 0.0f;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+#pragma clang loop unroll(disable)
+    for (int at = lane * 16; at < rows * Tile<DP>::kRowBytes; at += 1024) {
+        typedef T t2 __attribute__((ext_vector_type(2)));
+        const uint4 v = *reinterpret_cast<const uint4 *>(tile + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const t2 x = __builtin_bit_cast(t2, i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+            s = fmaf((float)x[0], 0.0f, fmaf((float)x[1], 0.0f, s));
+        }
+    }
+    return __any(s != 0.0f);
+}
+
+// o += (transposed tile) x weights as the products make it, but pair by pair and without the masked ones.  A masked pair's weight is 0,
+// which the matrix units multiply all the same: no number where the tile's value is not finite.  The second run of a block, whose
+// first one ended with such results, looks for such values in the steps with a mask and comes here if there are any.
+//   weights: the B operands of `rows` rows, [rows / 16][lane], `stride` of them apart; rows low .. high count for this lane's column;
+//   d0: the first of the ND times 32 dims.
+template <typename T, int DP, int ND>
+__device__ __forceinline__ void add_seen(f32x16 (&o)[ND], const char *tile, const s16x8 *weights, int stride, int rows, int low, int high, int d0)
+{
+    using L = Tile<DP>;
+#pragma clang loop unroll(disable)
+    for (int r = 0; r < rows; ++r) {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));     // (places are worked out here, where they are needed, and not kept in registers meanwhile)
+        const int h = lane >> 5;
+        const s16x8 *w8 = weights + (r >> 4) * stride + (lane & 31) + ((r >> 2) & 1) * 32;
+        const T w = reinterpret_cast<const T *>(w8)[(r & 3) + ((r >> 3) & 1) * 4];
+        if (r < low || r >= high)
+            continue;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+            if (d0 + d < L::kCols)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = (d0 + d) * 4 + i;        // the chunk of dims 8 c .., of which this half has four
+                    const T *v = reinterpret_cast<const T *>(tile + r * L::kRowBytes + ((c ^ L::turn(r)) << 4) + h * 8);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[d][i * 4 + e] = fmaf((float)w, (float)v[e], o[d][i * 4 + e]);
+                    __builtin_amdgcn_sched_barrier(0);     // (one after the other: no registers for more, which the products need)
+                }
+    }
+}
+
+// Whether any of the block's four waves says so; `lds`: 16 bytes that nothing is kept in.  Begins and ends as all waves do.
+__device__ __forceinline__ bool any_wave(bool v, char *lds)
+{
+    unsigned *said = reinterpret_cast<unsigned *>(lds);
+    const bool mine = __any(v);
+    if ((threadIdx.x & 63) == 0)
+        said[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    const uint4 all = *reinterpret_cast<const uint4 *>(lds);
+    __syncthreads();
+    return (all.x | all.y | all.z | all.w) != 0;
+}
+
+// What this wave has written to LDS may be read by its other lanes.
+__device__ __forceinline__ void wave_sees()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Zeros in all places of a kernel's tiles, where some stand for dims behind dim; ends with a barrier.
 __device__ __forceinline__ void clear_tiles(char *lds, int bytes)
 {
@@ -185,6 +258,33 @@ __device__ __forceinline__ void operands(s16x8 (&b)[DP / 16], const T *row, bool
         if (in && (s * 2 + h) * 8 < dim)
             b[s] = *reinterpret_cast<const s16x8 *>(row + (s * 2 + h) * 8);
     }
+}
+
+// 0 where all of them are finite, no number otherwise
+template <int DT>
+__device__ __forceinline__ float not_finite(const f32x16 (&o)[DT])
+{
+    float w = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            w += o[d][i] - o[d][i];
+    return w;
+}
+
+// A wave's 32 columns of 32 DT dims, rounded, to rows of a matrix.
+template <typename T, int DT>
+__device__ __forceinline__ void write_columns(const f32x16 (&o)[DT], float f, T *row, int h, int dim)
+{
+    typedef T t4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d * 32 + i * 8 + h * 4 < dim)
+                *reinterpret_cast<t4 *>(row + d * 32 + i * 8 + h * 4) =
+                    t4{(T)(o[d][i * 4] * f), (T)(o[d][i * 4 + 1] * f), (T)(o[d][i * 4 + 2] * f), (T)(o[d][i * 4 + 3] * f)};
 }
 
 }  // namespace fuse

@@ -378,6 +378,39 @@ def test_attention_masked_values_have_no_influence():
             assert dk[41:].isfinite().all() and dv[41:].isfinite().all()
 
 
+def test_attention_one_bad_value_reaches_what_sees_it():
+    """A value that is not finite: NaN or an infinity in its own dim of every query that sees it, and nowhere else."""
+    for dtype, dim in (("fp16", 128), ("bf16", 40)):
+        c = attn_case(19, dtype, 4, 2, dim, [210, 66])
+        clean, lse = check_forward(c)
+        c["v"][130, 1, 7] = math.inf
+        ref, _, far, _ = R.attention(c["q"], c["k"], c["v"], c["offsets"])
+        out, lse2 = F.fuse_attention(c["q"], c["k"], c["v"], **offs(c))
+        assert torch.equal(lse, lse2)
+        hit = ~ref.isfinite()
+        assert hit[130:210, 2:, 7].all() and int(hit.sum()) == 80 * 2
+        assert (~out.isfinite()).cpu().equal(hit)
+        R.within(out.cpu()[~hit], ref[~hit], far[~hit], "out")
+        # gradients: a bad query reaches the keys it sees, a bad key the queries that see it
+        c = attn_case(20, dtype, 2, 1, dim, [140])
+        out, lse = check_forward(c)
+        # what the bad value does not reach is the clean inputs' gradient within its bound, not to the bit: the sums of steps with
+        # such a value run in another order than the matrix units', with other fp32 roundings, which the bound counts
+        good = R.attention_grad(c["dout"], c["q"], c["k"], c["v"], out, lse, c["offsets"])
+        c["k"][90, 0, 3] = math.nan
+        dq, _, _ = F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, **offs(c))
+        R.within(dq[:90], good[0][0][:90], good[0][1][:90], "dq")
+        assert not dq[90:].isfinite().any()
+        c["k"][90, 0, 3] = 0.0
+        good = R.attention_grad(c["dout"], c["q"], c["k"], c["v"], out, lse, c["offsets"])       # of the keys as they are now
+        c["q"][50, 1, 5] = math.inf
+        _, dk, dv = F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, **offs(c))
+        R.within(dk[51:], good[1][0][51:], good[1][1][51:], "dk")
+        R.within(dv[51:], good[2][0][51:], good[2][1][51:], "dv")
+        for t in (dk, dv):
+            assert not t[:51].isfinite().all()
+
+
 def test_attention_same_results_again_and_on_other_streams():
     c = attn_case(17, "bf16", 8, 2, 128, [300, 77])
     o = offs(c)
@@ -527,6 +560,26 @@ def test_training_step_of_a_block():
         # some twelve roundings to bf16 on the way of every value, each off by at most half a step: 12 * 2^-8 in the 2-norm
         err = float((g.double().cpu().view_as(w) - w).norm() / w.norm())
         assert err <= 12 * 2.0 ** -8, (name, err)
+
+
+def test_first_calls_inside_a_capture():
+    """Nothing has to be warmed up: calls of sizes and types that this process has not made are captured and replayed."""
+    g = gen(51)
+    q = rnd(g, (90, 5, 48), torch.float16).cuda()
+    x, w = rnd(g, (7, 12000), torch.float16).cuda(), rnd(g, (12000,), torch.float16).cuda()
+    off = torch.tensor([0, 90], dtype=torch.int64, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = F.fuse_attention(q, q, q, off)
+        h, y = F.fuse_block_norm(x, x, post=w, pre=w)
+        grads = F.fuse_block_norm_backward(x, x, h, x, post=w, pre=w)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = list(F.fuse_attention(q, q, q, off)) + list(F.fuse_block_norm(x, x, post=w, pre=w))
+        want += [t for t in F.fuse_block_norm_backward(x, x, h, x, post=w, pre=w) if t is not None]
+        assert all(torch.equal(a, b) for a, b in zip([out, lse, h, y] + [t for t in grads if t is not None], want))
 
 
 def test_training_step_in_two_graphs():
