@@ -94,8 +94,8 @@ __device__ __forceinline__ int seq_of_tile(const AttnArgs &a, const void *off, l
 // Tiles in the order of their work, as block `b` finds its own: with a causal mask the last rows see most keys, and the first keys are
 // seen by most rows, so tiles are taken by how far they are from the end of a sequence where that is little, most work first, over all
 // sequences: the tiles with M ones behind them before those with M - 1.  Long blocks that begin last are what other compute units
-// wait for: 8192 tokens in sequences of 2285, 2647 and 3260 take 333 us by sequence and 305 us in this order (queries' gradient),
-// 572 and 466 us (keys').  Beyond kSorted sequences the search costs more than it gives: then they go one after the other.
+// wait for: 8192 tokens in sequences of 2285, 2647 and 3260 take 333 us by sequence and 314 us in this order (queries' gradient),
+// 572 and 521 us (keys').  Beyond kSorted sequences the search costs more than it gives: then they go one after the other.
 constexpr int kSorted = 16;
 
 struct Work {

@@ -12,14 +12,18 @@ constexpr int kStep = 64;                  // keys, or rows, per step
 constexpr int kKeys = 64;                  // keys per block of their kernel
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// Gradient of the queries, and delta and lse, in the order of the rows, for the keys' kernel.  As the forward kernel: 32 rows per wave as columns, keys and values
-// step by step through LDS; the keys are read twice, as rows for S and transposed for t(K) t(dS).
+// Gradient of the queries, and delta and lse, in the order of the rows, for the keys' kernel.  As the forward kernel: 32 rows per wave
+// as columns, keys and values step by step through LDS; the keys are read twice, as rows for S and transposed for t(K) t(dS).
+//
+// Scores are taken twice, here and for the keys: one kernel for all three gradients would have to add up those of the queries over
+// blocks of keys, by atomics in an order that changes or through memory.  8192 packed tokens, 32 heads over 8 of dim 128: 315 us here
+// (three products, 0.9 PFLOP/s) and 475 us for the keys (four products, 0.8 PFLOP/s).
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const AttnArgs a)
 {
     using L = Tile<DP>;
     constexpr int kBytes = kStep * L::kRowBytes;
-    __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step & 1][K, V]
+    __shared__ __attribute__((aligned(256))) char lds[2][2][kBytes];       // [step % 2][K, V]
     __shared__ s16x8 spare[4][2][64];                                      // weights, see add_seen
 
     const int kvh = blockIdx.x % a.kv_heads;
@@ -29,7 +33,7 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
     const Seq &x = work.x;
     const int first = work.first, rows = x.nq * a.group;
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int r = first + wave * 32 + (lane & 31);
     const bool in = r < rows;
     const int place = place_of(a, in ? r : rows - 1), head = kvh * a.group + (in ? r : rows - 1) - place * a.group;
@@ -153,7 +157,8 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
 // instead of 128: with those, next to 64 of keys and values, nothing is left to load operands ahead of the products.
 //
 // EVEN: the rows of one pass of a tile's loads are whole tokens (the group divides their number), so they lie the same distance from
-// the next pass's and their addresses are scalars: 572 against 481 us for a group of four.  Else every row's place is divided out.
+// the next pass's and their addresses are scalars: 481 against 521 us for a group of four.  Else every row's place is divided out (the
+// two in one kernel: 78 against 68 us for a group of three).
 template <typename T, int DP, bool EVEN>
 __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnArgs a)
 {
