@@ -53,19 +53,19 @@ __device__ __forceinline__ Seq seq_at(const AttnArgs &a, int s)
     return x;
 }
 
-// The same in scalar registers, for a sequence that is the same for the whole wave.
-__device__ __forceinline__ long long uniform(long long v)
+// Lane `from`'s sequence, in scalar registers: a lookup by many lanes is one round of loads, not another one for the one that is found.
+__device__ __forceinline__ long long of_lane(long long v, int from)
 {
-    return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)v) |
-                       (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+    return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)v, from) |
+                       (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), from) << 32);
 }
-__device__ __forceinline__ Seq uniform(const Seq &v)
+__device__ __forceinline__ Seq of_lane(const Seq &v, int from)
 {
     Seq x;
-    x.q0 = uniform(v.q0);
-    x.k0 = uniform(v.k0);
-    x.nq = __builtin_amdgcn_readfirstlane(v.nq);
-    x.nk = __builtin_amdgcn_readfirstlane(v.nk);
+    x.q0 = of_lane(v.q0, from);
+    x.k0 = of_lane(v.k0, from);
+    x.nq = __builtin_amdgcn_readlane(v.nq, from);
+    x.nk = __builtin_amdgcn_readlane(v.nk, from);
     return x;
 }
 
@@ -73,22 +73,41 @@ __device__ __forceinline__ Seq uniform(const Seq &v)
 // floor(offset / tile) + s, which leaves it at least as many tiles as it needs (some stay empty).
 __host__ __device__ inline long long first_tile(long long rows_before, int s, int tile) { return rows_before / tile + s; }
 
-// The sequence that tile t belongs to: the last one that starts at or before it.  A wave looks at 64 sequences per step.
-__device__ __forceinline__ int seq_of_tile(const AttnArgs &a, const void *off, long long tokens, int rows_per_token, int tile, long long t)
+// A tile of a sequence: of its keys, or of its rows.
+struct Work {
+    Seq x;
+    int first;                             // first row, or key
+    bool any;
+};
+
+// Tile t, sequence by sequence: the sequence is the last one that starts at or before it.  A wave looks at 64 sequences per step.
+template <bool KEYS>
+__device__ __forceinline__ Work tile_at(const AttnArgs &a, int tile, long long t)
 {
     const int lane = threadIdx.x & 63;
-    int found = 0;
+    Work w = {};
+    long long start = 0;
     for (int base = 0; base < a.seqs; base += 64) {
         const int s = base + lane;
+        Seq x = {};
+        long long at = 0;
         bool starts = false;
-        if (s < a.seqs)
-            starts = first_tile(min(max(offset_at(off, s, a.off64), 0LL), tokens) * rows_per_token, s, tile) <= t;
+        if (s < a.seqs) {
+            x = seq_at(a, s);
+            at = first_tile(KEYS ? x.k0 : x.q0 * a.group, s, tile);
+            starts = at <= t;
+        }
         const unsigned long long m = __ballot(starts);
         if (!m)
             break;
-        found = base + 63 - __builtin_clzll(m);
+        const int found = 63 - __builtin_clzll(m);
+        w.x = of_lane(x, found);
+        start = of_lane(at, found);
     }
-    return __builtin_amdgcn_readfirstlane(found);
+    const long long first = (t - start) * tile;
+    w.any = first < (KEYS ? (long long)w.x.nk : (long long)w.x.nq * a.group);
+    w.first = (int)first;
+    return w;
 }
 
 // Tiles in the order of their work, as block `b` finds its own: with a causal mask the last rows see most keys, and the first keys are
@@ -98,29 +117,18 @@ __device__ __forceinline__ int seq_of_tile(const AttnArgs &a, const void *off, l
 // 572 and 521 us (keys').  Beyond kSorted sequences the search costs more than it gives: then they go one after the other.
 constexpr int kSorted = 16;
 
-struct Work {
-    Seq x;
-    int first;                             // first row, or key
-    bool any;
-};
-
 // KEYS: tiles of keys, the first ones first; else of rows, the last ones first.
 template <bool KEYS>
 __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
 {
+    if (a.seqs > kSorted)
+        return tile_at<KEYS>(a, tile, b);
     Work w;
-    if (a.seqs > kSorted) {
-        const int s = KEYS ? seq_of_tile(a, a.k_off, a.k_tokens, 1, tile, b) : seq_of_tile(a, a.q_off, a.q_tokens, a.group, tile, b);
-        w.x = uniform(seq_at(a, s));
-        const long long at = (b - first_tile(KEYS ? w.x.k0 : w.x.q0 * a.group, s, tile)) * tile;
-        w.any = at < (KEYS ? (long long)w.x.nk : (long long)w.x.nq * a.group);
-        w.first = (int)at;
-        return w;
-    }
     const int lane = threadIdx.x & 63;
     int n = 0;                             // this lane's sequence's tiles
+    Seq x = {};
     if (lane < a.seqs) {
-        const Seq x = seq_at(a, lane);
+        x = seq_at(a, lane);
         n = ((KEYS ? x.nk : x.nq * a.group) + tile - 1) / tile;
     }
     int most = 0, total = 0;
@@ -153,7 +161,7 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
     for (int i = (int)b - before; i > 0; --i)
         have &= have - 1;
     const int s = __builtin_ctzll(have);
-    w.x = uniform(seq_at(a, s));
+    w.x = of_lane(x, s);
     w.first = (KEYS ? __builtin_amdgcn_readlane(n, s) - low : low - 1) * tile;
     return w;
 }

@@ -215,16 +215,14 @@ __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const 
 
 // Joins the splits of every row: a wave per row.  6 us for 512 rows of four splits, most of it the launch.
 template <typename T>
-__global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, const Parts parts, const int tile)
+__global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, const Parts parts)
 {
     const int kvh = blockIdx.x % a.kv_heads;
-    const long long t = blockIdx.x / a.kv_heads;
-    const int s = seq_of_tile(a, a.q_off, a.q_tokens, a.group, tile, t);
-    const Seq x = seq_at(a, s);
-    const long long first = (t - first_tile(x.q0 * a.group, s, tile)) * tile, rows = min(first + tile, (long long)x.nq * a.group);
-    const int lane = threadIdx.x & 63;
-    for (long long r = first + (threadIdx.x >> 6); r < rows; r += 4) {
-        const int place = (int)(r / a.group), head = kvh * a.group + (int)(r % a.group);
+    const Work work = tile_at<false>(a, kRows, blockIdx.x / a.kv_heads);
+    const Seq &x = work.x;
+    const int rows = work.any ? min(work.first + kRows, x.nq * a.group) : 0, lane = threadIdx.x & 63;
+    for (int r = work.first + (threadIdx.x >> 6); r < rows; r += 4) {
+        const int place = place_of(a, r), head = kvh * a.group + r - place * a.group;
         const long long at = part_at(a, parts, x.q0 + place, head, 0);
         const bool mine = lane < parts.splits;
         const float m = mine ? parts.m[at + lane] : -INFINITY, l = mine ? parts.l[at + lane] : 0.0f;
@@ -284,7 +282,7 @@ int launch(const AttnArgs &a, const Parts &p, unsigned tiles, hipStream_t s)
     int rc = launched("attention_kernel");
     if (rc || p.splits == 1)
         return rc;
-    attention_join_kernel<T><<<tiles * a.kv_heads, 256, 0, s>>>(a, p, kRows);
+    attention_join_kernel<T><<<tiles * a.kv_heads, 256, 0, s>>>(a, p);
     rc = launched("attention_join_kernel");
     if (!rc)
         set_last_kernel("attention_kernel");

@@ -229,10 +229,13 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
 #pragma unroll
         for (int d = 0; d < kHalfCols; ++d)
             dk[d] = dv[d] = f32x16{};
+        // from the last rows down: blocks that run at the same time see different first rows, but all of a sequence's last ones, so
+        // each step's tiles are in L2 for all of them (from the first rows up, half of what is read comes from behind it)
+        const int last = begin + (rows - 1 - begin) / kStep * kStep;
         if (begin < rows)
-            load(0, begin);
+            load(0, last);
         __syncthreads();
-        for (int r0 = begin, B = 0; r0 < rows; r0 += kStep, B ^= 1) {
+        for (int r0 = begin < rows ? last : begin - 1, B = 0; r0 >= begin; r0 -= kStep, B ^= 1) {
             const char *qt = lds[B][0], *gt = lds[B][1];
             const bool work = r0 + half * 32 + 32 > from_lo;
             f32x4u lse[4], delta[4];           // of rows 8 i + 4 h ..; behind the last row they are anything, and masked
@@ -245,8 +248,8 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (r0 + kStep < rows)
-                load(B ^ 1, r0 + kStep);
+            if (r0 > begin)
+                load(B ^ 1, r0 - kStep);
             __builtin_amdgcn_sched_barrier(0);
             if (work) {
                 f32x16 p = {}, dp = {};

@@ -12,6 +12,11 @@
 // 16 bytes of it per thread and step, so a row of up to 4096 columns of a 16 bit type is one step.  Statistics
 // of a layer norm are taken in two passes over the registers (mean, then squares of the differences): one pass of sums of
 // squares would lose the digits that a large mean has.
+//
+// 16384 x 4096 bf16, a norm on both sides and a gate per column: forward 99 us (5.4 TB/s), gradient 164 + 5 us (4.9 TB/s); a large copy
+// reaches 4.7 to 5.4 TB/s on the same card.  What it took: the next row loaded ahead (119 -> 101 us forward), sums by moves within the
+// registers instead of LDS (gradient 246 -> 203), branches around the columns' loops (203 -> 182), the next row asked for before the first sum
+// (182 -> 167).  Rows that are not on 16 bytes: 5003 x 1111 fp32, layer norms with a gate per cell, gradient 51 us (3.5 TB/s).
 #pragma once
 #include <algorithm>
 #include <atomic>
@@ -20,10 +25,9 @@
 
 namespace fuse {
 
-
 // Columns per thread and step: 16 bytes of a row, 32 of fp64.
 template <typename T> constexpr int kEach = sizeof(T) == 2 ? 8 : 4;
-constexpr int kMaxCols = 32768;            // 1024 threads x 4 steps
+constexpr int kMaxCols = 32768;            // 1024 threads, 32 columns each
 constexpr int kMaxThreads = 1024;
 constexpr int kGradBlocks = 512;           // blocks of a gradient call: each leaves one partial row of every column sum
 
@@ -367,6 +371,8 @@ __device__ __forceinline__ void leave_sum(const A (&v)[K][V], int lane, int mine
         }
 }
 
+// (Two blocks per compute unit for 16 bit types, which takes 128 registers: so does LAYER, with a few values in scratch memory.)
+//
 // Three sums per row at most: means (layer norms only); squares of h and z and what dy needs of h; what du needs of z.  The row after
 // this one is loaded meanwhile.
 template <typename T, int K, bool VEC, bool LAYER>
