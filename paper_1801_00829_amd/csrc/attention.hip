@@ -50,7 +50,8 @@ __device__ __forceinline__ void follow_max(float top, float c, float &m, float &
 // is visible) the matrix units are busy for 47 % of the time and the vector units for 52 %, mostly exp (a quarter of the rate of
 // other work); 489 us, 0.9 PFLOP/s.  Without its loads the same kernel takes 20 % less; four tiles of 32 KB each way from L2 per step
 // and compute unit do not hide entirely behind two blocks.  Tried without gain: the next step's scores among this one's exp
-// (500 to 510 us), transposed loads with waits of their own (509), a higher priority for waves in their products (528).
+// (500 to 510 us), transposed loads with waits of their own (509), a higher priority for waves in their products (528); blocks of 256
+// rows, which read half as much, take 472 us here but lose 4 to 24 % with fewer rows, fewer blocks or a dim of 64.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const AttnArgs a, const Parts parts)
 {

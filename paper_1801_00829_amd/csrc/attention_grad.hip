@@ -17,7 +17,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 //
 // Scores are taken twice, here and for the keys: one kernel for all three gradients would have to add up those of the queries over
 // blocks of keys, by atomics in an order that changes or through memory.  8192 packed tokens, 32 heads over 8 of dim 128: 315 us here
-// (three products, 0.9 PFLOP/s) and 475 us for the keys (four products, 0.8 PFLOP/s).
+// (three products, 0.9 PFLOP/s) and 440 us for the keys (four products, 0.85 PFLOP/s).
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const AttnArgs a)
 {
