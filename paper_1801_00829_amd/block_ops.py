@@ -106,31 +106,30 @@ def _block(x, z, gate, scale, post, pre, kind, eps, what):
     if kind not in NORM:
         raise ValueError("kind is 'rms' or 'layer', not %r" % (kind,))
     rows, cols = x.shape
-    b = L.Block(dtype=dtype, norm=NORM[kind], rows=rows, cols=cols, eps=float(eps), scale=float(scale), gate_kind=-1)
-    if z is not None:
-        b.z, b.z_ld = _rows_of(z, x, "z")
-    for name, p in (("post", post), ("pre", pre)):
-        w, bias = _weights(p)
-        if w is not None:
-            setattr(b, name + "_weight", _vector(w, x, cols, name + " weight"))
-        if bias is not None:
-            setattr(b, name + "_bias", _vector(bias, x, cols, name + " bias"))
+    zp, z_ld = (None, 0) if z is None else _rows_of(z, x, "z")
+    (post_w, post_b), (pre_w, pre_b) = _weights(post), _weights(pre)
+    post_wp = None if post_w is None else _vector(post_w, x, cols, "post weight")
+    post_bp = None if post_b is None else _vector(post_b, x, cols, "post bias")
+    pre_wp = None if pre_w is None else _vector(pre_w, x, cols, "pre weight")
+    pre_bp = None if pre_b is None else _vector(pre_b, x, cols, "pre bias")
     gk, gt = (None, None) if gate is None else gate
+    code, gp, g_ld = -1, None, 0
     if gk is not None:
         if gk not in ("rowvec", "colvec", "matrix"):
             raise ValueError("a gate is ('rowvec' | 'colvec' | 'matrix', tensor), not %r" % (gk,))
-        b.gate_kind = SIDE[gk]
+        code = SIDE[gk]
         if gk == "rowvec":
-            b.gate = _vector(gt, x, cols, "gate")
+            gp = _vector(gt, x, cols, "gate")
         elif gk == "matrix":
-            b.gate, b.gate_ld = _rows_of(gt, x, "gate")
+            gp, g_ld = _rows_of(gt, x, "gate")
         else:
             _like(gt, x, "gate")
             if gt.dim() != 1 or gt.numel() != rows:
                 raise ValueError("gate must be a vector of %d values" % rows)
-            b.gate, b.gate_ld = gt.data_ptr(), gt.stride(0) if rows > 1 else 1
+            gp, g_ld = gt.data_ptr(), gt.stride(0) if rows > 1 else 1
         if not gt.numel():
-            b.gate = x.data_ptr() or 16      # (no rows: never read)
+            gp = x.data_ptr() or 16              # (no rows: never read)
+    b = L.Block(dtype, NORM[kind], rows, cols, eps, scale, zp, z_ld, post_wp, post_bp, pre_wp, pre_bp, code, gp, g_ld)
     return b, gk, gt
 
 
@@ -148,11 +147,19 @@ def fuse_block_norm(x, z=None, gate=None, scale=1.0, post=None, pre=None, kind="
     xp, x_ld = _rows_of(x, x, "x")
 
     def call(handle):
-        rh = torch.empty_like(x, memory_format=torch.contiguous_format) if z is not None and h is None else h
-        ry = torch.empty_like(x, memory_format=torch.contiguous_format) if pre is not None and y is None else y
-        hp, h_ld = _rows_of(rh, x, "h") if rh is not None else (None, 0)
-        yp, y_ld = _rows_of(ry, x, "y") if ry is not None else (None, 0)
-        if x.numel():
+        rh, ry, hp, yp = h, y, None, None
+        h_ld = y_ld = b.cols
+        if h is not None:
+            hp, h_ld = _rows_of(h, x, "h")
+        elif z is not None:
+            rh = torch.empty_like(x, memory_format=torch.contiguous_format)
+            hp = rh.data_ptr()
+        if y is not None:
+            yp, y_ld = _rows_of(y, x, "y")
+        elif pre is not None:
+            ry = torch.empty_like(x, memory_format=torch.contiguous_format)
+            yp = ry.data_ptr()
+        if b.rows and b.cols:
             _check(L.load().fuse_block_norm(b, xp, x_ld, hp, h_ld, yp, y_ld, handle))
         return x if rh is None else rh, ry
 
@@ -254,9 +261,14 @@ def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=
     lib = L.load()
 
     def call(handle):
-        o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
-        l = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
-        op, o_token, o_head = _heads_of(o, q, "out", q.shape[0], q.shape[1])
+        n, heads, dim = q.shape
+        l = torch.empty((n, heads), dtype=torch.float32, device=q.device) if lse is None else lse
+        if out is None:
+            o = torch.empty_like(q, memory_format=torch.contiguous_format)
+            op, o_token, o_head = o.data_ptr(), heads * dim, dim
+        else:
+            o = out
+            op, o_token, o_head = _heads_of(o, q, "out", n, heads)
         nbytes = lib.fuse_attention_bytes(f)
         ws = _workspace(nbytes, q.device) if nbytes else None
         _check(lib.fuse_attention(f, op, o_token, o_head, l.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, handle))
