@@ -418,7 +418,7 @@ int fuse_block_norm_backward(const fuse_block *block, const void *dh, int64_t dh
  * queries' offsets); with k_lengths only the first k_lengths[s] of those keys: a cache with room for more.  Offsets and lengths are
  * device arrays of int32 or int64, non-decreasing from 0; they are not read on the host.  Values beyond
  * the arrays are cut down to them: no access leaves the arrays, whatever the offsets say.  Rows that belong to no sequence are
- * neither read nor written.
+ * neither read nor written.  Results overlap neither each other nor any input.
  * S and sums are fp32; exp(S - max) and the gradient of S are rounded to dtype before their products with V, Q, K and dout, as the
  * matrix units take them. */
 typedef struct {

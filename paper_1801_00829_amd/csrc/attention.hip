@@ -10,6 +10,7 @@ using namespace fuse;
 constexpr int kRows = 128;                 // rows per tile: 32 per wave
 constexpr int kKeys = 64;                  // keys per step
 constexpr int kMaxSplits = 64;
+constexpr int kJoinBlocks = 8;             // blocks that join a tile's rows: a row for each wave of 32 rows' worth
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Where a call's keys are split: unnormalised results and statistics of every row and split.
@@ -214,7 +215,7 @@ __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const 
     }
 }
 
-// Joins the splits of every row: a wave per row.  6 us for 512 rows of four splits, most of it the launch.
+// Joins the splits of every row: a wave per row.  6 to 7 us, most of it the launch.
 template <typename T>
 __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, const Parts parts)
 {
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
     const Work work = tile_at<false>(a, kRows, blockIdx.x / a.kv_heads);
     const Seq &x = work.x;
     const int rows = work.any ? min(work.first + kRows, x.nq * a.group) : 0, lane = threadIdx.x & 63;
-    for (int r = work.first + (threadIdx.x >> 6); r < rows; r += 4) {
+    for (int r = work.first + blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += 4 * kJoinBlocks) {
         const int place = place_of(a, r), head = kvh * a.group + r - place * a.group;
         const long long at = part_at(a, parts, x.q0 + place, head, 0);
         const bool mine = lane < parts.splits;
@@ -234,13 +235,23 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
         const float w = l == 0.0f ? 0.0f : exp2f((m - top) * (a.scale * kLog2e));
         const float sum = wave_sum(w * l);
         float o0 = 0.0f, o1 = 0.0f;
-        for (int i = 0; i < parts.splits; ++i) {
-            const float f = __shfl(w, i, 64);
-            const float *o = parts.o + (at + i) * a.dim;
-            if (lane < a.dim)
-                o0 = fmaf(f, o[lane], o0);
-            if (lane + 64 < a.dim)
-                o1 = fmaf(f, o[lane + 64], o1);
+        // eight splits' loads in flight, without a branch around them: one by one, 64 splits took 35 us
+        const float *o = parts.o + at * a.dim;
+        const int d0 = min(lane, a.dim - 1), d1 = min(lane + 64, a.dim - 1);
+        for (int i = 0; i < parts.splits; i += 8) {
+            float v0[8], v1[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int k = min(i + u, parts.splits - 1);
+                v0[u] = o[(long long)k * a.dim + d0];
+                v1[u] = o[(long long)k * a.dim + d1];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float f = __shfl(w, min(i + u, 63), 64);             // (0 behind the last split)
+                o0 = fmaf(f, v0[u], o0);
+                o1 = fmaf(f, v1[u], o1);
+            }
         }
         const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
         T *out = row_of<T>(a.out, x.q0 + place, head);
@@ -255,13 +266,17 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
 
 long long tiles_of(const fuse_attn *f) { return first_tile(f->q_tokens * (f->heads / f->kv_heads), (int)f->seqs, kRows); }
 
-// Splits of the keys: as many as it takes to have two blocks for each of 256 compute units, of at least eight steps each where all
-// sequences are equally long (a step takes about a microsecond alone, joining them a launch of five).
+// Splits of the keys: as many as it takes to have two blocks for each of 256 compute units, of at least four steps each where all
+// sequences are equally long (two: of at least eight): a step takes about a microsecond alone, the launch that joins them seven.  One token
+// of 32 heads over 8, dim 128, over 32768 places: 33 us with 64 splits; two tokens over 1500 places each: 17 us with splits of four steps,
+// 23 with splits of eight; 8 heads over 1, dim 64, over 512 places: 12 us without a split, 19 with two.
 int splits_of(const fuse_attn *f)
 {
     const long long blocks = tiles_of(f) * f->kv_heads, keys = f->k_tokens / (f->seqs > 0 ? f->seqs : 1);
     long long n = blocks > 0 ? 512 / blocks : 1;
-    n = n < keys / (8 * kKeys) ? n : keys / (8 * kKeys);
+    n = n < keys / (4 * kKeys) ? n : keys / (4 * kKeys);
+    if (n == 2 && keys < 16 * kKeys)
+        n = 1;
     return (int)(n < 1 ? 1 : n > kMaxSplits ? kMaxSplits : n);
 }
 
@@ -283,7 +298,7 @@ int launch(const AttnArgs &a, const Parts &p, unsigned tiles, hipStream_t s)
     int rc = launched("attention_kernel");
     if (rc || p.splits == 1)
         return rc;
-    attention_join_kernel<T><<<tiles * a.kv_heads, 256, 0, s>>>(a, p);
+    attention_join_kernel<T><<<dim3(tiles * a.kv_heads, kJoinBlocks), 256, 0, s>>>(a, p);
     rc = launched("attention_join_kernel");
     if (!rc)
         set_last_kernel("attention_kernel");

@@ -287,6 +287,8 @@ CROSS_CASES = {
     "no_keys": ("bf16", 4, 2, 128, [5, 3], [0, 9], None),
     "chunk": ("bf16", 4, 2, 128, [100, 64], [400, 1000], 1024),
     "chunk_long": ("fp16", 2, 1, 80, [40], [3000], None),
+    "token_many_splits": ("bf16", 4, 1, 64, [1], [20000], None),
+    "chunk_two_splits": ("bf16", 8, 2, 64, [900], [1500], None),
     "many": ("fp16", 16, 2, 128, [2] * 40, list(range(2, 162, 4)), 200),
 }
 
@@ -499,6 +501,88 @@ def test_grad_clip_values_that_are_no_numbers():
     assert float(F.fuse_grad_norm([torch.empty(0, device="cuda")])) == 0.0
     big_ = torch.full((3,), 3e38, device="cuda")
     assert abs(float(F.fuse_grad_norm([big_])) / (3e38 * math.sqrt(3.0)) - 1.0) < 1e-6     # squares beyond fp32
+
+
+# ---------------------------------------------------------------- large, and at once ---
+
+def test_attention_far_places():
+    """Keys and queries behind 2^31 elements."""
+    far, n, hk, hq, dim = 2200000, 100, 8, 16, 128
+    g = gen(61)
+    k, v = (torch.zeros(far + n, hk, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = attn_case(62, "bf16", hq, hk, dim, [3], [n])
+    k[far:], v[far:] = c["k"], c["v"]
+    off, key_off = (torch.tensor(x, dtype=torch.int64, device="cuda") for x in ([0, 0, 3], [0, far, far + n]))
+    out, lse = F.fuse_attention(c["q"], k, v, off, key_offsets=key_off)
+    ref, ref_lse, bound, bound_lse = R.attention(c["q"], c["k"], c["v"], c["offsets"], c["key_offsets"])
+    R.within(out, ref, bound, "out")
+    R.within(lse, ref_lse, bound_lse, "lse")
+    dq, dk, dv = F.fuse_attention_backward(c["dout"], c["q"], k, v, out, lse, off, key_offsets=key_off)
+    want = R.attention_grad(c["dout"], c["q"], c["k"], c["v"], out, lse, c["offsets"], c["key_offsets"])
+    for got, (value, far_), name in ((dq, want[0], "dq"), (dk[far:], want[1], "dk"), (dv[far:], want[2], "dv")):
+        R.within(got, value, far_, name)
+    assert not dk[:far:1001].any() and not dv[:far:1001].any()
+    del k, v, dk, dv
+    far, hq = 600000, 32
+    c = attn_case(63, "bf16", hq, hk, dim, [n])
+    q = torch.zeros(far + n, hq, dim, dtype=torch.bfloat16, device="cuda")
+    q[far:] = c["q"]
+    off, key_off = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, far, far + n], [0, 0, n]))
+    out, lse = F.fuse_attention(q, c["k"], c["v"], off, key_offsets=key_off)
+    ref, _, bound, _ = R.attention(c["q"], c["k"], c["v"], c["offsets"])
+    R.within(out[far:], ref, bound, "out")
+    assert not out[:far:997].any() and (lse[:far:997] == -math.inf).all()
+    torch.cuda.empty_cache()
+
+
+def test_norm_and_clip_far_places():
+    rows, cols = 540000, 4096                                      # 2.2e9 elements
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[-5:] = rnd(gen(64), (5, cols), torch.bfloat16).cuda()
+    w = rnd(gen(65), (cols,), torch.bfloat16, 0.2, 1.0).cuda()
+    h, y = F.fuse_block_norm(x, x, post=w, pre=w)
+    h5, y5 = F.fuse_block_norm(x[-5:].clone(), x[-5:].clone(), post=w, pre=w)
+    assert torch.equal(h[-5:], h5) and torch.equal(y[-5:], y5) and not h[:-5:1009].any()
+    got = F.fuse_block_norm_backward(x, x, h, x, post=w, pre=w)
+    five = F.fuse_block_norm_backward(x[-5:], x[-5:], h5, x[-5:], post=w, pre=w)
+    assert torch.equal(got.dx[-5:], five.dx) and torch.equal(got.dz[-5:], five.dz)
+    # the other rows add zeros; sums of five terms of size ten at most in two orders (fp32: 2 * 5 * 10 * 2^-24), both rounded to bf16
+    for a, b in ((got.dpre, five.dpre), (got.dpost, five.dpost)):
+        R.within(a, b, b.double().cpu().abs() * 2.0 ** -7 + 100 * R.F32, "dw")
+    del h, y, got
+    norm = F.fuse_grad_clip([x], 1.0)
+    total = math.sqrt(float(rnd(gen(64), (5, cols), torch.bfloat16).double().square().sum()))
+    assert abs(float(norm) - total) <= 1e-12 * total
+    assert abs(math.sqrt(float(x[-5:].double().square().sum())) - 1.0) < 2.0 ** -8       # clipped to 1, each cell rounded to bf16
+    del x
+    torch.cuda.empty_cache()
+
+
+def test_calls_of_several_threads():
+    import threading
+    cases = [step_state(71 + i) for i in range(3)]
+    want = [[t.clone() for t in step(s)] for s in cases]
+    torch.cuda.synchronize()
+    got, errors = [None] * 3, []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(5):
+                    got[i] = step(cases[i])
+            stream.synchronize()
+        except Exception as e:                                     # (looked at below, in the test's own thread)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for a, b in zip(got, want):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
 # ----------------------------------------------------------------------- all together ---
