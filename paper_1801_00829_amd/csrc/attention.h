@@ -80,29 +80,35 @@ struct Work {
     bool any;
 };
 
-// Tile t, sequence by sequence: the sequence is the last one that starts at or before it.  A wave looks at 64 sequences per step.
+// Tile t, sequence by sequence: the sequence is the last one that starts at or before it.  A wave looks at 64 sequences at a time, first
+// far apart, then between the two that are left: two rounds of loads for 4096 sequences, three for 262144.
 template <bool KEYS>
 __device__ __forceinline__ Work tile_at(const AttnArgs &a, int tile, long long t)
 {
     const int lane = threadIdx.x & 63;
     Work w = {};
     long long start = 0;
-    for (int base = 0; base < a.seqs; base += 64) {
-        const int s = base + lane;
+    int low = 0;
+    for (int step = (a.seqs + 63) / 64;; step = (step + 63) / 64) {
+        const long long s = low + (long long)lane * step;
         Seq x = {};
         long long at = 0;
         bool starts = false;
         if (s < a.seqs) {
-            x = seq_at(a, s);
-            at = first_tile(KEYS ? x.k0 : x.q0 * a.group, s, tile);
+            x = seq_at(a, (int)s);
+            at = first_tile(KEYS ? x.k0 : x.q0 * a.group, (int)s, tile);
             starts = at <= t;
         }
         const unsigned long long m = __ballot(starts);
         if (!m)
-            break;
+            return w;
         const int found = 63 - __builtin_clzll(m);
-        w.x = of_lane(x, found);
-        start = of_lane(at, found);
+        low += found * step;
+        if (step == 1) {
+            w.x = of_lane(x, found);
+            start = of_lane(at, found);
+            break;
+        }
     }
     const long long first = (t - start) * tile;
     w.any = first < (KEYS ? (long long)w.x.nk : (long long)w.x.nq * a.group);

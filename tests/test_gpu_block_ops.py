@@ -274,6 +274,7 @@ ATTN_CASES = {
     "group_3": ("fp16", 6, 2, 80, [129, 63]),
     "long": ("bf16", 4, 2, 128, [600, 257]),
     "seventy": ("bf16", 2, 2, 64, [1, 3, 0, 7, 33, 2, 64] * 10),
+    "thousands": ("bf16", 1, 1, 16, [1, 0, 2] * 1700),
     "dim_96": ("fp16", 2, 1, 96, [191]),
     "dim_104": ("bf16", 3, 1, 104, [150]),
     "dim_24": ("bf16", 2, 1, 24, [150, 20]),
