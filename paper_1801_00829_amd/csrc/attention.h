@@ -20,6 +20,8 @@ struct AttnArgs {
     Mat q, k, v, out, dout, dq, dk, dv;
     float *lse;                            // q_tokens x heads
     float *delta, *lse2;                   // gradients: sum of dout o out, and lse in base 2; see stat_at
+    float *parts;                          // gradients of keys and values by split: (key token, key head, split, K or V) x dim
+    int splits;
     const void *q_off, *k_off, *k_len;     // k_len NULL: the distances of k_off
     long long q_tokens, k_tokens;
     int seqs, heads, kv_heads, group, dim, causal, off64;

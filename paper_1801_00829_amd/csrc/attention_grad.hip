@@ -1,4 +1,5 @@
 // Attention over packed sequences, gradients (fuse_attention_backward).
+#include <algorithm>
 #include <type_traits>
 
 #include "attention_tiles.h"
@@ -10,6 +11,7 @@ using namespace fuse;
 constexpr int kRows = 128;                 // rows per block: 32 per wave
 constexpr int kStep = 64;                  // keys, or rows, per step
 constexpr int kKeys = 64;                  // keys per block of their kernel
+constexpr int kJoinBlocks = 4;             // blocks that join a tile's splits
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Gradient of the queries, and delta and lse, in the order of the rows, for the keys' kernel.  As the forward kernel: 32 rows per wave
@@ -169,7 +171,9 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
     // (80 KB for a dim of 128: two blocks per compute unit, whose steps overlap)
 
     const int kvh = blockIdx.x % a.kv_heads;
-    const Work tile = work_of<true>(a, kKeys, blockIdx.x / a.kv_heads);
+    const unsigned rest = blockIdx.x / a.kv_heads;
+    const int split = rest % a.splits;
+    const Work tile = work_of<true>(a, kKeys, rest / a.splits);
     if (!tile.any)
         return;
     const Seq &x = tile.x;
@@ -179,8 +183,10 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), keys = wave & 1, half = wave >> 1;
     const int key0 = first + keys * 32, key = key0 + (lane & 31);
     const bool in = key < x.nk;
-    // the rows that see a key: from row from(key) on
-    const int rows = x.nq * a.group, begin = first_that_sees(a, x, first) * a.group;
+    // the rows that see a key: from row from(key) on; this split's steps: rows begin .. of those that any key of the tile has
+    const int rows = x.nq * a.group, seen = first_that_sees(a, x, first) * a.group;
+    const int steps = (rows - seen + kStep - 1) / kStep, per = (steps + a.splits - 1) / a.splits;
+    const int begin = seen + min(split * per, steps) * kStep, last = seen + (min((split + 1) * per, steps) - 1) * kStep;
     const int from = first_that_sees(a, x, min(key, x.nk - 1)) * a.group;
     const int from_lo = key0 < x.nk ? __builtin_amdgcn_readfirstlane(from) : rows;
     const int from_hi = __builtin_amdgcn_readlane(from, 31);
@@ -231,11 +237,10 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
             dk[d] = dv[d] = f32x16{};
         // from the last rows down: blocks that run at the same time see different first rows, but all of a sequence's last ones, so
         // each step's tiles are in L2 for all of them (from the first rows up, half of what is read comes from behind it)
-        const int last = begin + (rows - 1 - begin) / kStep * kStep;
-        if (begin < rows)
+        if (begin <= last)
             load(0, last);
         __syncthreads();
-        for (int r0 = begin < rows ? last : begin - 1, B = 0; r0 >= begin; r0 -= kStep, B ^= 1) {
+        for (int r0 = last, B = 0; r0 >= begin; r0 -= kStep, B ^= 1) {
             const char *qt = lds[B][0], *gt = lds[B][1];
             const bool work = r0 + half * 32 + 32 > from_lo;
             f32x4u lse[4], delta[4];           // of rows 8 i + 4 h ..; behind the last row they are anything, and masked
@@ -312,15 +317,75 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
     if (any_wave(in && not_finite(dk) + not_finite(dv) != 0.0f, lds[0][0]))   // 0 for a masked row, times a row that is not finite
         sum_up(std::true_type());
 
-    if (in) {
-        const int d0 = half * kHalfCols * 32;
+    const int d0 = half * kHalfCols * 32;
+    if (in && a.splits > 1) {
+        float *part = a.parts + (((x.k0 + key) * a.kv_heads + kvh) * a.splits + split) * 2 * a.dim + d0;
+        write_columns<float>(dk, a.scale, part, h, a.dim - d0);
+        write_columns<float>(dv, 1.0f, part + a.dim, h, a.dim - d0);
+    } else if (in) {
         write_columns<T>(dk, a.scale, row_of<T>(a.dk, x.k0 + key, kvh) + d0, h, a.dim - d0);
         write_columns<T>(dv, 1.0f, row_of<T>(a.dv, x.k0 + key, kvh) + d0, h, a.dim - d0);
     }
 }
 
-// delta and lse2, each with room for a last step's rows behind the last row
-size_t backward_bytes(const fuse_attn *f) { return ((size_t)f->q_tokens * f->heads + kStep) * 2 * sizeof(float); }
+// Adds the splits of the keys' and values' gradients, in order.
+template <typename T>
+__global__ void __launch_bounds__(256) attention_key_join_kernel(const AttnArgs a)
+{
+    const int kvh = blockIdx.x % a.kv_heads;
+    const Work tile = tile_at<true>(a, kKeys, blockIdx.x / a.kv_heads);
+    if (!tile.any)
+        return;
+    const int quads = a.dim / 4, all = min(kKeys, tile.x.nk - tile.first) * 2 * quads;
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < all; i += 256 * kJoinBlocks) {
+        const int d = i % quads * 4, which = i / quads & 1;
+        const long long token = tile.x.k0 + tile.first + i / quads / 2;
+        const float *part = a.parts + ((token * a.kv_heads + kvh) * a.splits * 2 + which) * a.dim + d;
+        f32x4 sum = {};
+        for (int s = 0; s < a.splits; s += 4) {
+            f32x4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                v[u] = *reinterpret_cast<const f32x4 *>(part + (long long)min(s + u, a.splits - 1) * 2 * a.dim);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (s + u < a.splits)
+                    sum += v[u];
+        }
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<t4 *>(row_of<T>(which ? a.dv : a.dk, token, kvh) + d) = t4{(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
+    }
+}
+
+// Splits of the rows in the keys' kernel: as many as it takes to have two blocks for each of 256 compute units, of at least four steps each
+// where all sequences are equally long and half of the pairs are masked.
+int key_splits(const fuse_attn *f)
+{
+    if (f->seqs == 0)
+        return 1;
+    const long long blocks = first_tile(f->k_tokens, (int)f->seqs, kKeys) * f->kv_heads;
+    const long long steps = f->q_tokens * (f->heads / f->kv_heads) / f->seqs / kStep / 2;
+    const long long n = std::min(512 / blocks, steps / 4);
+    return (int)(n < 1 ? 1 : n > 32 ? 32 : n);
+}
+
+// delta and lse2, each with room for a last step's rows behind the last row, and the splits' sums
+size_t stat_floats(const fuse_attn *f) { return ((size_t)f->q_tokens * f->heads + kStep + 3) / 4 * 4; }
+size_t backward_bytes(const fuse_attn *f)
+{
+    const int splits = key_splits(f);
+    return (stat_floats(f) * 2 + (splits > 1 ? (size_t)f->k_tokens * f->kv_heads * splits * 2 * f->dim : 0)) * sizeof(float);
+}
+
+template <typename T, int DP>
+int launch_keys(const AttnArgs &a, unsigned blocks, hipStream_t s)
+{
+    if (Fill<T, DP, kStep>::kPerPass % a.group == 0)
+        attention_key_grad_kernel<T, DP, true><<<blocks, 256, 0, s>>>(a);
+    else
+        attention_key_grad_kernel<T, DP, false><<<blocks, 256, 0, s>>>(a);
+    return launched("attention_key_grad_kernel");
+}
 
 template <typename T, int DP>
 int launch_dim(const AttnArgs &a, hipStream_t s)
@@ -331,13 +396,19 @@ int launch_dim(const AttnArgs &a, hipStream_t s)
         if (const int rc = launched("attention_query_grad_kernel"))
             return rc;
     }
-    if (a.k_tokens > 0) {
-        if (Fill<T, DP, kStep>::kPerPass % a.group == 0)
-            attention_key_grad_kernel<T, DP, true><<<(unsigned)(k_tiles * a.kv_heads), 256, 0, s>>>(a);
-        else
-            attention_key_grad_kernel<T, DP, false><<<(unsigned)(k_tiles * a.kv_heads), 256, 0, s>>>(a);
+    if (a.k_tokens == 0)
+        return FUSE_OK;
+    const unsigned blocks = (unsigned)(k_tiles * a.kv_heads);
+    if (a.splits > 1) {
+        if (const int rc = launch_keys<T, DP>(a, blocks * a.splits, s))
+            return rc;
+        attention_key_join_kernel<T><<<dim3(blocks, kJoinBlocks), 256, 0, s>>>(a);
+        const int rc = launched("attention_key_join_kernel");
+        if (!rc)
+            set_last_kernel("attention_key_grad_kernel");
+        return rc;
     }
-    return launched("attention_key_grad_kernel");
+    return launch_keys<T, DP>(a, blocks, s);
 }
 
 template <typename T>
@@ -374,7 +445,9 @@ int backward_impl(const fuse_attn *f, const fuse_attn_grads *g, void *workspace,
     a.dv = {g->dv, g->dv_token_ld, g->dv_head_ld};
     a.lse = const_cast<float *>(g->lse);
     a.delta = static_cast<float *>(workspace);
-    a.lse2 = a.delta + f->q_tokens * f->heads + kStep;
+    a.lse2 = a.delta + stat_floats(f);
+    a.parts = a.lse2 + stat_floats(f);
+    a.splits = key_splits(f);
     return f->dtype == FUSE_BF16 ? launch_grads<__bf16>(a, (hipStream_t)stream) : launch_grads<_Float16>(a, (hipStream_t)stream);
 }
 
@@ -384,7 +457,7 @@ extern "C" {
 
 size_t fuse_attention_backward_bytes(const fuse_attn *attn)
 {
-    return attn && attn->q_tokens > 0 && attn->heads > 0 ? backward_bytes(attn) : 0;
+    return fuse::check_attn(attn) || attn->q_tokens == 0 ? 0 : backward_bytes(attn);
 }
 
 int fuse_attention_backward(const fuse_attn *attn, const fuse_attn_grads *grads, void *workspace, size_t workspace_bytes, void *stream)

@@ -274,6 +274,8 @@ ATTN_CASES = {
     "group_3": ("fp16", 6, 2, 80, [129, 63]),
     "long": ("bf16", 4, 2, 128, [600, 257]),
     "seventy": ("bf16", 2, 2, 64, [1, 3, 0, 7, 33, 2, 64] * 10),
+    "shared_by_8": ("bf16", 8, 1, 128, [700, 90, 0]),
+    "shared_by_6": ("fp16", 6, 1, 80, [1, 801]),
     "thousands": ("bf16", 1, 1, 16, [1, 0, 2] * 1700),
     "dim_96": ("fp16", 2, 1, 96, [191]),
     "dim_104": ("bf16", 3, 1, 104, [150]),
@@ -412,6 +414,18 @@ def test_attention_one_bad_value_reaches_what_sees_it():
         R.within(dv[51:], good[2][0][51:], good[2][1][51:], "dv")
         for t in (dk, dv):
             assert not t[:51].isfinite().all()
+
+
+def test_attention_bad_values_where_rows_are_split():
+    c = attn_case(22, "bf16", 8, 1, 64, [640])                     # the keys' gradients are sums of several blocks
+    out, lse = check_forward(c)
+    good = R.attention_grad(c["dout"], c["q"], c["k"], c["v"], out, lse, c["offsets"])
+    c["dout"][300, 5, 9] = math.nan
+    c["q"][301, 2, 1] = math.inf
+    _, dk, dv = F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, **offs(c))
+    R.within(dk[302:], good[1][0][302:], good[1][1][302:], "dk")
+    R.within(dv[302:], good[2][0][302:], good[2][1][302:], "dv")
+    assert not dv[:301].isfinite().all()
 
 
 def test_attention_same_results_again_and_on_other_streams():
