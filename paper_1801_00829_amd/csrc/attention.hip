@@ -24,17 +24,30 @@ __device__ __forceinline__ long long part_at(const AttnArgs &a, const Parts &p, 
     return (token * a.heads + head) * p.splits + split;
 }
 
+// What a column's weights are multiplied with before they are rounded, as a power of two (LIFT), and how many powers of two the maximum
+// that they are taken against may lag behind (SLACK).  Every weight is at most 2^(LIFT + SLACK), and the sum, which carries the same factor, is
+// at least 2^LIFT.
+//
+// bf16 has fp32's range: nothing to lift.  fp16 ends at 2^16 and is coarser below 2^-14, so weights take its whole range: those down to
+// 2^-25 of the largest one are rounded by half a step of their own value, and smaller ones by 2^-36 of the sum at most.  Unlifted,
+// a weight of 2^-25 would be 0, and many of them next to one key that takes almost all of the weight (with a value near 0) are what the
+// result is made of.  The slack decides how often results are rescaled: 12288 packed tokens, 32 heads over 8, dim 128, fp16 take 492 us with
+// lift 11 and slack 4 as with 7 and 8, 499 us with 13 and 2, 515 us with 15 and 0.
+template <typename T> constexpr int kLift = 0;
+template <typename T> constexpr int kSlack = 8;
+template <> constexpr int kLift<_Float16> = 11;
+template <> constexpr int kSlack<_Float16> = 4;
+
 // Running maximum and sum of a column, and its 32 new scores: rescales the result's DT tiles where the maximum has moved.
 //
-// The maximum that is subtracted is not always the largest score so far: it is moved only when a score is more than 2^8 times
-// larger, so that most steps leave the results as they are.  exp is then at most 2^8, well inside every type's range, and the
-// rounding of a 16 bit type is relative, so nothing is lost.
-template <int DT>
+// The maximum that is subtracted is not always the largest score so far: it is moved only when a score's weight is more than 2^SLACK times
+// larger, so that most steps leave the results as they are.
+template <typename T, int DT>
 __device__ __forceinline__ void follow_max(float top, float c, float &m, float &mc, float &l, f32x16 (&o)[DT])
 {
-    if (!__any((top - m) * c > 8.0f))
+    if (!__any((top - m) * c > (float)kSlack<T>))
         return;
-    const float next = fmaxf(m, top), to = next == -INFINITY ? 0.0f : next * c;
+    const float next = fmaxf(m, top), to = (next == -INFINITY ? 0.0f : next * c) - (float)kLift<T>;
     const float f = m == -INFINITY ? 0.0f : exp2f(mc - to);
     m = next;
     mc = to;
@@ -42,6 +55,13 @@ __device__ __forceinline__ void follow_max(float top, float c, float &m, float &
 #pragma unroll
     for (int d = 0; d < DT; ++d)
         o[d] *= f;
+}
+
+// log of a sum of lifted weights
+template <typename T>
+__device__ __forceinline__ float log_of(float sum)
+{
+    return logf(sum * (1.0f / (1 << kLift<T>)));
 }
 
 // One block: 128 rows, 32 per wave as columns (attention_tiles.h), the keys and values that they see in steps of 64 through LDS, loaded
@@ -147,7 +167,7 @@ __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const 
 #pragma unroll
                 for (int i = 1; i < 32; ++i)
                     top = fmaxf(top, p[i / 16][i % 16]);
-                follow_max<L::kCols>(both_max(top), c, m, mc, l, o);
+                follow_max<T, L::kCols>(both_max(top), c, m, mc, l, o);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     p[i / 16][i % 16] = __builtin_amdgcn_exp2f(fmaf(p[i / 16][i % 16], c, -mc));
@@ -211,7 +231,7 @@ __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const 
     if (in) {
         write_columns<T>(o, f, row_of<T>(a.out, x.q0 + place, head), h, a.dim);
         if (a.lse && h == 0)
-            a.lse[(x.q0 + place) * a.heads + head] = l == 0.0f ? -INFINITY : fmaf(m, a.scale, logf(l));
+            a.lse[(x.q0 + place) * a.heads + head] = l == 0.0f ? -INFINITY : fmaf(m, a.scale, log_of<T>(l));
     }
 }
 
@@ -260,7 +280,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
         if (lane + 64 < a.dim)
             out[lane + 64] = (T)(o1 * f);
         if (a.lse && lane == 0)
-            a.lse[(x.q0 + place) * a.heads + head] = sum == 0.0f ? -INFINITY : fmaf(top, a.scale, logf(sum));
+            a.lse[(x.q0 + place) * a.heads + head] = sum == 0.0f ? -INFINITY : fmaf(top, a.scale, log_of<T>(sum));
     }
 }
 
