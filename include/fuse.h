@@ -420,7 +420,8 @@ int fuse_block_norm_backward(const fuse_block *block, const void *dh, int64_t dh
  * the arrays are cut down to them: no access leaves the arrays, whatever the offsets say.  Rows that belong to no sequence are
  * neither read nor written.  Results overlap neither each other nor any input.
  * S and sums are fp32; exp(S - max) and the gradient of S are rounded to dtype before their products with V, Q, K and dout, as the
- * matrix units take them. */
+ * matrix units take them; for FUSE_F16 multiplied with powers of two first, so that small ones keep their digits and large ones stay
+ * within its range. */
 typedef struct {
     int32_t dtype, heads, kv_heads, dim;
     int32_t causal, offsets_are_64;

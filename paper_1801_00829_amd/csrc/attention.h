@@ -20,6 +20,7 @@ struct AttnArgs {
     Mat q, k, v, out, dout, dq, dk, dv;
     float *lse;                            // q_tokens x heads
     float *delta, *lse2;                   // gradients: sum of dout o out, and lse in base 2; see stat_at
+    int *lifts;                            // gradients in fp16: of every 32 rows, see lift_at
     float *parts;                          // gradients of keys and values by split: (key token, key head, split, K or V) x dim
     int splits;
     const void *q_off, *k_off, *k_len;     // k_len NULL: the distances of k_off
@@ -78,6 +79,7 @@ __host__ __device__ inline long long first_tile(long long rows_before, int s, in
 // A tile of a sequence: of its keys, or of its rows.
 struct Work {
     Seq x;
+    int seq;
     int first;                             // first row, or key
     bool any;
 };
@@ -108,6 +110,7 @@ __device__ __forceinline__ Work tile_at(const AttnArgs &a, int tile, long long t
         low += found * step;
         if (step == 1) {
             w.x = of_lane(x, found);
+            w.seq = low;
             start = of_lane(at, found);
             break;
         }
@@ -131,7 +134,7 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
 {
     if (a.seqs > kSorted)
         return tile_at<KEYS>(a, tile, b);
-    Work w;
+    Work w = {};
     const int lane = threadIdx.x & 63;
     int n = 0;                             // this lane's sequence's tiles
     Seq x = {};
@@ -146,7 +149,6 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
         total += m;
     }
     w.any = (int)b < total;
-    w.first = 0;
     if (!w.any)
         return w;
     // the largest M with more than b tiles that have at least M - 1 behind them: 64 values of M at a time
@@ -170,6 +172,7 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
         have &= have - 1;
     const int s = __builtin_ctzll(have);
     w.x = of_lane(x, s);
+    w.seq = s;
     w.first = (KEYS ? __builtin_amdgcn_readlane(n, s) - low : low - 1) * tile;
     return w;
 }
@@ -203,6 +206,13 @@ __device__ __forceinline__ T *row_of(const Mat &m, long long token, int head)
 __device__ __forceinline__ long long stat_at(const AttnArgs &a, long long token, int head)
 {
     return (head / a.group * a.q_tokens + token) * a.group + head % a.group;
+}
+
+// Place of the lift of a sequence's rows r .. r + 31 (r a multiple of 32): key heads x tiles of 32 rows.
+__host__ __device__ inline long long lift_tiles(const AttnArgs &a) { return first_tile(a.q_tokens * a.group, a.seqs, 32); }
+__device__ __forceinline__ long long lift_at(const AttnArgs &a, const Work &w, int kvh, int r)
+{
+    return kvh * lift_tiles(a) + first_tile(w.x.q0 * a.group, w.seq, 32) + r / 32;
 }
 
 // Checks of both directions, and the arguments that both have (host).

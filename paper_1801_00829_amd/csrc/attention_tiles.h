@@ -231,6 +231,21 @@ __device__ __forceinline__ bool any_wave(bool v, char *lds)
     return (all.x | all.y | all.z | all.w) != 0;
 }
 
+// The least of all 256 threads' values, in a scalar register; `lds` as above.
+__device__ __forceinline__ int least_of_block(int v, char *lds)
+{
+    int *said = reinterpret_cast<int *>(lds);
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1)
+        v = min(v, __shfl_xor(v, i, 64));
+    if ((threadIdx.x & 63) == 0)
+        said[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const int4 all = *reinterpret_cast<const int4 *>(lds);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(min(min(all.x, all.y), min(all.z, all.w)));
+}
+
 // What this wave has written to LDS may be read by its other lanes.
 __device__ __forceinline__ void wave_sees()
 {

@@ -63,3 +63,78 @@ def test_attention_small_weights_beside_a_large_one(score, value, keys, queries,
             R.within(out, ref, far, "out")
             _, want, _, far_lse = R.attention(c["q"], c["k"], c["v"], c["offsets"], c["key_offsets"], None, causal, 1.0)
             R.within(lse, want, far_lse, "lse")
+
+
+def gradients(c, out, lse, causal, scale):
+    """((dq, bound), (dk, bound), (dv, bound)).  P and dS are rounded to half a step of their own values, or in fp16 to 2^-40 and to 2^-36 of
+    the largest dS of the row (dq) or of the rows of all heads that share the key head (dk) where that is more."""
+    t = c["q"].dtype
+    sub = 1.0 if t == torch.float16 else 0.0
+    dout, q, k, v, out, lse = (x.double().cpu() for x in (c["dout"], c["q"], c["k"], c["v"], out, lse))
+    group, d = q.shape[1] // k.shape[1], q.shape[2]
+    dq, dk, dv = (torch.zeros_like(x) for x in (q, k, v))
+    fq, fk, fv = (torch.zeros_like(x) for x in (q, k, v))
+    for qs, ks in R.sequences(c["offsets"], c["key_offsets"], c["key_lengths"]):
+        n = (qs.stop - qs.start) * group
+        if not n or ks.stop == ks.start:
+            continue
+        more = (max(n, ks.stop - ks.start) // 16 + 16) * R.F32
+        for hk in range(k.shape[1]):
+            kh, vh = k[ks, hk], v[ks, hk]
+            found = []
+            for h in range(hk * group, hk * group + group):
+                s = R._scores(q[qs, h], kh, scale, causal)
+                seen = (s != -math.inf).double()
+                p = seen * torch.exp(s - lse[qs, h][:, None])
+                off, size = R._spread(q[qs, h], kh, scale), (dout[qs, h] * out[qs, h]).abs().sum(1)[:, None]
+                ds = p * (dout[qs, h] @ vh.T - (dout[qs, h] * out[qs, h]).sum(1)[:, None])
+                fds = 1.05 * ((R.half_step(t) + off + more) * ds.abs() + p * (d + 8) * 2 * R.F32 * (dout[qs, h].abs() @ vh.abs().T + size))
+                found.append((h, seen, p, ds, fds, off))
+            top = max(float(x[3].abs().max()) for x in found)
+            for h, seen, p, ds, fds, off in found:
+                dq[qs, h] = scale * (ds @ kh)
+                fq[qs, h] = scale * (fds + sub * 2.0 ** -36 * seen * ds.abs().amax(1, keepdim=True)) @ kh.abs()
+                dk[ks, hk] += scale * (ds.T @ q[qs, h])
+                fk[ks, hk] += scale * (fds + sub * 2.0 ** -36 * top * seen).T @ q[qs, h].abs()
+                dv[ks, hk] += p.T @ dout[qs, h]
+                fv[ks, hk] += 1.05 * ((R.half_step(t) + off + more) * p + sub * 2.0 ** -40 * seen).T @ dout[qs, h].abs()
+    return (dq, fq + rounded(dq, t)), (dk, fk + rounded(dk, t)), (dv, fv + rounded(dv, t))
+
+
+def check_gradients(c, causal=True, scale=None):
+    scale = c["q"].shape[2] ** -0.5 if scale is None else scale
+    out, lse = F.fuse_attention(c["q"], c["k"], c["v"], **offs(c), causal=causal, scale=scale)
+    got = F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, **offs(c), causal=causal, scale=scale)
+    for x, (want, far), name in zip(got, gradients(c, out, lse, causal, scale), ("dq", "dk", "dv")):
+        R.within(x, want, far, name)
+    return got
+
+
+@pytest.mark.parametrize("dtype,heads,kv_heads,dim,lens", [("fp16", 2, 1, 128, [2048]), ("fp16", 4, 4, 64, [701, 0, 300]), ("fp16", 3, 1, 80, [900]),
+                                                           ("fp16", 16, 2, 64, [5] * 40), ("bf16", 2, 1, 128, [700])])
+@pytest.mark.parametrize("size", [1e-2, 1e-3, 1e-4])
+def test_attention_small_gradients(dtype, heads, kv_heads, dim, lens, size):
+    for causal in (True, False):
+        c = attn_case(82, dtype, heads, kv_heads, dim, lens)
+        c["dout"] = rnd(gen(83), c["dout"].shape, DT[dtype], size).cuda()
+        check_gradients(c, causal)
+
+
+def test_attention_large_gradients():
+    """dS beyond fp16's range where dq, dk and dv are within it."""
+    for dim, lens in ((64, [500, 3]), (128, [200])):
+        c = attn_case(84, "fp16", 4, 2, dim, lens)
+        c["v"].mul_(20.0)
+        c["dout"].mul_(1000.0)
+        got = check_gradients(c, scale=0.01)
+        assert all(x.isfinite().all() for x in got)
+
+
+def test_attention_gradients_of_different_sizes():
+    """A few queries with gradients much larger than all the others': what does not see them keeps its digits."""
+    c = attn_case(85, "fp16", 2, 1, 64, [900, 300])
+    c["dout"].mul_(1e-3)
+    c["dout"][[0, 1, 40, 899, 1000]] *= 1e4
+    check_gradients(c)
+    c["v"][500] *= 100.0                                           # one key with a value much larger than the others', met midway
+    check_gradients(c)
