@@ -267,11 +267,12 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
                 v1[u] = o[(long long)k * a.dim + d1];
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float f = __shfl(w, min(i + u, 63), 64);             // (0 behind the last split)
-                o0 = fmaf(f, v0[u], o0);
-                o1 = fmaf(f, v1[u], o1);
-            }
+            for (int u = 0; u < 8; ++u)
+                if (i + u < parts.splits) {                                // (its weight would be 0, but not 0 times what is not finite)
+                    const float f = __shfl(w, i + u, 64);
+                    o0 = fmaf(f, v0[u], o0);
+                    o1 = fmaf(f, v1[u], o1);
+                }
         }
         const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
         T *out = row_of<T>(a.out, x.q0 + place, head);

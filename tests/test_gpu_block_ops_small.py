@@ -138,3 +138,19 @@ def test_attention_gradients_of_different_sizes():
     check_gradients(c)
     c["v"][500] *= 100.0                                           # one key with a value much larger than the others', met midway
     check_gradients(c)
+
+
+@pytest.mark.parametrize("dtype,keys", [("bf16", 800), ("fp16", 1400), ("bf16", 2048), ("fp16", 2600)])
+def test_attention_infinite_values_where_keys_are_split(dtype, keys):
+    """An infinite value that all queries see, in the first, a middle or the last split, is an infinity in its own dim, whatever the splits."""
+    c = attn_case(86, dtype, 4, 2, 72, [1], [keys])
+    ref, _, far, _ = R.attention(c["q"], c["k"], c["v"], c["offsets"], c["key_offsets"])
+    hit = torch.zeros(ref.shape, dtype=torch.bool)
+    hit[:, 2:, 5] = True
+    for at in (0, keys // 2, keys - 1):
+        for bad in (math.inf, -math.inf):
+            c["v"][at, 1, 5], kept = bad, float(c["v"][at, 1, 5])
+            out = F.fuse_attention(c["q"], c["k"], c["v"], **offs(c))[0].cpu()
+            c["v"][at, 1, 5] = kept
+            assert (out[hit] == bad).all(), (at, bad)
+            R.within(out[~hit], ref[~hit], far[~hit], "out")
