@@ -165,7 +165,8 @@ struct Fill {
     }
 };
 
-// Whether any of `rows` rows of a tile in LDS holds a value that is not finite (0 times it is no number), for a whole wave.
+// Whether any of `rows` rows of a tile in LDS holds a value that is not finite (0 times it is no number), for a whole wave.  Places that a
+// row leaves free (dims of 65 to 96) hold what an earlier block left there and are not looked at: results would depend on it.
 template <typename T, int DP>
 __device__ __forceinline__ bool holds_no_number(const char *tile, int rows)
 {
@@ -174,7 +175,10 @@ __device__ __forceinline__ bool holds_no_number(const char *tile, int rows)
     asm volatile("" : "+v"(lane));
 #pragma clang loop unroll(disable)
     for (int at = lane * 16; at < rows * Tile<DP>::kRowBytes; at += 1024) {
+        using L = Tile<DP>;
         typedef T t2 __attribute__((ext_vector_type(2)));
+        if (L::kUsed < L::kChunks && (((at >> 4) % L::kChunks) ^ L::turn(at / L::kRowBytes)) >= L::kUsed)
+            continue;
         const uint4 v = *reinterpret_cast<const uint4 *>(tile + at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

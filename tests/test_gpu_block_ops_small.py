@@ -154,3 +154,31 @@ def test_attention_infinite_values_where_keys_are_split(dtype, keys):
             c["v"][at, 1, 5] = kept
             assert (out[hit] == bad).all(), (at, bad)
             R.within(out[~hit], ref[~hit], far[~hit], "out")
+
+
+def test_attention_results_do_not_depend_on_earlier_calls():
+    """Results that are not finite send a block through its tiles again; what earlier kernels left in LDS has no say in that."""
+    def before(value, t):
+        x = torch.full((20000, 4, 128), value, dtype=t, device="cuda")
+        off = torch.arange(0, 20001, 50, dtype=torch.int32, device="cuda")
+        o, l = F.fuse_attention(x, x, x, off)
+        F.fuse_attention_backward(x, x, x, x, o, l, off)
+
+    for dtype, dim in (("bf16", 96), ("fp16", 96), ("bf16", 88), ("fp16", 128), ("bf16", 64)):
+        c = attn_case(87, dtype, 8, 4, dim, [200, 130, 31] * 4)
+        o = offs(c)
+        out, lse = F.fuse_attention(c["q"], c["k"], c["v"], **o)
+        c["v"][::50, :, 3] = math.inf
+        bad_q, bad_k = c["q"].clone(), c["k"].clone()
+        bad_q[::70, :, 1] = math.inf
+        bad_k[::90, :, 2] = math.nan
+        found = []
+        for value in (0.0, math.nan, 0.0, math.inf):
+            before(value, DT[dtype])
+            got = list(F.fuse_attention(c["q"], c["k"], c["v"], **o))
+            before(value, DT[dtype])
+            got += F.fuse_attention_backward(c["dout"], bad_q, bad_k, c["q"][:, :4].contiguous(), out, lse, **o)
+            torch.cuda.synchronize()
+            found.append([t.view(torch.int32 if t.dtype == torch.float32 else torch.int16) for t in got])
+        for again in found[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(found[0], again)), (dtype, dim)
