@@ -439,7 +439,8 @@ int fuse_attention(const fuse_attn *attn, void *out, int64_t out_token_ld, int64
                    size_t workspace_bytes, void *stream);
 
 /* The gradients of q, k and v, given dout, the gradient of out, and the forward call's out and lse.  Keys that no query sees
- * get 0.  Gradients of a shared key head are summed over its query heads. */
+ * get 0.  Gradients of a shared key head are summed over its query heads.  Rows that belong to no sequence -- before the first and
+ * behind the last one, and behind a sequence's k_lengths -- are left as they were; fuse_attention_zero_rest sets those of dq, dk and dv to 0 (NULL: not that one's), and nothing else. */
 typedef struct {
     const void *dout, *out;  const float *lse;
     int64_t dout_token_ld, dout_head_ld, out_token_ld, out_head_ld;
@@ -449,6 +450,7 @@ typedef struct {
 size_t fuse_attention_backward_bytes(const fuse_attn *attn);
 int fuse_attention_backward(const fuse_attn *attn, const fuse_attn_grads *grads, void *workspace, size_t workspace_bytes,
                             void *stream);
+int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads, void *stream);
 
 /* The norm of all gradients, and clipping by it.
  *   fuse_grad_norm : norm[0] = sqrt(sum over the tensors of the sum of squares of their cells), one fp64 value

@@ -121,6 +121,7 @@ def load():
                        ("fuse_block_norm_backward", [P(Block), vp, i64, vp, i64, vp, i64, P(BlockGrads), vp, size, vp]),
                        ("fuse_attention", [P(Attn), vp, i64, i64, vp, vp, size, vp]),
                        ("fuse_attention_backward", [P(Attn), P(AttnGrads), vp, size, vp]),
+                       ("fuse_attention_zero_rest", [P(Attn), P(AttnGrads), vp]),
                        ("fuse_grad_norm", [vp, i64, vp, vp, size, vp]),
                        ("fuse_grad_clip", [vp, i64, f64, f64, vp, vp, vp, size, vp])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, ci

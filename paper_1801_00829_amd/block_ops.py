@@ -279,7 +279,10 @@ def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=
 
 def fuse_attention_backward(dout, q, k, v, out, lse, offsets, key_offsets=None, key_lengths=None, causal=True, scale=None,
                             dq=None, dk=None, dv=None, stream=None):
-    """C: fuse_attention_backward.  Gradients (dq, dk, dv) of fuse_attention's out, given its results and its other arguments."""
+    """C: fuse_attention_backward.  Gradients (dq, dk, dv) of fuse_attention's out, given its results and its other arguments.
+
+    dq, dk, dv: tensors to write to.  Rows that belong to no sequence (before the first and behind the last one, and behind a sequence's
+    key_lengths) are left as they were in these, and 0 in results made here."""
     f = _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale)
     if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != q.device:
         raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % (tuple(q.shape[:2]), q.device))
@@ -291,6 +294,10 @@ def fuse_attention_backward(dout, q, k, v, out, lse, offsets, key_offsets=None, 
               (("dout", dout, q), ("out", out, q), ("dq", got[0], q), ("dk", got[1], k), ("dv", got[2], v))]
         g = L.AttnGrads(at[0][0], at[1][0], lse.data_ptr(), *at[0][1:], *at[1][1:], at[2][0], at[3][0], at[4][0], *at[2][1:], *at[3][1:],
                         *at[4][1:])
+        if dq is None or dk is None or dv is None:
+            own = L.AttnGrads.from_buffer_copy(g)
+            own.dq, own.dk, own.dv = [a[0] if t is None else None for a, t in zip(at[2:], (dq, dk, dv))]
+            _check(lib.fuse_attention_zero_rest(f, own, handle))
         ws = _workspace(lib.fuse_attention_backward_bytes(f), q.device)
         _check(lib.fuse_attention_backward(f, g, ws.data_ptr(), ws.numel(), handle))
         return tuple(got)

@@ -418,6 +418,41 @@ __global__ void __launch_bounds__(256) attention_key_join_kernel(const AttnArgs 
     }
 }
 
+// Zeros in the rows of no sequence, in those of dq, dk and dv that are given: block x takes the rows between two sequences (before the first
+// one, behind the last one), y some of them, z = 0 those of the queries, z = 1 those of the keys.  3 us where there are none.
+__global__ void __launch_bounds__(256) attention_rest_kernel(const AttnArgs a)
+{
+    constexpr int kTokens = 16;            // at a time
+    const bool keys = blockIdx.z == 1;
+    if (keys ? !a.dk.p && !a.dv.p : !a.dq.p)
+        return;
+    const int heads = keys ? a.kv_heads : a.heads, chunks = a.dim / 8, per = heads * chunks;
+    for (int s = blockIdx.x; s <= a.seqs; s += gridDim.x) {
+        long long begin = 0, end = keys ? a.k_tokens : a.q_tokens;
+        if (s > 0) {
+            const Seq x = seq_at(a, s - 1);
+            begin = keys ? x.k0 + x.nk : x.q0 + x.nq;
+        }
+        if (s < a.seqs) {
+            const Seq x = seq_at(a, s);
+            end = keys ? x.k0 : x.q0;
+        }
+        for (long long t = begin + blockIdx.y * kTokens; t < end; t += gridDim.y * kTokens)
+            for (int i = threadIdx.x; i < per * kTokens; i += 256) {
+                const long long token = t + i / per;
+                const int head = i % per / chunks, d = i % chunks * 8;
+                if (token >= end)
+                    break;
+                if (!keys)
+                    *reinterpret_cast<uint4 *>(row_of<short>(a.dq, token, head) + d) = make_uint4(0, 0, 0, 0);
+                if (keys && a.dk.p)
+                    *reinterpret_cast<uint4 *>(row_of<short>(a.dk, token, head) + d) = make_uint4(0, 0, 0, 0);
+                if (keys && a.dv.p)
+                    *reinterpret_cast<uint4 *>(row_of<short>(a.dv, token, head) + d) = make_uint4(0, 0, 0, 0);
+            }
+    }
+}
+
 // Splits of the rows in the keys' kernel: as many as it takes to have five blocks for each of 256 compute units (two run at a time, and
 // they are not equally long), of at least three steps each where all sequences are equally long and half of the pairs are masked.  Whole
 // backward passes, without splits and with them: 2048 tokens, 32 heads over 1, dim 128: 1639 and 200 us; two sequences of 2048, 32 over 4: 499 and
@@ -485,6 +520,36 @@ int launch_grads(const AttnArgs &a, hipStream_t s)
     return a.dim <= 64 ? launch_dim<T, 64>(a, s) : a.dim <= 96 ? launch_dim<T, 96>(a, s) : launch_dim<T, 128>(a, s);
 }
 
+// The arguments of both calls: the inputs and the results.
+AttnArgs grad_args(const fuse_attn *f, const fuse_attn_grads *g)
+{
+    AttnArgs a = attn_args(f);
+    a.dq = {g->dq, g->dq_token_ld, g->dq_head_ld};
+    a.dk = {g->dk, g->dk_token_ld, g->dk_head_ld};
+    a.dv = {g->dv, g->dv_token_ld, g->dv_head_ld};
+    return a;
+}
+
+int zero_rest_impl(const fuse_attn *f, const fuse_attn_grads *g, void *stream)
+{
+    report(FUSE_OK, "");
+    int rc = check_attn(f);
+    if (rc)
+        return rc;
+    if (!g)
+        return report(FUSE_EINVAL, "grads is NULL");
+    if ((g->dq && (rc = check_rows(f, g->dq, g->dq_token_ld, g->dq_head_ld, f->heads, f->q_tokens, "dq"))) ||
+        (g->dk && (rc = check_rows(f, g->dk, g->dk_token_ld, g->dk_head_ld, f->kv_heads, f->k_tokens, "dk"))) ||
+        (g->dv && (rc = check_rows(f, g->dv, g->dv_token_ld, g->dv_head_ld, f->kv_heads, f->k_tokens, "dv"))))
+        return rc;
+    if ((!g->dq || f->q_tokens == 0) && ((!g->dk && !g->dv) || f->k_tokens == 0))
+        return FUSE_OK;
+    const AttnArgs a = grad_args(f, g);
+    const unsigned gaps = std::min(a.seqs + 1, 512);
+    attention_rest_kernel<<<dim3(gaps, 512 / gaps, 2), 256, 0, (hipStream_t)stream>>>(a);
+    return launched("attention_rest_kernel");
+}
+
 int backward_impl(const fuse_attn *f, const fuse_attn_grads *g, void *workspace, size_t workspace_bytes, void *stream)
 {
     report(FUSE_OK, "");
@@ -505,12 +570,9 @@ int backward_impl(const fuse_attn *f, const fuse_attn_grads *g, void *workspace,
         return report(FUSE_EINVAL, "lse is NULL or not aligned to its type");
     if (f->q_tokens > 0 && (!workspace || !on_16_bytes(workspace) || workspace_bytes < backward_bytes(f)))
         return report(FUSE_EINVAL, "workspace: " + std::to_string(backward_bytes(f)) + " bytes on 16 are needed");
-    AttnArgs a = attn_args(f);
+    AttnArgs a = grad_args(f, g);
     a.dout = {const_cast<void *>(g->dout), g->dout_token_ld, g->dout_head_ld};
     a.out = {const_cast<void *>(g->out), g->out_token_ld, g->out_head_ld};
-    a.dq = {g->dq, g->dq_token_ld, g->dq_head_ld};
-    a.dk = {g->dk, g->dk_token_ld, g->dk_head_ld};
-    a.dv = {g->dv, g->dv_token_ld, g->dv_head_ld};
     a.lse = const_cast<float *>(g->lse);
     a.delta = static_cast<float *>(workspace);
     a.lse2 = a.delta + stat_floats(f);
@@ -527,6 +589,11 @@ extern "C" {
 size_t fuse_attention_backward_bytes(const fuse_attn *attn)
 {
     return fuse::check_attn(attn) || attn->q_tokens == 0 ? 0 : backward_bytes(attn);
+}
+
+int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads, void *stream)
+{
+    return fuse::guard([&] { return zero_rest_impl(attn, grads, stream); });
 }
 
 int fuse_attention_backward(const fuse_attn *attn, const fuse_attn_grads *grads, void *workspace, size_t workspace_bytes, void *stream)

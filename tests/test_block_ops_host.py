@@ -233,3 +233,14 @@ def test_python_refusals():
         F.fuse_grad_clip([x], 1.0, out=[])
     with pytest.raises(TypeError, match="result 0"):
         F.fuse_grad_clip([x], 1.0, out=[x.float()])
+
+
+def test_attention_zero_rest_refuses():
+    lib = L.load()
+    call = lambda f, g: lib.fuse_attention_zero_rest(ctypes.byref(f), ctypes.byref(g) if g else None, None)  # noqa: E731
+    refused(call(attn(), None), EINVAL, "grads")
+    refused(call(attn(dim=60), attn_grads()), EUNSUPPORTED, "dim")
+    refused(call(attn(), attn_grads(dv_token_ld=4)), EUNSUPPORTED, "dv")
+    refused(call(attn(), attn_grads(dq_head_ld=56)), ESHAPE, "dq")
+    refused(call(attn(), attn_grads(dk=FAR + 4)), EUNSUPPORTED, "dk")
+    assert call(attn(), L.AttnGrads()) == 0                                # no result is asked for: nothing is launched

@@ -182,3 +182,88 @@ def test_attention_results_do_not_depend_on_earlier_calls():
             found.append([t.view(torch.int32 if t.dtype == torch.float32 else torch.int16) for t in got])
         for again in found[1:]:
             assert all(torch.equal(a, b) for a, b in zip(found[0], again)), (dtype, dim)
+
+
+def covered(c):
+    """Which queries, and which keys, belong to a sequence."""
+    q, k = (torch.zeros(c[n].shape[0], dtype=torch.bool) for n in "qk")
+    for qs, ks in R.sequences(c["offsets"], c["key_offsets"], c["key_lengths"]):
+        q[qs], k[ks] = True, True
+    return q.cuda(), k.cuda()
+
+
+def stale(c):
+    """Memory that the next allocations of these sizes will get, full of NaN."""
+    kept = [torch.full_like(t, math.nan, memory_format=torch.contiguous_format) for t in (c["q"], c["k"], c["v"]) for _ in range(3)]
+    torch.cuda.synchronize()
+    del kept
+
+
+REST_CASES = {
+    # type, heads, kv_heads, dim, lengths, key lengths, room, spare rows; the first sequence's start
+    "padded": ("bf16", 6, 2, 64, [37, 1, 130], None, None, 25, 0),
+    "begins_late": ("fp16", 2, 1, 128, [70], None, None, 90, 17),
+    "cache": ("bf16", 4, 4, 72, [1, 3, 0], [5, 96, 40], 96, 9, 0),
+    "other_keys": ("fp16", 8, 1, 96, [9, 14], [100, 3], None, 3, 2),
+    "many": ("bf16", 2, 2, 64, [1, 0, 3] * 700, [2, 1, 5] * 700, 8, 1, 0),
+    "all_taken": ("bf16", 4, 2, 128, [64, 200], None, None, 0, 0),
+    "long_gap": ("bf16", 3, 1, 24, [5], [7], 60000, 0, 0),
+}
+
+
+@pytest.mark.parametrize("name", sorted(REST_CASES))
+def test_attention_gradients_of_no_sequence_are_zero(name):
+    dtype, heads, kv_heads, dim, lens, keys, room, spare, late = REST_CASES[name]
+    c = attn_case(88, dtype, heads, kv_heads, dim, lens, keys, room, spare=spare)
+    if late:
+        c["offsets"] += late
+        if c["key_offsets"] is not None:
+            c["key_offsets"] += late
+    o, (in_q, in_k) = offs(c), covered(c)
+    out, lse = torch.zeros_like(c["q"]), torch.zeros(c["q"].shape[:2], device="cuda")
+    F.fuse_attention(c["q"], c["k"], c["v"], **o, out=out, lse=lse)
+    args = (c["dout"], c["q"], c["k"], c["v"], out, lse)
+    kept = [torch.full_like(t, 7.0, memory_format=torch.contiguous_format) for t in (c["q"], c["k"], c["v"])]
+    F.fuse_attention_backward(*args, **o, dq=kept[0], dk=kept[1], dv=kept[2])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        stale(c)
+        got = F.fuse_attention_backward(*args, **o, stream=stream)
+        torch.cuda.synchronize()
+        for x, want, rows in zip(got, kept, (in_q, in_k, in_k)):
+            assert torch.equal(x[rows], want[rows]) and not x[~rows].any()
+            assert (want[~rows] == 7.0).all()
+    stale(c)
+    mine = torch.full_like(kept[1], 7.0)                           # some results given, some made by the call
+    dq, dk, dv = F.fuse_attention_backward(*args, **o, dk=mine)
+    assert dk is mine and (dk[~in_k] == 7.0).all() and not dq[~in_q].any() and not dv[~in_k].any()
+    assert torch.equal(dk[in_k], kept[1][in_k]) and torch.equal(dq[in_q], kept[0][in_q])
+
+
+def test_attention_gradients_without_a_sequence():
+    q = torch.ones(5, 2, 64, dtype=torch.bfloat16, device="cuda")
+    off = torch.zeros(1, dtype=torch.int32, device="cuda")
+    stale(dict(q=q, k=q, v=q))
+    got = F.fuse_attention_backward(q, q, q, q, q, torch.zeros(5, 2, device="cuda"), off)
+    assert not any(t.any() for t in got)
+
+
+def test_attention_gradients_of_padded_batches_in_a_graph():
+    """Offsets change between the replays of a captured call: what belongs to no sequence now is 0, whatever the replay before left there."""
+    c = attn_case(89, "bf16", 4, 2, 64, [150, 50])
+    off = c["offsets"].cuda()
+    call = lambda: F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], *made, off)  # noqa: E731
+    made = F.fuse_attention(c["q"], c["k"], c["v"], off)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for ends in ([0, 150, 200], [0, 20, 21], [30, 150, 190], [0, 150, 200]):
+        off.copy_(torch.tensor(ends, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert not any(t[ends[-1]:].any() or t[:ends[0]].any() for t in got)
