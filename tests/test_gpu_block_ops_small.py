@@ -267,3 +267,58 @@ def test_attention_gradients_of_padded_batches_in_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         assert not any(t[ends[-1]:].any() or t[:ends[0]].any() for t in got)
+
+
+@pytest.mark.parametrize("dtype", ["fp64", "fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("inplace", [True, False])
+def test_grad_clip_writes_its_tensors_only(dtype, inplace):
+    """Cells between views that are clipped, on every alignment and of every length around what the kernels move at once."""
+    t = DT[dtype]
+    base = rnd(gen(91), (60000,), t).cuda()
+    spans, at = [], 1
+    for n in (1, 2, 3, 5, 7, 8, 9, 15, 16, 17, 31, 33, 100, 255, 257, 1023, 1025, 8191, 8193, 16385):
+        for skip in (1, 2, 3):                                     # cells left free in front of a view
+            if at + skip + n < 59000:
+                spans.append((at + skip, n))
+                at += skip + n
+    free = torch.ones(60000, dtype=torch.bool)
+    for first, n in spans:
+        free[first:first + n] = False
+    grads = [base[i:i + n] for i, n in spans]
+    kept = base.clone()
+    where = base if inplace else torch.full_like(base, 3.0)
+    out = None if inplace else [where[i + 1:i + 1 + n] for i, n in spans]
+    norm = F.fuse_grad_clip(grads, 1.0, out=out)
+    total = math.sqrt(sum(float(kept[i:i + n].double().square().sum()) for i, n in spans))
+    assert abs(float(norm) - total) <= 1e-12 * total
+    if inplace:
+        assert torch.equal(base[free.cuda()], kept[free.cuda()])
+    else:
+        moved = torch.cat([torch.ones(1, dtype=torch.bool), free[:-1]]).cuda()
+        assert torch.equal(base, kept) and (where[moved] == 3.0).all()
+    # the factor is rounded to the arithmetic's type, then the product, then the result
+    steps = R.half_step(t) + 4 * (2.0 ** -53 if t == torch.float64 else R.F32) + 1e-12
+    for i, (first, n) in enumerate(spans):
+        want = kept[first:first + n].double().cpu() / (total + 1e-6)
+        R.within(grads[i] if inplace else out[i], want, want.abs() * steps + (2.0 ** -25 if t == torch.float16 else 0.0), "clipped")
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("fp16", 72), ("fp16", 96), ("bf16", 40)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_attention_gradients_beside_a_bad_key(dtype, dim, bad):
+    """With the clean call's out and lse, a key that is not finite reaches its own gradients and those of the queries that see it: the others
+    are the clean inputs' within their bounds."""
+    c = attn_case(92, dtype, 4, 2, dim, [170])
+    out, lse = F.fuse_attention(c["q"], c["k"], c["v"], **offs(c))
+    (dq, fq), (dk, fk), (dv, fv) = gradients(c, out, lse, True, dim ** -0.5)
+    for names in ("k", "v", "kv"):
+        kept = {n: c[n][100].clone() for n in names}
+        for n in names:
+            c[n][100] = bad
+        got = F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, **offs(c))
+        R.within(got[0][:100], dq[:100], fq[:100], "dq")
+        others = torch.arange(170) != 100
+        R.within(got[1].cpu()[others], dk[others], fk[others], "dk")
+        R.within(got[2].cpu()[others], dv[others], fv[others], "dv")
+        for n in names:
+            c[n][100] = kept[n]
