@@ -36,10 +36,14 @@ __device__ __forceinline__ void lower(float (&w)[16], int &lift, f32x16 (&o)[DT]
 #pragma unroll
     for (int i = 1; i < 16; ++i)
         top = fmaxf(top, fabsf(w[i]));
-    top = both_max(top);
-    const bool over = top > 32768.0f && top < INFINITY;
-    if (!__any(over))
+    if (!__any(both_max(top) > 32768.0f))
         return;
+    top = 0.0f;                            // the largest of those that are numbers
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        top = fabsf(w[i]) < INFINITY ? fmaxf(top, fabsf(w[i])) : top;
+    top = both_max(top);
+    const bool over = top > 32768.0f;
     const int down = over ? __builtin_amdgcn_frexp_expf(top) - 12 : 0;     // (to between 2^11 and 2^12)
     const float f = ldexpf(1.0f, -down);
     lift -= down;

@@ -322,3 +322,21 @@ def test_attention_gradients_beside_a_bad_key(dtype, dim, bad):
         R.within(got[2].cpu()[others], dv[others], fv[others], "dv")
         for n in names:
             c[n][100] = kept[n]
+
+
+@pytest.mark.parametrize("dtype,dim", [("fp16", 64), ("fp16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("lens", [[20], [33, 64], [300]])
+def test_attention_gradients_of_keys_beside_an_infinite_one(dtype, dim, lens):
+    """All queries see a key whose value is infinite, so none of the sizes of their dS is a number to scale by."""
+    c = attn_case(93, dtype, 4, 2, dim, lens)
+    c["dout"].mul_(8.0)
+    out, lse = F.fuse_attention(c["q"], c["k"], c["v"], **offs(c))
+    _, (dk, fk), (dv, fv) = gradients(c, out, lse, True, dim ** -0.5)
+    bad = c["offsets"][:-1].long() + 1
+    for value in (math.inf, -math.inf, math.nan):
+        c["v"][bad.cuda(), :, 3] = value                           # (in one dim: dS is infinite and not NaN)
+        _, got_k, got_v = F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, **offs(c))
+        others = torch.ones(dk.shape[0], dtype=torch.bool)
+        others[bad] = False
+        R.within(got_k.cpu()[others], dk[others], fk[others], "dk")
+        R.within(got_v.cpu()[others], dv[others], fv[others], "dv")
