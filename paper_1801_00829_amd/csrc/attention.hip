@@ -366,8 +366,8 @@ int check_rows(const fuse_attn *f, const void *p, int64_t token_ld, int64_t head
         return report(FUSE_EUNSUPPORTED, std::string(what) + ": rows are not on 16 bytes");
     if ((tokens > 1 && token_ld < f->dim) || (heads > 1 && head_ld < f->dim))
         return report(FUSE_ESHAPE, std::string(what) + ": stride < dim");
-    if (token_ld > (1 << 25) || head_ld > (1 << 25))        // (a tile's rows are 32 bit offsets in bytes from its first)
-        return report(FUSE_EUNSUPPORTED, std::string(what) + ": stride too large");
+    if (token_ld > (INT64_C(1) << 40) || head_ld > (INT64_C(1) << 40))
+        return report(FUSE_EUNSUPPORTED, std::string(what) + ": stride > 2^40");
     return FUSE_OK;
 }
 

@@ -213,8 +213,8 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
 // instead of 128: with those, next to 64 of keys and values, nothing is left to load operands ahead of the products.
 //
 // EVEN: the rows of one pass of a tile's loads are whole tokens (the group divides their number), so they lie the same distance from
-// the next pass's and their addresses are scalars: 481 against 521 us for a group of four.  Else every row's place is divided out (the
-// two in one kernel: 78 against 68 us for a group of three).
+// the next pass's and their addresses are scalars with 32 bit offsets per lane: 481 against 521 us for a group of four.  Else, and where
+// heads or tokens are far apart, every row's place is divided out (the two in one kernel: 78 against 68 us for a group of three).
 template <typename T, int DP, bool EVEN>
 __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnArgs a)
 {
@@ -487,7 +487,9 @@ size_t backward_bytes(const fuse_attn *f)
 template <typename T, int DP>
 int launch_keys(const AttnArgs &a, unsigned blocks, hipStream_t s)
 {
-    if (Fill<T, DP, kStep>::kPerPass % a.group == 0)
+    // (a pass's rows are 32 bit offsets in bytes from its first)
+    const bool near = std::max(std::max(a.q.token, a.q.head), std::max(a.dout.token, a.dout.head)) <= 1 << 25;
+    if (near && Fill<T, DP, kStep>::kPerPass % a.group == 0)
         attention_key_grad_kernel<T, DP, true><<<blocks, 256, 0, s>>>(a);
     else
         attention_key_grad_kernel<T, DP, false><<<blocks, 256, 0, s>>>(a);

@@ -340,3 +340,30 @@ def test_attention_gradients_of_keys_beside_an_infinite_one(dtype, dim, lens):
         others[bad] = False
         R.within(got_k.cpu()[others], dk[others], fk[others], "dk")
         R.within(got_v.cpu()[others], dv[others], fv[others], "dv")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_heads_far_apart(dtype):
+    """Heads one behind the other in a long cache, and queries and gradients laid out likewise: 38 million elements between two heads."""
+    room, n, dim, t = 300000, 150, 128, DT[dtype]
+
+    def laid(x):
+        big = torch.zeros(x.shape[1], room, dim, dtype=t, device="cuda")
+        big[:, 7:7 + n] = x.transpose(0, 1)
+        return big.transpose(0, 1)
+
+    c = attn_case(94, dtype, 4, 2, dim, [n])
+    off = torch.tensor([7, 7 + n], dtype=torch.int64, device="cuda")
+    near = F.fuse_attention(c["q"], c["k"], c["v"], **offs(c))
+    grads = F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], *near, **offs(c))
+    q, k, v, dout = (laid(c[x]) for x in ("q", "k", "v", "dout"))
+    out, lse = torch.zeros_like(q), torch.zeros(room, 4, device="cuda")
+    F.fuse_attention(q, k, v, off, out=out, lse=lse)
+    assert torch.equal(out[7:7 + n], near[0]) and torch.equal(lse[7:7 + n], near[1])
+    far = [torch.zeros_like(x) for x in (q, k, v)]
+    F.fuse_attention_backward(dout, q, k, v, out, lse, off, dq=far[0], dk=far[1], dv=far[2])
+    bounds = gradients(c, *near, True, dim ** -0.5)                # (which rows share a step differs, so sums may be in another order)
+    for x, (want, bound), name in zip(far, bounds, ("dq", "dk", "dv")):
+        R.within(x[7:7 + n], want, bound, name)
+        assert not x[:7].any() and not x[7 + n:].any()
+    assert torch.equal(far[0][7:7 + n], grads[0])
