@@ -458,7 +458,7 @@ int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads
  *                    norm_in[0] (a device value: for instance one that several processes have summed up), or with norm_in NULL
  *                    it is computed as by fuse_grad_norm and left in norm_out[0].  Exactly one of the two is given.
  * Tensors are contiguous arrays of any fuse_dtype, mixed freely, of any alignment of their type; empty ones are allowed.  Outputs
- * may overlap neither each other nor the data of another tensor (FUSE_EINVAL).  The list is read during the call only (host memory).
+ * may overlap neither each other nor the data of another tensor, nor the norm (FUSE_EINVAL); norm_out no data either.  The list is read during the call only (host memory).
  * A norm that is NaN makes every result NaN; an infinite one makes finite cells 0.
  *   fuse_grad_norm_bytes : bytes of the workspace of both (0 for a list that is refused). */
 typedef struct {

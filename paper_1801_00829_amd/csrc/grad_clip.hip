@@ -252,6 +252,21 @@ int check_overlap(const fuse_tensor *tensors, int64_t n)
     return FUSE_OK;
 }
 
+// The norm is read, or written, while tensors are: it must not lie in one that is written, nor be written into one that is read.
+int check_norm(const fuse_tensor *tensors, int64_t n, const double *norm, bool written)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(norm);
+    if (p % sizeof(double))
+        return report(FUSE_EINVAL, "the norm is not aligned to its type");
+    for (int64_t i = 0; i < n; ++i) {
+        const size_t bytes = (size_t)tensors[i].count * dtype_size(tensors[i].dtype);
+        const uintptr_t d = reinterpret_cast<uintptr_t>(tensors[i].data), o = tensors[i].out ? reinterpret_cast<uintptr_t>(tensors[i].out) : d;
+        if ((p < o + bytes && o < p + sizeof(double)) || (written && p < d + bytes && d < p + sizeof(double)))
+            return report(FUSE_EINVAL, "the norm overlaps tensor " + std::to_string(i));
+    }
+    return FUSE_OK;
+}
+
 // The next launch's tensors, from tensor `at` and its cell `from` on; false: none are left.  A launch takes at most 2^30
 // chunks, so a longer tensor is continued by the next one.
 bool next_table(const fuse_tensor *tensors, int64_t n, int64_t &at, int64_t &from, Table &t)
@@ -353,9 +368,11 @@ int grad_clip_impl(const fuse_tensor *tensors, int64_t n, double max_norm, doubl
         return report(FUSE_EINVAL, "one of norm_in and norm_out is needed");
     hipStream_t s = (hipStream_t)stream;
     int count = -1;
+    if (!norm_in && (rc = check_workspace(tensors, n, workspace, workspace_bytes)))
+        return rc;
+    if ((rc = check_norm(tensors, n, norm_in ? norm_in : norm_out, !norm_in)))
+        return rc;
     if (!norm_in) {
-        if ((rc = check_workspace(tensors, n, workspace, workspace_bytes)))
-            return rc;
         if ((rc = squares_of(tensors, n, static_cast<double *>(workspace), s, count)))
             return rc;
         if (count == 0) {                  // no cells at all: a norm of 0 and nothing to clip

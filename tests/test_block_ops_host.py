@@ -244,3 +244,19 @@ def test_attention_zero_rest_refuses():
     refused(call(attn(), attn_grads(dq_head_ld=56)), ESHAPE, "dq")
     refused(call(attn(), attn_grads(dk=FAR + 4)), EUNSUPPORTED, "dk")
     assert call(attn(), L.AttnGrads()) == 0                                # no result is asked for: nothing is launched
+
+
+def test_grad_clip_refuses_a_norm_within_its_tensors():
+    lib = L.load()
+
+    def clip(rows, norm_in=None, norm_out=None):
+        return lib.fuse_grad_clip(*tensors(*rows), 1.0, 1e-6, norm_in, norm_out, FAR + (1 << 19), 1 << 18, None)
+
+    place, away = FAR, FAR + 4096
+    for at in (FAR, FAR + 72):                                             # its first and its last cell
+        refused(clip([(place, None, 10, 0)], norm_out=at), EINVAL, "norm")                     # written while it is read
+        refused(clip([(place, None, 10, 0)], norm_in=at), EINVAL, "norm")                      # read while it is written
+        refused(clip([(away, None, 3, 1), (away + 64, place, 10, 0)], norm_in=at), EINVAL, "norm")
+        refused(clip([(place, away, 10, 0)], norm_out=at), EINVAL, "norm")
+    refused(clip([(place, None, 10, 2)], norm_out=FAR + 16), EINVAL, "norm")
+    refused(clip([(place, None, 10, 2)], norm_out=FAR + 1004), EINVAL, "aligned")
