@@ -369,7 +369,7 @@ typedef enum { FUSE_NORM_RMS = 0, FUSE_NORM_LAYER = 1 } fuse_norm_kind;
  * Matrices are rows x cols with unit column stride and a leading dimension in elements; weights and biases have cols
  * values.  The gate is addressed like a side input: FUSE_SIDE_ROWVEC (cols values), FUSE_SIDE_COLVEC (rows values,
  * gate_ld apart) or FUSE_SIDE_MATRIX.  cols <= 32768 (FUSE_EUNSUPPORTED beyond).  Rows of any alignment; 16-byte
- * aligned rows of a multiple of 8 columns are faster. */
+ * aligned rows of a multiple of 8 columns are faster.  Rows of more than 8192 columns (fp64: 4096) are several times slower per cell. */
 typedef struct {
     int32_t dtype;                          /* fuse_dtype of every array                              */
     int32_t norm;                           /* fuse_norm_kind of both norms                           */
@@ -440,7 +440,8 @@ int fuse_attention(const fuse_attn *attn, void *out, int64_t out_token_ld, int64
 
 /* The gradients of q, k and v, given dout, the gradient of out, and the forward call's out and lse.  Keys that no query sees
  * get 0.  Gradients of a shared key head are summed over its query heads.  Rows that belong to no sequence -- before the first and
- * behind the last one, and behind a sequence's k_lengths -- are left as they were; fuse_attention_zero_rest sets those of dq, dk and dv to 0 (NULL: not that one's), and nothing else. */
+ * behind the last one, and behind a sequence's k_lengths -- are left as they were; fuse_attention_zero_rest sets those of dq, dk and dv
+ * to 0 (NULL: not that one's), and nothing else. */
 typedef struct {
     const void *dout, *out;  const float *lse;
     int64_t dout_token_ld, dout_head_ld, out_token_ld, out_head_ld;
@@ -458,7 +459,8 @@ int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads
  *                    norm_in[0] (a device value: for instance one that several processes have summed up), or with norm_in NULL
  *                    it is computed as by fuse_grad_norm and left in norm_out[0].  Exactly one of the two is given.
  * Tensors are contiguous arrays of any fuse_dtype, mixed freely, of any alignment of their type; empty ones are allowed.  Outputs
- * may overlap neither each other nor the data of another tensor, nor the norm (FUSE_EINVAL); norm_out no data either.  The list is read during the call only (host memory).
+ * may overlap neither each other nor the data of another tensor, nor the norm (FUSE_EINVAL); norm_out no data either.  The list is read
+ * during the call only (host memory).
  * A norm that is NaN makes every result NaN; an infinite one makes finite cells 0.
  *   fuse_grad_norm_bytes : bytes of the workspace of both (0 for a list that is refused). */
 typedef struct {

@@ -69,7 +69,7 @@ __device__ __forceinline__ float log_of(float sum)
 //
 // Bound by how products and vector work share a compute unit: of 12288 packed tokens, 32 heads over 8 of dim 128 (438 GFLOP of what
 // is visible) the matrix units are busy for 47 % of the time and the vector units for 52 %, mostly exp (a quarter of the rate of
-// other work); 489 us, 0.9 PFLOP/s.  Without its loads the same kernel takes 20 % less; four tiles of 32 KB each way from L2 per step
+// other work); 481 us, 0.91 PFLOP/s.  Without its loads the same kernel takes 20 % less; four tiles of 32 KB each way from L2 per step
 // and compute unit do not hide entirely behind two blocks.  Tried without gain: the next step's scores among this one's exp
 // (500 to 510 us), transposed loads with waits of their own (509), a higher priority for waves in their products (528); blocks of 256
 // rows, which read half as much, take 472 us here but lose 4 to 24 % with fewer rows, fewer blocks or a dim of 64.
@@ -290,7 +290,8 @@ long long tiles_of(const fuse_attn *f) { return first_tile(f->q_tokens * (f->hea
 // Splits of the keys: as many as it takes to have two blocks for each of 256 compute units, of at least four steps each where all
 // sequences are equally long (two: of at least eight): a step takes about a microsecond alone, the launch that joins them seven.  One token
 // of 32 heads over 8, dim 128, over 32768 places: 33 us with 64 splits; two tokens over 1500 places each: 17 us with splits of four steps,
-// 23 with splits of eight; 8 heads over 1, dim 64, over 512 places: 12 us without a split, 19 with two.
+// 23 with splits of eight; 8 heads over 1, dim 64, over 512 places: 12 us without a split, 19 with two.  The lengths are the device's: a long
+// history among many short ones, or one that fills little of its room, has the splits of the mean room.
 int splits_of(const fuse_attn *f)
 {
     const long long blocks = tiles_of(f) * f->kv_heads, keys = f->k_tokens / (f->seqs > 0 ? f->seqs : 1);

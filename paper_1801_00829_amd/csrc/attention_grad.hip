@@ -59,8 +59,8 @@ __device__ __forceinline__ void lower(float (&w)[16], int &lift, f32x16 (&o)[DT]
 // as columns, keys and values step by step through LDS; the keys are read twice, as rows for S and transposed for t(K) t(dS).
 //
 // Scores are taken twice, here and for the keys: one kernel for all three gradients would have to add up those of the queries over
-// blocks of keys, by atomics in an order that changes or through memory.  8192 packed tokens, 32 heads over 8 of dim 128: 315 us here
-// (three products, 0.9 PFLOP/s) and 440 us for the keys (four products, 0.85 PFLOP/s).
+// blocks of keys, by atomics in an order that changes or through memory.  8192 packed tokens, 32 heads over 8 of dim 128: 297 us here
+// (three products, 0.94 PFLOP/s) and 420 us for the keys (four products, 0.89 PFLOP/s).
 template <typename T, int DP>
 __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const AttnArgs a)
 {
@@ -210,7 +210,8 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
 //
 // Two waves share 32 keys, as columns.  Each takes half of a step's rows for S, dP, P and dS, the two exchange P and dS through LDS, and
 // each adds all rows' products to half of the dims of dV and dK.  That is the same work as a wave for itself, but 64 registers of sums
-// instead of 128: with those, next to 64 of keys and values, nothing is left to load operands ahead of the products.
+// instead of 128: with those, next to 64 of keys and values, nothing is left to load operands ahead of the products.  For a dim of 128 all 256
+// registers are taken and 16 to 20 bytes per lane are in scratch memory.
 //
 // EVEN: the rows of one pass of a tile's loads are whole tokens (the group divides their number), so they lie the same distance from
 // the next pass's and their addresses are scalars with 32 bit offsets per lane: 481 against 521 us for a group of four.  Else, and where
@@ -423,7 +424,7 @@ __global__ void __launch_bounds__(256) attention_key_join_kernel(const AttnArgs 
 }
 
 // Zeros in the rows of no sequence, in those of dq, dk and dv that are given: block x takes the rows between two sequences (before the first
-// one, behind the last one), y some of them, z = 0 those of the queries, z = 1 those of the keys.  3 us where there are none.
+// one, behind the last one), y some of them, z = 0 those of the queries, z = 1 those of the keys.  3 to 4 us where there are none.
 __global__ void __launch_bounds__(256) attention_rest_kernel(const AttnArgs a)
 {
     constexpr int kTokens = 16;            // at a time

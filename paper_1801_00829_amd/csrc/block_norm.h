@@ -8,15 +8,20 @@
 //   dv = r (g - n mean(g n) [- mean(g)]),  dw = sum over the rows of dy o n,  db = sum over the rows of dy
 //   dx = dh + dv(h);  dgate = scale dx o u, summed over what the gate is broadcast over;  dz = dv(z) of scale dx o gate
 //
-// Bound by memory: a row is read once and stays in registers through all its statistics.  A group of G threads owns a row,
-// 16 bytes of it per thread and step, so a row of up to 4096 columns of a 16 bit type is one step.  Statistics
-// of a layer norm are taken in two passes over the registers (mean, then squares of the differences): one pass of sums of
+// Bound by memory: a row is read once and, up to 8192 columns (fp64: 4096, gradients 2048), stays in registers through all its statistics.
+// A group of G threads owns a row, 16 bytes of it per thread and step, so a row of up to 4096 columns of a 16 bit type is one step.  Longer
+// rows take the form of 32 columns per thread, whose blocks of up to 1024 threads leave 128 registers each: most of a row then goes through
+// scratch memory, 630 to 1820 bytes per lane (fp64: 2.1 to 3.9 KB; 100 to 1150 from 2048 or 4096 columns on), and this is what bounds these
+// rows.  Statistics of a layer norm are taken in two passes over the registers (mean, then squares of the differences): one pass of sums of
 // squares would lose the digits that a large mean has.
 //
-// 16384 x 4096 bf16, a norm on both sides and a gate per column: forward 99 us (5.4 TB/s), gradient 164 + 5 us (4.9 TB/s); a large copy
-// reaches 4.7 to 5.4 TB/s on the same card.  What it took: the next row loaded ahead (119 -> 101 us forward), sums by moves within the
-// registers instead of LDS (gradient 246 -> 203), branches around the columns' loops (203 -> 182), the next row asked for before the first sum
-// (182 -> 167).  Rows that are not on 16 bytes: 5003 x 1111 fp32, layer norms with a gate per cell, gradient 51 us (3.5 TB/s).
+// 16384 x 4096 bf16, a norm on both sides and a gate per column: forward 102 us (5.3 TB/s), gradient 170 + 5 us (4.6 TB/s); a large copy
+// reaches 4.7 to 5.4 TB/s on the same card.  Of as many cells (forward, gradient; TB/s): 8192 columns 4.4, 3.5; 8200 columns 0.7, 0.5;
+// 12288, 16384 and 32768 columns 1.0, 0.5 to 0.6; fp32 of 12288 columns 1.1, 1.0; fp64 of 4096, 8192 and 16384 (layer) columns 5.1, 3.6 /
+// 3.6, 2.0 / 0.6, 0.4; layer norms in bf16 of 4096 columns 4.5, 2.2, of 8192 columns 4.5, 3.0.  What it took: the next row loaded ahead
+// (119 -> 101 us forward), sums by moves within the registers instead of LDS (gradient 246 -> 203), branches around the columns' loops (203
+// -> 182), the next row asked for before the first sum (182 -> 167).  Rows that are not on 16 bytes: 5003 x 1111 fp32, layer norms with a
+// gate per cell, gradient 51 us (3.5 TB/s); 16380 x 4097 bf16, as above: forward 183 us (2.9 TB/s), gradient 359 us (2.2 TB/s).
 #pragma once
 #include <algorithm>
 #include <atomic>
@@ -371,7 +376,8 @@ __device__ __forceinline__ void leave_sum(const A (&v)[K][V], int lane, int mine
         }
 }
 
-// (Two blocks per compute unit for 16 bit types, which takes 128 registers: so does LAYER, with a few values in scratch memory.)
+// (Two blocks per compute unit for 16 bit types, which takes 128 registers: so does LAYER, with 72 bytes per lane in scratch memory in bf16
+// and 40 in fp16; 16384 x 4096 bf16: 360 us.)
 //
 // Three sums per row at most: means (layer norms only); squares of h and z and what dy needs of h; what du needs of z.  The row after
 // this one is loaded meanwhile.
