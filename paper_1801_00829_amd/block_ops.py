@@ -254,7 +254,8 @@ def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=
     one projection can be passed as they are.  offsets: the sequences' first queries and the end of the last one; key_offsets likewise
     for the keys (None: the same), with key_lengths only so many keys from each sequence's first one on (a cache with room).
     causal: the last query sees all keys, the one before it all but the last, and so on.  scale: None is 1 / sqrt(dim).  lse:
-    (tokens, heads) float32.  Rows that belong to no sequence are not written: in results made here they hold anything."""
+    (tokens, heads) float32.  Rows that belong to no sequence are not written: in results made here they hold anything (NaN
+    among it: a padded batch whose other rows go on into sums over all rows takes out=torch.zeros_like(q))."""
     f = _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale)
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != q.device):
         raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % (tuple(q.shape[:2]), q.device))
