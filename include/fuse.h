@@ -412,8 +412,8 @@ int fuse_block_norm_backward(const fuse_block *block, const void *dh, int64_t dh
  * masked keys and values hold, NaN and infinities included, has no influence.
  * Query head h reads key head h / (heads / kv_heads).  q: q_tokens x heads x dim, k and v: k_tokens x kv_heads x dim, unit
  * stride along dim; strides between tokens and between heads in elements, so parts of one projection can be passed as they
- * are.  Every row on 16 bytes (pointers on 16 bytes, strides a multiple of 8), dim a multiple of 8 up to 128, dtype FUSE_BF16
- * or FUSE_F16 (FUSE_EUNSUPPORTED otherwise).
+ * are.  Every row on 16 bytes (pointers on 16 bytes, strides a multiple of 8 and at most 2^40), dim a multiple of 8 up to 128,
+ * dtype FUSE_BF16 or FUSE_F16 (FUSE_EUNSUPPORTED otherwise).
  * Sequence s has the queries q_offsets[s] .. q_offsets[s + 1] and the keys k_offsets[s] .. k_offsets[s + 1] (k_offsets NULL: the
  * queries' offsets); with k_lengths only the first k_lengths[s] of those keys: a cache with room for more.  Offsets and lengths are
  * device arrays of int32 or int64, non-decreasing from 0; they are not read on the host.  Values beyond
