@@ -453,6 +453,50 @@ int fuse_attention_backward(const fuse_attn *attn, const fuse_attn_grads *grads,
                             void *stream);
 int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads, void *stream);
 
+/* Norms of queries and keys per head with the rotation by their positions, in one pass: for every token and head
+ *     n = x / sqrt(mean(x^2) + eps) o weight         (over the head's dim values; n = x without a weight)
+ *     pair (a, b) of n:  a' = a cos(t) - b sin(t),  b' = a sin(t) + b cos(t),  t = position * freqs[pair]
+ * The first 2 * (number of pairs) dims of a head turn, the others are passed on as they are (after the norm).
+ *   FUSE_PAIR_HALVES     : pair i is dims i and i + number of pairs
+ *   FUSE_PAIR_NEIGHBOURS : pair i is dims 2 i and 2 i + 1
+ * A token has a position on each of 1 to 4 axes (text: one; images and video: height, width, time): the first sections[0] pairs turn by its
+ * position on axis 0, the next sections[1] by that on axis 1, and so on.  positions: axes x tokens of int32 or int64, position_ld apart,
+ * of any sign; freqs: an fp64 value per pair, in radians per position.  Angles are taken in fp64.
+ * dim even, up to 256 (FUSE_EUNSUPPORTED otherwise).  Unit stride along dim; strides between tokens and heads in elements, so parts of one
+ * projection can be passed as they are.  Rows of any alignment; rows on 16 bytes and numbers of pairs (turning, and others for
+ * FUSE_PAIR_HALVES) that are a multiple of 16 bytes' worth are faster.  kv_heads may be 0: no keys.  A result may be its own input, with
+ * the same strides; other overlaps of outputs with inputs are not allowed. */
+typedef enum { FUSE_PAIR_HALVES = 0, FUSE_PAIR_NEIGHBOURS = 1 } fuse_pair_kind;
+#define FUSE_MAX_AXES 4
+typedef struct {
+    int32_t dtype, heads, kv_heads, dim;
+    int32_t pairs;                          /* fuse_pair_kind */
+    int32_t axes, positions_are_64;
+    int32_t sections[FUSE_MAX_AXES];        /* pairs of each axis */
+    int64_t tokens, position_ld;
+    const void *positions;
+    const double *freqs;
+    const void *q_weight, *k_weight;        /* dim values each, of dtype; NULL: no norm */
+    double eps;
+    const void *q, *k;
+    int64_t q_token_ld, q_head_ld, k_token_ld, k_head_ld;
+} fuse_rotary;
+int fuse_qk_rotary(const fuse_rotary *rotary, void *q_out, int64_t q_token_ld, int64_t q_head_ld, void *k_out, int64_t k_token_ld,
+                   int64_t k_head_ld, void *stream);
+
+/* Gradients of fuse_qk_rotary: dq_out and dk_out are those of its results, q and k its inputs (not read where there is no norm; then
+ * they may be NULL).  dq_weight and dk_weight go with the weights and are summed over tokens and heads.  dq may be dq_out or q itself, with the
+ * same strides, and dk likewise. */
+typedef struct {
+    const void *dq_out, *dk_out;
+    int64_t dq_out_token_ld, dq_out_head_ld, dk_out_token_ld, dk_out_head_ld;
+    void *dq, *dk;
+    int64_t dq_token_ld, dq_head_ld, dk_token_ld, dk_head_ld;
+    void *dq_weight, *dk_weight;
+} fuse_rotary_grads;
+size_t fuse_qk_rotary_backward_bytes(const fuse_rotary *rotary);
+int fuse_qk_rotary_backward(const fuse_rotary *rotary, const fuse_rotary_grads *grads, void *workspace, size_t workspace_bytes, void *stream);
+
 /* The norm of all gradients, and clipping by it.
  *   fuse_grad_norm : norm[0] = sqrt(sum over the tensors of the sum of squares of their cells), one fp64 value
  *   fuse_grad_clip : out = data * min(1, max_norm / (norm + eps)) for every tensor; out NULL: in place.  The norm is taken from

@@ -61,6 +61,22 @@ class AttnGrads(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("dq_token_ld", "dq_head_ld", "dk_token_ld", "dk_head_ld", "dv_token_ld", "dv_head_ld")]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "dim", "pairs", "axes", "positions_are_64")] + \
+               [("sections", ctypes.c_int32 * 4), ("tokens", ctypes.c_int64), ("position_ld", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("positions", "freqs", "q_weight", "k_weight")] + [("eps", ctypes.c_double)] + \
+               [(n, ctypes.c_void_p) for n in ("q", "k")] + \
+               [(n, ctypes.c_int64) for n in ("q_token_ld", "q_head_ld", "k_token_ld", "k_head_ld")]
+
+
+class RotaryGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dq_out", "dk_out")] + \
+               [(n, ctypes.c_int64) for n in ("dq_out_token_ld", "dq_out_head_ld", "dk_out_token_ld", "dk_out_head_ld")] + \
+               [(n, ctypes.c_void_p) for n in ("dq", "dk")] + \
+               [(n, ctypes.c_int64) for n in ("dq_token_ld", "dq_head_ld", "dk_token_ld", "dk_head_ld")] + \
+               [(n, ctypes.c_void_p) for n in ("dq_weight", "dk_weight")]
+
+
 class Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
@@ -122,11 +138,13 @@ def load():
                        ("fuse_attention", [P(Attn), vp, i64, i64, vp, vp, size, vp]),
                        ("fuse_attention_backward", [P(Attn), P(AttnGrads), vp, size, vp]),
                        ("fuse_attention_zero_rest", [P(Attn), P(AttnGrads), vp]),
+                       ("fuse_qk_rotary", [P(Rotary), vp, i64, i64, vp, i64, i64, vp]),
+                       ("fuse_qk_rotary_backward", [P(Rotary), P(RotaryGrads), vp, size, vp]),
                        ("fuse_grad_norm", [vp, i64, vp, vp, size, vp]),
                        ("fuse_grad_clip", [vp, i64, f64, f64, vp, vp, vp, size, vp])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, ci
     for name, args in (("fuse_block_norm_backward_bytes", [P(Block)]), ("fuse_attention_bytes", [P(Attn)]),
-                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_grad_norm_bytes", [vp, i64])):
+                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_qk_rotary_backward_bytes", [P(Rotary)]), ("fuse_grad_norm_bytes", [vp, i64])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, size
     lib.fuse_last_error.restype = ctypes.c_char_p
     lib.fuse_last_kernel.restype = ctypes.c_char_p
