@@ -497,6 +497,58 @@ typedef struct {
 size_t fuse_qk_rotary_backward_bytes(const fuse_rotary *rotary);
 int fuse_qk_rotary_backward(const fuse_rotary *rotary, const fuse_rotary_grads *grads, void *workspace, size_t workspace_bytes, void *stream);
 
+/* A cache of keys and values in 8 bits, on pages: a page has `page_size` places (any number) for every key head, each with dim values of
+ * e4m3 (4 bits of exponent, 3 of mantissa, largest value 448) and a scale in fp32; x = scale * value.
+ *   data   : k, v: pages x kv_heads x page_size rows of dim bytes, unit stride along dim; page_ld, head_ld, place_ld in bytes, the same for both
+ *   scales : k_scale, v_scale: pages x kv_heads x page_size, unit stride along the places
+ *   table  : seqs x table_width int32, table_ld apart: place p of sequence s is place p % page_size of page table[s][p / page_size]
+ * Sequence s has the new tokens offsets[s] .. offsets[s + 1] of packed arrays, and with them lengths[s] keys: its new tokens are its last
+ * keys.  offsets and lengths are device arrays of int32 or int64, not read on the host; values beyond the arrays are cut down to them.  Pages that
+ * do not exist are not written, and the nearest one that exists is read in their place: no access leaves the arrays, whatever the tables say.
+ * dim a multiple of 8 up to 128, dtype (of the packed arrays) FUSE_BF16 or FUSE_F16, their rows on 16 bytes, those of the cache on 8 (on 16 with
+ * dim a multiple of 16: faster); table_width * page_size < 2^31 - 4096 (FUSE_EUNSUPPORTED otherwise). */
+typedef struct {
+    int32_t dtype, kv_heads, dim, offsets_are_64;
+    int64_t tokens, seqs, pages, page_size;
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int64_t page_ld, head_ld, place_ld;     /* bytes */
+    int64_t scale_page_ld, scale_head_ld;   /* values */
+    const int32_t *table;
+    int64_t table_ld, table_width;
+    const void *offsets, *lengths;
+} fuse_cache;
+
+/* Writes the new tokens' keys and values (tokens x kv_heads x dim) to their places: scale = max(|x|_max, 2^-100) / 448 of every row,
+ * value = x / scale rounded to nearest, ties to even.  A row that holds an infinity or no number gets a scale that is no number, and zeros.
+ * All other places are left as they were, those of rows of no sequence and of tokens before place 0 (lengths[s] less than the new tokens) do
+ * not exist.  A place that two tokens are written to holds a mix of both. */
+int fuse_cache_write(const fuse_cache *cache, const void *k, int64_t k_token_ld, int64_t k_head_ld, const void *v, int64_t v_token_ld,
+                     int64_t v_head_ld, void *stream);
+
+/* Attention of the new tokens' queries (tokens x heads x dim) over the cache, which holds their own keys already:
+ *     S = scale * Q t(K), or cap * tanh(scale * Q t(K) / cap) where cap is not 0, then - slopes[h] * |distance| in places where there are slopes
+ *     lse_i = log(sum_j exp(S_ij)),  out = exp(S - lse) V
+ * over the keys that a query may see: all of the sequence's, or with `causal` those up to its own place, or with a tree all keys before
+ * the new tokens and of these the ones whose bits are set in the query's word: bit b of tree[token] is new token b of its sequence, up to 64 of them
+ * (those behind are seen by none).  A query that sees no key gets out = 0 and lse = -inf.  What masked keys and values hold has no influence.
+ * Query head h reads key head h / (heads / kv_heads).  S and sums are fp32; exp(S - max) times the value's scale is rounded to dtype before the
+ * product with V, for FUSE_F16 multiplied with powers of two first.  Scales must not be negative.  For a single new token per sequence up to a
+ * few dozen; rows of no sequence are neither read nor written.
+ * Results overlap neither each other nor any input.
+ *   fuse_attention_cache_bytes : bytes of the workspace (0 where none is needed, and for a call that is refused). */
+typedef struct {
+    const void *q;
+    int64_t q_token_ld, q_head_ld;
+    int32_t heads, causal;
+    double scale, cap;                      /* scale > 0; cap: 0 for none, else 1e-3 to 1e6 */
+    const float *slopes;                    /* heads values, or NULL */
+    const int64_t *tree;                    /* tokens values, or NULL; goes with causal, and without slopes */
+} fuse_cache_query;
+size_t fuse_attention_cache_bytes(const fuse_cache *cache, const fuse_cache_query *query);
+int fuse_attention_cache(const fuse_cache *cache, const fuse_cache_query *query, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
 /* The norm of all gradients, and clipping by it.
  *   fuse_grad_norm : norm[0] = sqrt(sum over the tensors of the sum of squares of their cells), one fp64 value
  *   fuse_grad_clip : out = data * min(1, max_norm / (norm + eps)) for every tensor; out NULL: in place.  The norm is taken from

@@ -1,7 +1,8 @@
 """Python binding of libfuse: fused-operator templates (Cell, MAgg, Row, Outer) on MI355X.
 
 Beside the templates: the operators of a transformer block (attention over packed sequences, the norms around a block,
-the norm of all gradients with clipping, the norms of queries and keys per head with rotary positions), in bf16, fp16 and fp32 as well.
+the norm of all gradients with clipping, the norms of queries and keys per head with rotary positions, a cache in 8 bits
+with attention over it), in bf16, fp16 and fp32 as well.
 
 Only argument marshalling happens here; every step of a call runs in the HIP
 kernels of ``libfuse.so`` (see ``include/fuse.h``).  PyTorch is used for device
@@ -14,4 +15,5 @@ from .api import (FuseError, Csr, fuse_cell, fuse_magg, fuse_magg_noalloc, fuse_
                   AGG, SIDE, OPS, lib_path)
 from .block_ops import (BlockGrads, fuse_block_norm, fuse_block_norm_backward, fuse_attention, fuse_attention_backward,  # noqa: F401
                         fuse_grad_norm, fuse_grad_clip, NORM, DTYPE)
-from .head_ops import RotaryGrads, fuse_qk_rotary, fuse_qk_rotary_backward, PAIRS  # noqa: F401
+from .head_ops import (Cache, RotaryGrads, fuse_qk_rotary, fuse_qk_rotary_backward, cache_new, fuse_cache_write,  # noqa: F401
+                       fuse_attention_cache, PAIRS)

@@ -77,6 +77,21 @@ class RotaryGrads(ctypes.Structure):
                [(n, ctypes.c_void_p) for n in ("dq_weight", "dk_weight")]
 
 
+class Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "kv_heads", "dim", "offsets_are_64")] + \
+               [(n, ctypes.c_int64) for n in ("tokens", "seqs", "pages", "page_size")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + \
+               [(n, ctypes.c_int64) for n in ("page_ld", "head_ld", "place_ld", "scale_page_ld", "scale_head_ld")] + \
+               [("table", ctypes.c_void_p), ("table_ld", ctypes.c_int64), ("table_width", ctypes.c_int64), ("offsets", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p)]
+
+
+class CacheQuery(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_token_ld", ctypes.c_int64), ("q_head_ld", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("scale", ctypes.c_double), ("cap", ctypes.c_double), ("slopes", ctypes.c_void_p),
+                ("tree", ctypes.c_void_p)]
+
+
 class Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
@@ -140,11 +155,14 @@ def load():
                        ("fuse_attention_zero_rest", [P(Attn), P(AttnGrads), vp]),
                        ("fuse_qk_rotary", [P(Rotary), vp, i64, i64, vp, i64, i64, vp]),
                        ("fuse_qk_rotary_backward", [P(Rotary), P(RotaryGrads), vp, size, vp]),
+                       ("fuse_cache_write", [P(Cache), vp, i64, i64, vp, i64, i64, vp]),
+                       ("fuse_attention_cache", [P(Cache), P(CacheQuery), vp, i64, i64, vp, vp, size, vp]),
                        ("fuse_grad_norm", [vp, i64, vp, vp, size, vp]),
                        ("fuse_grad_clip", [vp, i64, f64, f64, vp, vp, vp, size, vp])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, ci
     for name, args in (("fuse_block_norm_backward_bytes", [P(Block)]), ("fuse_attention_bytes", [P(Attn)]),
-                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_qk_rotary_backward_bytes", [P(Rotary)]), ("fuse_grad_norm_bytes", [vp, i64])):
+                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_qk_rotary_backward_bytes", [P(Rotary)]),
+                       ("fuse_attention_cache_bytes", [P(Cache), P(CacheQuery)]), ("fuse_grad_norm_bytes", [vp, i64])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, size
     lib.fuse_last_error.restype = ctypes.c_char_p
     lib.fuse_last_kernel.restype = ctypes.c_char_p

@@ -225,6 +225,24 @@ def _places(t, like, device, count, what):
     return t.data_ptr()
 
 
+def _row(t, like, dtype, count, what):
+    """Pointer of a contiguous vector of `count` values of a type, on like's device."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
+        raise TypeError("%s must be a %s tensor" % (what, dtype))
+    if t.device != like.device:
+        raise ValueError("%s is on %s, not on %s" % (what, t.device, like.device))
+    if t.dim() != 1 or t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous vector of %d values" % (what, count))
+    return t.data_ptr()
+
+
+def _cap(cap):
+    """0: none"""
+    if cap is not None and not cap > 0.0:
+        raise ValueError("cap must be positive, or None for no cap")
+    return 0.0 if cap is None else cap
+
+
 def _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale):
     dtype = _dtype(q, "q")
     qs, ks = q.shape, k.shape

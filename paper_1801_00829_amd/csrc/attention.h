@@ -86,8 +86,8 @@ struct Work {
 
 // Tile t, sequence by sequence: the sequence is the last one that starts at or before it.  A wave looks at 64 sequences at a time, first
 // far apart, then between the two that are left: two rounds of loads for 4096 sequences, three for 262144.
-template <bool KEYS>
-__device__ __forceinline__ Work tile_at(const AttnArgs &a, int tile, long long t)
+template <bool KEYS, typename Args>
+__device__ __forceinline__ Work tile_at(const Args &a, int tile, long long t)
 {
     const int lane = threadIdx.x & 63;
     Work w = {};

@@ -11,7 +11,6 @@ constexpr int kRows = 128;                 // rows per tile: 32 per wave
 constexpr int kKeys = 64;                  // keys per step
 constexpr int kMaxSplits = 64;
 constexpr int kJoinBlocks = 8;             // blocks that join a tile's rows: a row for each wave of 32 rows' worth
-constexpr float kLog2e = 1.44269504088896340736f;
 
 // Where a call's keys are split: unnormalised results and statistics of every row and split.
 struct Parts {
@@ -22,46 +21,6 @@ struct Parts {
 __device__ __forceinline__ long long part_at(const AttnArgs &a, const Parts &p, long long token, int head, int split)
 {
     return (token * a.heads + head) * p.splits + split;
-}
-
-// What a column's weights are multiplied with before they are rounded, as a power of two (LIFT), and how many powers of two the maximum
-// that they are taken against may lag behind (SLACK).  Every weight is at most 2^(LIFT + SLACK), and the sum, which carries the same factor, is
-// at least 2^LIFT.
-//
-// bf16 has fp32's range: nothing to lift.  fp16 ends at 2^16 and is coarser below 2^-14, so weights take its whole range: those down to
-// 2^-25 of the largest one are rounded by half a step of their own value, and smaller ones by 2^-36 of the sum at most.  Unlifted,
-// a weight of 2^-25 would be 0, and many of them next to one key that takes almost all of the weight (with a value near 0) are what the
-// result is made of.  The slack decides how often results are rescaled: 12288 packed tokens, 32 heads over 8, dim 128, fp16 take 492 us with
-// lift 11 and slack 4 as with 7 and 8, 499 us with 13 and 2, 515 us with 15 and 0.
-template <typename T> constexpr int kLift = 0;
-template <typename T> constexpr int kSlack = 8;
-template <> constexpr int kLift<_Float16> = 11;
-template <> constexpr int kSlack<_Float16> = 4;
-
-// Running maximum and sum of a column, and its 32 new scores: rescales the result's DT tiles where the maximum has moved.
-//
-// The maximum that is subtracted is not always the largest score so far: it is moved only when a score's weight is more than 2^SLACK times
-// larger, so that most steps leave the results as they are.
-template <typename T, int DT>
-__device__ __forceinline__ void follow_max(float top, float c, float &m, float &mc, float &l, f32x16 (&o)[DT])
-{
-    if (!__any((top - m) * c > (float)kSlack<T>))
-        return;
-    const float next = fmaxf(m, top), to = (next == -INFINITY ? 0.0f : next * c) - (float)kLift<T>;
-    const float f = m == -INFINITY ? 0.0f : exp2f(mc - to);
-    m = next;
-    mc = to;
-    l *= f;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-        o[d] *= f;
-}
-
-// log of a sum of lifted weights
-template <typename T>
-__device__ __forceinline__ float log_of(float sum)
-{
-    return logf(sum * (1.0f / (1 << kLift<T>)));
 }
 
 // One block: 128 rows, 32 per wave as columns (attention_tiles.h), the keys and values that they see in steps of 64 through LDS, loaded

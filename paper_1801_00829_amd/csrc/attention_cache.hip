@@ -1,0 +1,705 @@
+// A cache of keys and values in 8 bits on pages (fuse_cache_write), and attention over it (fuse_attention_cache).
+//
+// Every place of the cache and key head has a row of `dim` values of e4m3 and a scale in fp32:  x = scale * value,
+//   scale = max(|x|_max, 2^-100) / 448,  value = x / scale, rounded to nearest, ties to even.
+#include <algorithm>
+
+#include "attention_tiles.h"
+
+namespace {
+
+using namespace fuse;
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kMostE4m3 = 448.0f;
+constexpr float kLeastMax = 0x1p-100f;     // so that neither a scale nor its inverse leaves fp32's normal range
+
+// r / d for r < 2^31, exact (see place_of).
+struct Divider {
+    unsigned d, mul, shift;
+};
+__device__ __forceinline__ int quotient(const Divider &v, int r) { return v.d == 1 ? r : (int)(__umulhi((unsigned)r, v.mul) >> v.shift); }
+Divider divider(unsigned d)
+{
+    int n = 0;
+    while (((uint64_t)1 << n) < d)
+        ++n;
+    return {d, (unsigned)(((uint64_t)1 << (31 + n)) / d + 1), n > 0 ? (unsigned)n - 1 : 0};
+}
+
+struct Pages {
+    unsigned char *k, *v;
+    float *k_scale, *v_scale;
+    long long page_ld, head_ld, place_ld;  // bytes
+    long long scale_page_ld, scale_head_ld;
+    const int *table;
+    long long table_ld;
+    int count, width;                      // pages; entries of a sequence's table
+    Divider size;                          // places per page
+};
+
+struct CacheArgs {
+    Mat q, out;
+    Mat k, v;                              // writing: rows that go into the cache
+    float *lse;
+    Pages pages;
+    float *parts;                          // (row, split): dim values; then maxima, then sums
+    const void *q_off, *lengths;
+    const long long *tree;
+    const float *slopes;
+    long long q_tokens;
+    int seqs, heads, kv_heads, group, dim, causal, off64, splits;
+    float scale, cap;
+    Divider by_group;
+};
+
+// Sequence s: its new tokens, and its keys, the last of which are those of the new tokens.
+__device__ __forceinline__ Seq seq_at(const CacheArgs &a, int s)
+{
+    Seq x;
+    const long long q0 = offset_at(a.q_off, s, a.off64), q1 = offset_at(a.q_off, s + 1, a.off64);
+    const long long room = (long long)a.pages.width * a.pages.size.d;      // (below 2^31 - 4096, which the host checks)
+    x.q0 = min(max(q0, 0LL), a.q_tokens);
+    x.nq = (int)(min(max(q1, x.q0), a.q_tokens) - x.q0);
+    x.k0 = 0;
+    x.nk = (int)min(max(offset_at(a.lengths, s, a.off64), 0LL), room);
+    return x;
+}
+
+// ----------------------------------------------------------------------------------- writing ---
+
+constexpr int kWriteTokens = 8;            // per block
+
+// Larger of two, and no number if either is none.
+__device__ __forceinline__ float max_or_nan(float a, float b) { return a >= b || a != a ? a : b; }
+
+// Keys and values of new tokens into the cache: sixteen lanes per row, 16 bytes of it each.  Bound by memory: a row is read and written
+// once.  value = (448 x) / max: 448 x is exact in fp32 (both are taken 2^-10 times, within its range), and the quotient is corrected to the
+// last bit, so that ties are ties.
+template <typename T>
+__global__ void __launch_bounds__(256) cache_write_kernel(const CacheArgs a)
+{
+    const Work w = tile_at<false>(a, kWriteTokens, blockIdx.x);
+    if (!w.any)
+        return;
+    const Pages &g = a.pages;
+    const int tokens = min(kWriteTokens, w.x.nq - w.first), chunk = threadIdx.x & 15;
+    const int per = 2 * a.kv_heads;
+    for (int r = threadIdx.x >> 4; r < tokens * per; r += 16) {
+        const int t = r / per, head = (r - t * per) >> 1, value = r & 1;
+        const int place = w.first + t + w.x.nk - w.x.nq;
+        if (place < 0)
+            continue;
+        const int n = quotient(g.size, place), page = g.table[w.seq * g.table_ld + n], within = place - n * (int)g.size.d;
+        if (page < 0 || page >= g.count)
+            continue;
+        const Mat &m = value ? a.v : a.k;
+        typedef T t8 __attribute__((ext_vector_type(8)));
+        float x[8] = {};
+        const bool in = chunk * 8 < a.dim;
+        if (in) {
+            const t8 u = *reinterpret_cast<const t8 *>(row_of<const T>(m, w.x.q0 + w.first + t, head) + chunk * 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x[i] = (float)u[i];
+        }
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            top = max_or_nan(top, fabsf(x[i]));
+        top = max_or_nan(top, moved<0xB1>(top));
+        top = max_or_nan(top, moved<0x4E>(top));
+        top = max_or_nan(top, moved<0x141>(top));
+        top = max_or_nan(top, moved<0x140>(top));
+        const bool fine = top < INFINITY;  // else the scale is no number, and so is all that is made of the row
+        top = fine ? fmaxf(top, kLeastMax) : 1.0f;
+        const float part = top * 0x1p-10f, inv = 1.0f / part;
+        int bits[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            float q[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float y = fine ? x[i + e] * (kMostE4m3 * 0x1p-10f) : 0.0f, about = y * inv;
+                q[e] = fmaf(fmaf(-about, part, y), inv, about);
+            }
+            if (i % 4 == 0)
+                bits[i / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], bits[i / 4], false);
+            else
+                bits[i / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], bits[i / 4], true);
+        }
+        if (in)
+            *reinterpret_cast<uint2 *>((value ? g.v : g.k) + page * g.page_ld + head * g.head_ld + within * g.place_ld + chunk * 8) =
+                make_uint2(bits[0], bits[1]);
+        if (chunk == 0)
+            (value ? g.v_scale : g.k_scale)[page * g.scale_page_ld + head * g.scale_head_ld + within] = fine ? top / kMostE4m3 : NAN;
+    }
+}
+
+// ----------------------------------------------------------------------------------- reading ---
+
+constexpr int kRows = 32;                  // per block, as the columns of all products
+constexpr int kKeys = 32;                  // per step and wave
+constexpr int kWaves = 4;
+constexpr int kMaxSplits = 64;
+
+template <typename T> __device__ __forceinline__ s16x8 widened(uint2 v);
+template <> __device__ __forceinline__ s16x8 widened<__bf16>(uint2 v)
+{
+    typedef __bf16 t2 __attribute__((ext_vector_type(2)));
+    const t2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v.x, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v.x, 1.0f, true);
+    const t2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v.y, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v.y, 1.0f, true);
+    return __builtin_bit_cast(s16x8, bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]});
+}
+template <> __device__ __forceinline__ s16x8 widened<_Float16>(uint2 v)
+{
+    typedef _Float16 t2 __attribute__((ext_vector_type(2)));
+    const t2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v.x, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v.x, 1.0f, true);
+    const t2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v.y, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v.y, 1.0f, true);
+    return __builtin_bit_cast(s16x8, f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]});
+}
+
+// A wave's tiles of 32 keys and values in LDS, as they lie in the cache, rows 16 bytes apart more than they are long: 4 r words modulo
+// 64 banks are all different for sixteen rows, for both kinds of reads.  CHUNK: bytes of a load, 16 where all rows lie on 16.
+template <int DP, int CHUNK>
+struct Tiles8 {
+    static constexpr int kPitch = DP + 16;
+    static constexpr int kLanes = (DP == 64 ? 64 : 128) / CHUNK;           // per row of a load
+    static constexpr int kPerPass = 64 / kLanes, kPasses = kKeys / kPerPass;
+    static constexpr int kBytes = 2 * kKeys * kPitch + 3 * kKeys * 4;      // K, V; K's scales, V's, and their logarithms
+    typedef unsigned Part __attribute__((ext_vector_type(CHUNK / 4)));
+};
+
+__device__ __forceinline__ long long shuffled(long long v, int from)
+{
+    const int lo = __shfl((int)v, from, 64), hi = __shfl((int)(v >> 32), from, 64);
+    return (long long)((unsigned long long)(unsigned)lo | (unsigned long long)(unsigned)hi << 32);
+}
+
+// One block: 32 rows (queries of the heads of one key head, see attention.h) as columns; its keys in steps of 32 per wave, the four waves
+// beside each other, each with its own tiles, maxima and sums, which are joined at the end.  Values stay in 8 bits up to the registers that
+// feed the matrix units.  Scales of keys multiply the scores, those of values the weights before these are rounded.
+//
+// fp16's range: the maximum that a column's weights are taken against is that of score + log2(scale of the value), so that weights times
+// scales lie where fp16 has most digits, whatever the scales are; the sum of the weights carries the same factor.
+template <typename T, int DP, int CHUNK>
+__global__ void __launch_bounds__(256, 2) attention_cache_kernel(const CacheArgs a)
+{
+    using Q = Tile<DP>;
+    using L = Tiles8<DP, CHUNK>;
+    constexpr bool kNarrow = kLift<T> > 0;                 // (fp16)
+    constexpr int kJoinPitch = 36;                         // floats, per column of 32 dims
+    static_assert(kWaves * L::kBytes >= kWaves * 32 * kJoinPitch * 4, "the joining takes the tiles' place");
+    __shared__ __attribute__((aligned(256))) char lds[kWaves * L::kBytes];
+    __shared__ float stats[kWaves][2][32];
+
+    const int kvh = blockIdx.x % a.kv_heads;
+    const unsigned rest = blockIdx.x / a.kv_heads;
+    const int split = rest % a.splits;
+    const Work work = tile_at<false>(a, kRows, rest / a.splits);
+    if (!work.any)
+        return;
+    const Seq &x = work.x;
+    const int first = work.first, rows = x.nq * a.group;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    const int r = first + col;
+    const bool in = r < rows;
+    const int place = quotient(a.by_group, in ? r : rows - 1), head = kvh * a.group + (in ? r : rows - 1) - place * a.group;
+    const int before = x.nk - x.nq;                        // keys that are there already
+    int seen = x.nk, seen_lo = x.nk, end = x.nk;
+    if (a.tree) {
+        seen_lo = max(before, 0);
+    } else if (a.causal) {
+        seen = min(max(place + x.nk - x.nq + 1, 0), x.nk);
+        seen_lo = __builtin_amdgcn_readfirstlane(seen);
+        end = __builtin_amdgcn_readlane(seen, 31);
+    }
+    const unsigned long long tree = a.tree ? (unsigned long long)a.tree[x.q0 + place] : 0;
+    const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+
+    int begin = 0;
+    if (a.splits > 1) {
+        const int per = ((end + a.splits - 1) / a.splits + kKeys * kWaves - 1) / (kKeys * kWaves) * (kKeys * kWaves);
+        begin = min(split * per, end);
+        end = min(begin + per, end);
+    }
+
+    s16x8 q[Q::kSteps];
+    operands<T, DP>(q, row_of<const T>(a.q, x.q0 + place, head), in, a.dim);
+
+    char *const tiles = lds + wave * L::kBytes;
+    char *const kt = tiles, *const vt = tiles + kKeys * L::kPitch;
+    float *const kscale = reinterpret_cast<float *>(tiles + 2 * kKeys * L::kPitch), *const vscale = kscale + kKeys, *const vlog = vscale + kKeys;
+    if (a.dim < DP) {                                      // zeros behind dim
+        for (int i = lane * 16; i < 2 * kKeys * L::kPitch; i += 1024)
+            *reinterpret_cast<uint4 *>(tiles + i) = make_uint4(0, 0, 0, 0);
+    }
+    const Pages &g = a.pages;
+    const int *table = g.table + work.seq * g.table_ld;
+    const int load_row = lane / L::kLanes, load_at = lane % L::kLanes * CHUNK;
+    const bool loads = load_at < a.dim;
+    const unsigned char *const kbase = g.k + kvh * g.head_ld + load_at, *const vbase = g.v + kvh * g.head_ld + load_at;
+    const float *const sbase = (h ? g.v_scale : g.k_scale) + kvh * g.scale_head_ld;
+
+    typename L::Part kp[L::kPasses], vp[L::kPasses];
+    float sc = 0.0f;
+    auto page_at = [&](int j) { return min(max(table[quotient(g.size, min(j + col, x.nk - 1))], 0), g.count - 1); };
+    auto load = [&](int j, int page) {
+        const int key = min(j + col, x.nk - 1), within = key - quotient(g.size, key) * (int)g.size.d;
+        const long long at = page * g.page_ld + within * g.place_ld;
+        sc = sbase[page * g.scale_page_ld + within];
+#pragma unroll
+        for (int i = 0; i < L::kPasses; ++i) {
+            const long long from = shuffled(at, i * L::kPerPass + load_row);
+            if (loads) {
+                kp[i] = *reinterpret_cast<const typename L::Part *>(kbase + from);
+                vp[i] = *reinterpret_cast<const typename L::Part *>(vbase + from);
+            }
+        }
+    };
+
+    f32x16 o[Q::kCols];
+#pragma unroll
+    for (int d = 0; d < Q::kCols; ++d)
+        o[d] = f32x16{};
+    float m = -INFINITY, mc = 0.0f, l = 0.0f;
+    const float c = a.cap > 0.0f ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e, cap = a.cap * kLog2e;
+    constexpr int kStride = kKeys * kWaves;
+    int j = begin + wave * kKeys, page = 0;
+    if (j < end) {
+        load(j, page_at(j));
+        page = page_at(j + kStride);
+    }
+    for (; j < end; j += kStride) {
+        const bool masked = j + kKeys > seen_lo;
+        // the tiles that were loaded, to LDS
+        if (h == 0) {
+            kscale[col] = sc * c;
+        } else {
+            vscale[col] = sc;
+            if (kNarrow)
+                vlog[col] = __builtin_amdgcn_logf(fmaxf(sc, 0x1p-90f));
+        }
+        if (loads)
+#pragma unroll
+            for (int i = 0; i < L::kPasses; ++i) {
+                const int row = i * L::kPerPass + load_row;
+                *reinterpret_cast<typename L::Part *>(kt + row * L::kPitch + load_at) = kp[i];
+                if (masked) {              // bytes that are no number would reach rows that do not see them: their row's scale says it instead
+                    unsigned any = 0;
+#pragma unroll
+                    for (int u = 0; u < CHUNK / 4; ++u) {
+                        const unsigned bad = ((vp[i][u] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                        vp[i][u] &= ~((bad >> 7) * 255u);
+                        any |= bad;
+                    }
+                    if (any)
+                        vscale[row] = NAN;
+                }
+                *reinterpret_cast<typename L::Part *>(vt + row * L::kPitch + load_at) = vp[i];
+            }
+        if (j + kStride < end) {
+            load(j + kStride, page);
+            page = page_at(j + 2 * kStride);
+        }
+        wave_sees();
+
+        f32x16 p = {};
+#pragma unroll
+        for (int i = 0; i < Q::kSteps; ++i)
+            p = product<T>(widened<T>(*reinterpret_cast<const uint2 *>(kt + col * L::kPitch + i * 16 + h * 8)), q[i], p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 s = *reinterpret_cast<const f32x4 *>(kscale + i * 8 + h * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                p[i * 4 + e] *= s[e];
+        }
+        if (a.cap > 0.0f)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)   // tanh(y) = 1 - 2 / (exp(2 y) + 1)
+                p[i] = fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(p[i]) + 1.0f), cap);
+        if (a.slopes) {
+            const float far = (float)(j + 4 * h - (place + x.nk - x.nq));
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                p[i] = fmaf(-slope, fabsf(far + (float)(8 * (i / 4) + i % 4)), p[i]);
+        }
+        if (masked) {
+            const int left = seen - j - 4 * h, drafted = j + 4 * h - before;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int k = 8 * (i / 4) + i % 4, bit = drafted + k;
+                bool sees = k < left;
+                if (a.tree && bit >= 0)
+                    sees = sees && bit < 64 && (tree >> (bit & 63) & 1);
+                if (!sees)
+                    p[i] = -INFINITY;
+            }
+        }
+        float s[16];                       // what the maximum is taken of
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4 v = {};
+            if (kNarrow)
+                v = *reinterpret_cast<const f32x4 *>(vlog + i * 8 + h * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                s[i * 4 + e] = kNarrow ? p[i * 4 + e] + v[e] : p[i * 4 + e];
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i)
+            top = fmaxf(top, s[i]);
+        follow_max<T, Q::kCols>(both_max(top), 1.0f, m, mc, l, o);
+        float w[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(vscale + i * 8 + h * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float weight = __builtin_amdgcn_exp2f(p[i * 4 + e] - mc);
+                l += weight;
+                w[i * 4 + e] = weight * v[e];
+                if (masked && p[i * 4 + e] == -INFINITY)
+                    w[i * 4 + e] = 0.0f;   // (its scale may be no number)
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const s16x8 b = rounded<T>(w + 8 * u);
+#pragma unroll
+            for (int d = 0; d < Q::kCols; ++d) {
+                // eight keys of one dim, in the order that the weights lie in (attention_tiles.h)
+                using P = __attribute__((address_space(3))) i32x2 *;
+                const int i = lane & 15, key = u * 16 + h * 4 + (i >> 1) % 4 + (i >> 3) * 8;
+                const auto v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((P)(vt + key * L::kPitch + d * 32 + ((lane >> 4) & 1) * 16 + (i & 1) * 8));
+                o[d] = product<T>(widened<T>(make_uint2(v[0], v[1])), b, o[d]);
+            }
+        }
+        wave_sees();
+    }
+
+    // the four waves' sums
+    l = both_sum(l);
+    if (h == 0) {
+        stats[wave][0][col] = l == 0.0f ? -INFINITY : m;   // (nothing seen: a sum of 0)
+        stats[wave][1][col] = l;
+    }
+    __syncthreads();
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+        top = fmaxf(top, stats[i][0][col]);
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+        sum += stats[i][1][col] == 0.0f ? 0.0f : stats[i][1][col] * exp2f(stats[i][0][col] - top);
+    const float mine = l == 0.0f ? 0.0f : exp2f(m - top);
+    const float f = a.splits > 1 ? mine : sum > 0.0f ? mine / sum : sum == 0.0f ? 0.0f : NAN;
+    if (in && wave == 0 && h == 0) {
+        const long long row = (x.q0 + place) * a.heads + head;
+        if (a.splits > 1) {
+            float *stat = a.parts + a.q_tokens * a.heads * a.splits * a.dim;
+            stat[row * a.splits + split] = top;
+            stat[(a.q_tokens * a.heads + row) * a.splits + split] = sum;
+        } else if (a.lse) {
+            a.lse[row] = sum == 0.0f ? -INFINITY : fmaf(top, 1.0f / kLog2e, log_of<T>(sum));
+        }
+    }
+    float *const join = reinterpret_cast<float *>(lds);
+    const int jc = threadIdx.x >> 3, jd = (threadIdx.x & 7) * 4, jr = first + jc;
+#pragma unroll
+    for (int d = 0; d < Q::kCols; ++d) {
+        if (d * 32 >= a.dim)
+            break;
+        if (d > 0)
+            __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4 *>(join + (wave * 32 + col) * kJoinPitch + i * 8 + h * 4) =
+                f32x4{o[d][i * 4] * f, o[d][i * 4 + 1] * f, o[d][i * 4 + 2] * f, o[d][i * 4 + 3] * f};
+        __syncthreads();
+        if (jr >= rows || d * 32 + jd >= a.dim)
+            continue;
+        f32x4 v = *reinterpret_cast<const f32x4 *>(join + jc * kJoinPitch + jd);
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i)
+            v += *reinterpret_cast<const f32x4 *>(join + (i * 32 + jc) * kJoinPitch + jd);
+        const int jp = quotient(a.by_group, jr), jh = kvh * a.group + jr - jp * a.group;
+        if (a.splits > 1) {
+            *reinterpret_cast<f32x4 *>(a.parts + (((x.q0 + jp) * a.heads + jh) * a.splits + split) * a.dim + d * 32 + jd) = v;
+        } else {
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<t4 *>(row_of<T>(a.out, x.q0 + jp, jh) + d * 32 + jd) = t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+        }
+    }
+}
+
+// Joins the splits of every row: a wave per row.
+template <typename T>
+__global__ void __launch_bounds__(256) attention_cache_join_kernel(const CacheArgs a)
+{
+    const int kvh = blockIdx.x % a.kv_heads;
+    const Work work = tile_at<false>(a, kRows, blockIdx.x / a.kv_heads);
+    if (!work.any)
+        return;
+    const Seq &x = work.x;
+    const int lane = threadIdx.x & 63, r = work.first + blockIdx.y * 4 + (threadIdx.x >> 6);
+    if (r >= x.nq * a.group || r >= work.first + kRows)
+        return;
+    const int place = quotient(a.by_group, r), head = kvh * a.group + r - place * a.group;
+    const long long row = (x.q0 + place) * a.heads + head;
+    const float *stat = a.parts + a.q_tokens * a.heads * a.splits * a.dim;
+    const bool mine = lane < a.splits;
+    const float m = mine ? stat[row * a.splits + lane] : -INFINITY, l = mine ? stat[(a.q_tokens * a.heads + row) * a.splits + lane] : 0.0f;
+    float top = m;
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1)
+        top = fmaxf(top, __shfl_xor(top, i, 64));
+    const float w = l == 0.0f ? 0.0f : exp2f(m - top);
+    const float sum = wave_sum(w * l);
+    float o0 = 0.0f, o1 = 0.0f;
+    const float *o = a.parts + row * a.splits * a.dim;
+    const int d0 = min(lane, a.dim - 1), d1 = min(lane + 64, a.dim - 1);
+    for (int i = 0; i < a.splits; i += 8) {                // eight splits' loads in flight
+        float v0[8], v1[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int k = min(i + u, a.splits - 1);
+            v0[u] = o[(long long)k * a.dim + d0];
+            v1[u] = o[(long long)k * a.dim + d1];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u < a.splits) {
+                const float f = __shfl(w, i + u, 64);
+                o0 = fmaf(f, v0[u], o0);
+                o1 = fmaf(f, v1[u], o1);
+            }
+    }
+    const float f = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : NAN;
+    T *out = row_of<T>(a.out, x.q0 + place, head);
+    if (lane < a.dim)
+        out[lane] = (T)(o0 * f);
+    if (lane + 64 < a.dim)
+        out[lane + 64] = (T)(o1 * f);
+    if (a.lse && lane == 0)
+        a.lse[row] = sum == 0.0f ? -INFINITY : fmaf(top, 1.0f / kLog2e, log_of<T>(sum));
+}
+
+// -------------------------------------------------------------------------------------- host ---
+
+int check_rows16(const char *what, const void *p, int64_t rows, int64_t token_ld, int64_t head_ld, int64_t heads, int64_t dim)
+{
+    if (!p)
+        return rows > 0 ? report(FUSE_EINVAL, std::string(what) + " is NULL") : FUSE_OK;
+    if (!on_16_bytes(p) || token_ld % 8 || head_ld % 8)
+        return report(FUSE_EUNSUPPORTED, std::string(what) + ": rows are not on 16 bytes");
+    if ((rows > 1 && token_ld < dim) || (heads > 1 && head_ld < dim))
+        return report(FUSE_ESHAPE, std::string(what) + ": stride < dim");
+    if (token_ld > (INT64_C(1) << 40) || head_ld > (INT64_C(1) << 40))
+        return report(FUSE_EUNSUPPORTED, std::string(what) + ": stride > 2^40");
+    return FUSE_OK;
+}
+
+int check_cache(const fuse_cache *f)
+{
+    if (!f)
+        return report(FUSE_EINVAL, "cache is NULL");
+    if (f->dtype != FUSE_BF16 && f->dtype != FUSE_F16)
+        return report(known_dtype(f->dtype) ? FUSE_EUNSUPPORTED : FUSE_EINVAL, "dtype is neither FUSE_BF16 nor FUSE_F16");
+    if (f->kv_heads < 1 || f->dim < 1 || f->tokens < 0 || f->seqs < 0 || f->pages < 0 || f->page_size < 1 || f->table_width < 0)
+        return report(FUSE_EINVAL, "kv_heads, dim and page_size must be positive, counts must not be negative");
+    if (f->dim % 8 || f->dim > kMaxDim)
+        return report(FUSE_EUNSUPPORTED, "dim is no multiple of 8 up to " + std::to_string(kMaxDim));
+    if (f->tokens >= (INT64_C(1) << 31) || f->pages >= (INT64_C(1) << 31) || f->seqs >= (1 << 24) || f->kv_heads > 4096 ||
+        f->page_size > (1 << 30) || f->table_width >= (INT64_C(1) << 31))
+        return report(FUSE_EUNSUPPORTED, "2^31 tokens, pages or pages of a sequence, 2^24 sequences, 4096 heads or 2^30 places per page, or more");
+    if (f->table_width * f->page_size >= (INT64_C(1) << 31) - 4096)
+        return report(FUSE_EUNSUPPORTED, "a sequence has room for 2^31 - 4096 places or more");
+    if (f->seqs > 0 && f->tokens > 0) {
+        if (!f->offsets || !f->lengths)
+            return report(FUSE_EINVAL, "offsets or lengths is NULL");
+        if (f->table_width > 0 && (!f->table || (f->seqs > 1 && f->table_ld < f->table_width)))
+            return report(f->table ? FUSE_ESHAPE : FUSE_EINVAL, "table is NULL or its stride < table_width");
+        if (f->pages > 0 && (!f->k || !f->v || !f->k_scale || !f->v_scale))
+            return report(FUSE_EINVAL, "a part of the cache is NULL");
+    }
+    const uintptr_t width = f->offsets_are_64 ? 8 : 4;
+    for (const void *p : {f->offsets, f->lengths})
+        if (reinterpret_cast<uintptr_t>(p) % width)
+            return report(FUSE_EINVAL, "offsets or lengths are not aligned to their type");
+    for (const void *p : {(const void *)f->table, (const void *)f->k_scale, (const void *)f->v_scale})
+        if (reinterpret_cast<uintptr_t>(p) % 4)
+            return report(FUSE_EINVAL, "table or scales are not aligned to their type");
+    for (const void *p : {f->k, f->v})
+        if (reinterpret_cast<uintptr_t>(p) % 8)
+            return report(FUSE_EUNSUPPORTED, "rows of the cache are not on 8 bytes");
+    if (f->page_ld % 8 || f->head_ld % 8 || f->place_ld % 8)
+        return report(FUSE_EUNSUPPORTED, "rows of the cache are not on 8 bytes");
+    if ((f->page_size > 1 && f->place_ld < f->dim) || (f->kv_heads > 1 && f->head_ld < f->dim) || (f->pages > 1 && f->page_ld < f->dim) ||
+        (f->kv_heads > 1 && f->scale_head_ld < 1) || (f->pages > 1 && f->scale_page_ld < 1))
+        return report(FUSE_ESHAPE, "the cache's strides are less than its rows");
+    for (int64_t ld : {f->page_ld, f->head_ld, f->place_ld, f->scale_page_ld, f->scale_head_ld, f->table_ld})
+        if (ld > (INT64_C(1) << 40))
+            return report(FUSE_EUNSUPPORTED, "stride > 2^40");
+    return FUSE_OK;
+}
+
+CacheArgs cache_args(const fuse_cache *f)
+{
+    CacheArgs a = {};
+    Pages &g = a.pages;
+    g.k = static_cast<unsigned char *>(f->k), g.v = static_cast<unsigned char *>(f->v), g.k_scale = f->k_scale, g.v_scale = f->v_scale;
+    g.page_ld = f->page_ld, g.head_ld = f->head_ld, g.place_ld = f->place_ld;
+    g.scale_page_ld = f->scale_page_ld, g.scale_head_ld = f->scale_head_ld;
+    g.table = f->table, g.table_ld = f->table_ld, g.count = (int)f->pages, g.width = f->pages > 0 ? (int)f->table_width : 0;
+    g.size = divider((unsigned)f->page_size);
+    a.q_off = f->offsets, a.lengths = f->lengths, a.off64 = f->offsets_are_64 != 0;
+    a.q_tokens = f->tokens, a.seqs = (int)f->seqs, a.kv_heads = f->kv_heads, a.dim = f->dim, a.group = 1;
+    return a;
+}
+
+int write_impl(const fuse_cache *f, const void *k, int64_t k_token_ld, int64_t k_head_ld, const void *v, int64_t v_token_ld, int64_t v_head_ld,
+               void *stream)
+{
+    report(FUSE_OK, "");
+    int rc = check_cache(f);
+    if (!rc)
+        rc = check_rows16("k", k, f->tokens, k_token_ld, k_head_ld, f->kv_heads, f->dim);
+    if (!rc)
+        rc = check_rows16("v", v, f->tokens, v_token_ld, v_head_ld, f->kv_heads, f->dim);
+    if (rc)
+        return rc;
+    if (f->tokens == 0 || f->seqs == 0)
+        return FUSE_OK;
+    CacheArgs a = cache_args(f);
+    a.k = {const_cast<void *>(k), k_token_ld, k_head_ld};
+    a.v = {const_cast<void *>(v), v_token_ld, v_head_ld};
+    const unsigned blocks = (unsigned)first_tile(f->tokens, (int)f->seqs, kWriteTokens);
+    if (f->dtype == FUSE_BF16)
+        cache_write_kernel<__bf16><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
+    else
+        cache_write_kernel<_Float16><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
+    return launched("cache_write_kernel");
+}
+
+int check_read(const fuse_cache *f, const fuse_cache_query *q)
+{
+    int rc = check_cache(f);
+    if (rc)
+        return rc;
+    if (!q)
+        return report(FUSE_EINVAL, "query is NULL");
+    if (q->heads < 1 || q->heads > 4096)
+        return report(q->heads < 1 ? FUSE_EINVAL : FUSE_EUNSUPPORTED, "heads must lie between 1 and 4096");
+    if (q->heads % f->kv_heads)
+        return report(FUSE_ESHAPE, "heads is no multiple of kv_heads");
+    if (!(q->scale >= 1e-30) || !(q->scale <= 1e30))
+        return report(FUSE_EINVAL, "scale must lie between 1e-30 and 1e30");
+    if (q->cap != 0.0 && (!(q->cap >= 1e-3) || !(q->cap <= 1e6)))
+        return report(FUSE_EINVAL, "cap must be 0 (none) or lie between 1e-3 and 1e6");
+    if (q->tree && (!q->causal || q->slopes))
+        return report(FUSE_EINVAL, "a tree goes with causal, and without slopes");
+    if (reinterpret_cast<uintptr_t>(q->slopes) % 4 || reinterpret_cast<uintptr_t>(q->tree) % 8)
+        return report(FUSE_EINVAL, "slopes or tree are not aligned to their type");
+    if (f->tokens * q->heads >= (INT64_C(1) << 36) || first_tile(f->tokens * (q->heads / f->kv_heads), (int)f->seqs, kRows) * f->kv_heads >= (1 << 24))
+        return report(FUSE_EUNSUPPORTED, "more tiles of queries than one launch has blocks");
+    return check_rows16("q", q->q, f->tokens, q->q_token_ld, q->q_head_ld, q->heads, f->dim);
+}
+
+long long tiles_of(const fuse_cache *f, const fuse_cache_query *q) { return first_tile(f->tokens * (q->heads / f->kv_heads), (int)f->seqs, kRows); }
+
+int splits_of(const fuse_cache *f, const fuse_cache_query *q)
+{
+    const long long blocks = tiles_of(f, q) * f->kv_heads, room = f->table_width * f->page_size;
+    const long long n = std::min(blocks > 0 ? 1024 / blocks : 1, room / (2 * kKeys * kWaves));
+    return (int)std::max(1LL, std::min<long long>(n, kMaxSplits));
+}
+
+size_t read_bytes(const fuse_cache *f, const fuse_cache_query *q)
+{
+    const int splits = splits_of(f, q);
+    return splits > 1 ? (size_t)f->tokens * q->heads * splits * (f->dim + 2) * sizeof(float) : 0;
+}
+
+template <typename T, int CHUNK>
+void launch_dim(const CacheArgs &a, unsigned blocks, hipStream_t s)
+{
+    if (a.dim <= 64)
+        attention_cache_kernel<T, 64, CHUNK><<<blocks, 256, 0, s>>>(a);
+    else if (a.dim <= 96)
+        attention_cache_kernel<T, 96, CHUNK><<<blocks, 256, 0, s>>>(a);
+    else
+        attention_cache_kernel<T, 128, CHUNK><<<blocks, 256, 0, s>>>(a);
+}
+
+template <typename T>
+int launch_read(const CacheArgs &a, unsigned tiles, hipStream_t s)
+{
+    const Pages &g = a.pages;
+    const bool wide = a.dim % 16 == 0 && on_16_bytes(g.k) && on_16_bytes(g.v) && g.page_ld % 16 == 0 && g.head_ld % 16 == 0 && g.place_ld % 16 == 0;
+    if (wide)
+        launch_dim<T, 16>(a, tiles * a.kv_heads * a.splits, s);
+    else
+        launch_dim<T, 8>(a, tiles * a.kv_heads * a.splits, s);
+    int rc = launched("attention_cache_kernel");
+    if (rc || a.splits == 1)
+        return rc;
+    attention_cache_join_kernel<T><<<dim3(tiles * a.kv_heads, kRows / 4), 256, 0, s>>>(a);
+    rc = launched("attention_cache_join_kernel");
+    if (!rc)
+        set_last_kernel("attention_cache_kernel");
+    return rc;
+}
+
+int read_impl(const fuse_cache *f, const fuse_cache_query *q, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse, void *workspace,
+              size_t workspace_bytes, void *stream)
+{
+    report(FUSE_OK, "");
+    int rc = check_read(f, q);
+    if (!rc)
+        rc = check_rows16("out", out, f->tokens, out_token_ld, out_head_ld, q->heads, f->dim);
+    if (rc)
+        return rc;
+    if (reinterpret_cast<uintptr_t>(lse) % 4)
+        return report(FUSE_EINVAL, "lse is not aligned to its type");
+    if (f->tokens == 0 || f->seqs == 0)
+        return FUSE_OK;
+    const size_t need = read_bytes(f, q);
+    if (need && (!workspace || !on_16_bytes(workspace) || workspace_bytes < need))
+        return report(FUSE_EINVAL, "workspace: " + std::to_string(need) + " bytes on 16 are needed");
+    CacheArgs a = cache_args(f);
+    a.q = {const_cast<void *>(q->q), q->q_token_ld, q->q_head_ld};
+    a.out = {out, out_token_ld, out_head_ld};
+    a.lse = lse, a.parts = static_cast<float *>(workspace);
+    a.heads = q->heads, a.group = q->heads / f->kv_heads, a.by_group = divider((unsigned)a.group);
+    a.causal = q->causal != 0, a.scale = (float)q->scale, a.cap = (float)q->cap, a.slopes = q->slopes;
+    a.tree = reinterpret_cast<const long long *>(q->tree), a.splits = splits_of(f, q);
+    const unsigned tiles = (unsigned)tiles_of(f, q);
+    return f->dtype == FUSE_BF16 ? launch_read<__bf16>(a, tiles, (hipStream_t)stream) : launch_read<_Float16>(a, tiles, (hipStream_t)stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int fuse_cache_write(const fuse_cache *cache, const void *k, int64_t k_token_ld, int64_t k_head_ld, const void *v, int64_t v_token_ld,
+                     int64_t v_head_ld, void *stream)
+{
+    return fuse::guard([&] { return write_impl(cache, k, k_token_ld, k_head_ld, v, v_token_ld, v_head_ld, stream); });
+}
+
+size_t fuse_attention_cache_bytes(const fuse_cache *cache, const fuse_cache_query *query)
+{
+    return check_read(cache, query) ? 0 : read_bytes(cache, query);
+}
+
+int fuse_attention_cache(const fuse_cache *cache, const fuse_cache_query *query, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse,
+                         void *workspace, size_t workspace_bytes, void *stream)
+{
+    return fuse::guard([&] { return read_impl(cache, query, out, out_token_ld, out_head_ld, lse, workspace, workspace_bytes, stream); });
+}
+
+}  // extern "C"

@@ -12,7 +12,6 @@ constexpr int kRows = 128;                 // rows per block: 32 per wave
 constexpr int kStep = 64;                  // keys, or rows, per step
 constexpr int kKeys = 64;                  // keys per block of their kernel
 constexpr int kJoinBlocks = 4;             // blocks that join a tile's splits
-constexpr float kLog2e = 1.44269504088896340736f;
 
 // fp16: P and dS = P o (dP - delta) are multiplied with powers of two before they are rounded, and their products with the inverse.  P is some
 // 1 / keys and gradients are small, so dS as it is falls among the numbers below 2^-14, of which fp16 keeps few digits (below 2^-25 none);

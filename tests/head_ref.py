@@ -88,3 +88,110 @@ def rotary_grad(dy, x, weight, angle, pairs, eps, dtype):
     fw = ((far + chain * f * g.abs()) * x.abs() * r).sum((0, 1))
     return (dx, 1.01 * half_step(dtype) * dx.abs() + (2 * dim + 48) * f * size + 1.01 * more + tiny(dtype)), \
         (dw, 1.01 * half_step(dtype) * dw.abs() + 1.01 * fw + tiny(dtype))
+
+
+# ------------------------------------------------------------------------ cache in 8 bits ---
+
+def e4m3(x):
+    """The nearest value of e4m3 to one of at most 448, ties to even, in 64 bits."""
+    step = torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=2.0 ** -6))) - 3)
+    return torch.round(x / step) * step
+
+
+def quantised(x):
+    """(values, scales) in 64 bits of rows (..., dim) in 64 bits.  A scale is rounded to fp32; a value is that of x over the scale before that."""
+    top = x.abs().amax(-1)
+    fine = torch.isfinite(top)
+    top = torch.where(fine, top, torch.ones(())).clamp(min=2.0 ** -100)
+    values = torch.where(fine[..., None], e4m3(torch.where(fine[..., None], x, torch.zeros((), dtype=x.dtype)) * 448.0 / top[..., None]), 0.0)
+    return values, torch.where(fine, (top.float() / 448.0).double(), torch.nan)
+
+
+def cache_rows(c, s, hk, count):
+    """(values of keys, of values, scales of keys, of values) of the first `count` places of sequence s, in 64 bits."""
+    place = torch.arange(count)
+    page = c["table"].cpu()[s].long()[place // c["page"]].clamp(0, c["cache"].k.shape[0] - 1)
+    at = place % c["page"]
+    k, v = (t.cpu().double()[page, hk, at] for t in c["cache"][:2])
+    ks, vs = (t.cpu().double()[page, hk, at] for t in c["cache"][2:])
+    return k, v, ks, vs
+
+
+def shaped_scores(qh, kh, scale, cap, slope, place, meet):
+    """(scores, -inf where masked; tanh or None; how far off each may be) of queries at `place` of the keys' places."""
+    d = qh.shape[1]
+    x = scale * (qh @ kh.T)
+    size = scale * (qh.abs() @ kh.abs().T)
+    off = torch.zeros_like(x) + ((d + 16) * 2 * F32 * max(1.0, float(size[torch.isfinite(size)].max()) if size.numel() else 1.0))
+    t = None
+    if cap:
+        t = torch.tanh(x / cap)
+        x = cap * t
+        off = off + 6 * F32 * cap
+    if slope:
+        bias = slope * (place[:, None] - torch.arange(kh.shape[0])[None]).abs()
+        x = x - bias
+        off = off + 4 * F32 * bias
+    off = off + 2 * F32 * torch.nan_to_num(x, nan=0.0, posinf=0.0, neginf=0.0).abs()
+    return x.masked_fill(~meet, -torch.inf), t, off
+
+
+def attend(x, off, v, size, dtype, lost=None):
+    """(out, lse, bound, bound of lse) of scores x (rows, keys) over values v; size: |v|.  lost: per row and key, what the rounding of a
+    weight leaves beside half a step of its own value."""
+    step = half_step(dtype)
+    if not x.shape[1]:
+        z = torch.zeros((x.shape[0], v.shape[1]), dtype=torch.float64)
+        return z, torch.full((x.shape[0],), -torch.inf, dtype=torch.float64), z, z[:, 0] if v.shape[1] else None
+    lse = torch.logsumexp(x, 1)
+    p = torch.where(x == -torch.inf, 0.0, torch.exp(x - lse[:, None]))
+    out = _product(p, v)
+    e = step + off + (x.shape[1] // 16 + 24) * F32
+    far = _product(p * e, size) + _product(p * off, torch.ones_like(size)) * out.abs()
+    if lost is not None:
+        far = far + _product(lost(p), torch.ones_like(size))
+    far = 1.05 * far + step * out.abs() + (2.0 ** -25 if dtype == torch.float16 else torch.finfo(dtype).tiny)
+    return out, lse, far, 1.05 * (p * off).sum(1) + (x.shape[1] // 16 + 24) * F32 + 4 * F32 * torch.nan_to_num(lse, neginf=0.0).abs()
+
+
+def _product(p, v):
+    """p @ v where 0 times what is not finite is 0."""
+    if bool(torch.isfinite(v).all()):
+        return p @ v
+    return torch.where(p[:, :, None] == 0, torch.zeros((), dtype=p.dtype), p[:, :, None] * v[None]).sum(1)
+
+
+def cache_attention(c, causal=True, scale=None, cap=None, slopes=None, tree=None):
+    """(out, lse, bound, bound of lse) of attention over a cache; rows of no sequence are NaN."""
+    q = c["q"].double().cpu()
+    t = c["q"].dtype
+    n, heads, d = q.shape
+    hk = c["cache"].k.shape[1]
+    scale = d ** -0.5 if scale is None else scale
+    out, lse = torch.full(q.shape, torch.nan, dtype=torch.float64), torch.full(q.shape[:2], torch.nan, dtype=torch.float64)
+    far, far_lse = torch.zeros_like(out), torch.zeros_like(lse)
+    offsets, room = c["offsets"].tolist(), c["table"].shape[1] * c["page"]
+    for s, length in enumerate(c["lengths"].tolist()):
+        rows = slice(offsets[s], offsets[s + 1])
+        nq, nk = rows.stop - rows.start, min(max(length, 0), room)
+        place = torch.arange(nq) + nk - nq
+        j = torch.arange(nk)
+        meet = (j[None] <= place[:, None]) if causal else torch.ones(nq, nk, dtype=torch.bool)
+        if tree is not None:
+            b = j - (nk - nq)
+            bits = tree.cpu()[rows]
+            meet = (b < 0)[None] | ((b >= 0) & (b < 64))[None] & ((bits[:, None] >> b.clamp(0, 63)[None]) & 1).bool()
+        for g in range(hk):
+            k8, v8, ks, vs = cache_rows(c, s, g, nk)
+            for h in range(g * heads // hk, (g + 1) * heads // hk):
+                x, _, off = shaped_scores(q[rows, h], k8 * ks[:, None], scale, cap, 0.0 if slopes is None else float(slopes[h]), place, meet)
+
+                def lost(p):                               # fp16: 2^-36 of the row's largest weight times scale, times the value
+                    top = torch.nan_to_num(p * vs).amax(1, keepdim=True)
+                    return 2.0 ** -36 * top * (meet.double() @ torch.nan_to_num(v8.abs()).amax(1, keepdim=True)) * torch.ones_like(p) / max(1, nk)
+
+                out[rows, h], lse[rows, h], far[rows, h], f = attend(x, off, v8 * vs[:, None], (v8 * vs[:, None]).abs(), t,
+                                                                     lost if t == torch.float16 else None)
+                if f is not None:
+                    far_lse[rows, h] = f
+    return out, lse, far, far_lse

@@ -86,3 +86,117 @@ def test_qk_rotary_backward(i, dtype):
     c = rotary_case(i, dtype, *ROTARY_CASES[i])
     got = F.fuse_qk_rotary_backward(c["dq_out"], c["dk_out"], c["q"], c["k"], c["positions"], c["freqs"], **rotary_args(c))
     check_rotary_grad(c, got)
+
+
+# ------------------------------------------------------------------------ cache in 8 bits ---
+
+def cache_case(seed, dtype, heads, kv_heads, dim, page, new, lengths, index=torch.int32, spare=2, pitch=0):
+    """Sequences with `new` tokens each and `lengths` keys, on pages in any order; pitch: places of this many more bytes than dim."""
+    g, t = gen(seed), DT[dtype]
+    width = max([1] + [-(-n // page) for n in lengths])
+    pages = len(new) * width + spare
+    shape = (pages, kv_heads, page, dim + pitch)
+    data = [(rnd(g, shape, torch.float32, 150.0).clamp_(-448, 448).to(torch.float8_e4m3fn).cuda())[..., :dim] for _ in range(2)]
+    scales = [(torch.rand(shape[:3], generator=g) * 0.01 + 0.003).cuda() for _ in range(2)]
+    ends = [0]
+    for n in new:
+        ends.append(ends[-1] + n)
+    kv = rnd(g, (ends[-1], 2 * kv_heads, dim), t).cuda()
+    return dict(cache=F.Cache(*data, *scales), page=page, q=rnd(g, (ends[-1], heads, dim), t).cuda(), k=kv[:, :kv_heads], v=kv[:, kv_heads:],
+                table=torch.randperm(pages, generator=g)[:len(new) * width].view(len(new), width).to(torch.int32).cuda(),
+                offsets=torch.tensor(ends, dtype=index).cuda(), lengths=torch.tensor(lengths, dtype=index).cuda())
+
+
+def bits(t):
+    """e4m3 as its bytes; also of a view with gaps"""
+    return t.view(torch.uint8) if t.is_contiguous() else torch.stack([x.contiguous().view(torch.uint8) for x in t.unbind(0)])
+
+
+def check_write(c):
+    """Writes, and compares every place of the cache: the new ones with their definition, the others with what they were."""
+    before = [t.clone() for t in c["cache"]]
+    F.fuse_cache_write(c["k"], c["v"], c["cache"], c["offsets"], c["table"], c["lengths"])
+    want = [before[0].cpu().double(), before[1].cpu().double(), before[2].cpu(), before[3].cpu()]
+    offsets, pages = c["offsets"].tolist(), before[0].shape[0]
+    for s, length in enumerate(c["lengths"].tolist()):
+        n = offsets[s + 1] - offsets[s]
+        for i in range(n):
+            place = length - n + i
+            if place < 0 or place >= c["table"].shape[1] * c["page"]:
+                continue
+            page = int(c["table"][s, place // c["page"]])
+            if not 0 <= page < pages:
+                continue
+            for w, x in ((0, c["k"]), (1, c["v"])):
+                values, scales = H.quantised(x[offsets[s] + i].double().cpu())
+                want[w][page, :, place % c["page"]] = values
+                want[w + 2][page, :, place % c["page"]] = scales.float()
+    for got, w, name in zip(c["cache"], want, c["cache"]._fields):
+        got = got.cpu().double()
+        same = (got == w.double()) | (got.isnan() & w.double().isnan())
+        assert bool(same.all()), (name, (~same).nonzero()[0].tolist(), float(got[~same][0]), float(w[~same][0]))
+
+
+WRITE_CASES = [
+    # heads of the cache, dim, page, new, lengths
+    (1, 64, 16, [1], [1]), (8, 128, 16, [1] * 5, [1, 16, 17, 40, 33]), (2, 80, 24, [30, 0, 7], [30, 50, 24]), (4, 128, 64, [200, 13], [230, 13]),
+    (3, 8, 1, [5, 9], [6, 9]), (1, 120, 7, [33], [40]), (2, 96, 1000, [300, 300], [300, 777]), (2, 40, 16, [9, 3], [4, 0]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("i", range(len(WRITE_CASES)))
+def test_cache_write(i, dtype):
+    kv_heads, dim, page, new, lengths = WRITE_CASES[i]
+    check_write(cache_case(i, dtype, kv_heads, kv_heads, dim, page, new, lengths, [torch.int32, torch.int64][i % 2]))
+
+
+def check_cache_attention(c, **kw):
+    got = F.fuse_attention_cache(c["q"], c["cache"], c["offsets"], c["table"], c["lengths"], **kw)
+    want = H.cache_attention(c, **kw)
+    rows = ~want[1].isnan().all(1)
+    R.within(got[0].cpu()[rows], want[0][rows], want[2][rows], "out")
+    R.within(got[1].cpu()[rows], want[1][rows], want[3][rows], "lse")
+    return got
+
+
+READ_CASES = [
+    # heads, kv_heads, dim, page, new, lengths
+    (1, 1, 64, 16, [1], [1]), (8, 1, 64, 16, [1], [512]), (32, 8, 128, 16, [1] * 5, [1, 700, 33, 4001, 0]), (4, 4, 128, 64, [1, 1], [31, 2000]),
+    (6, 2, 80, 24, [1, 0, 5], [300, 20, 129]), (12, 4, 96, 7, [3, 3], [3, 500]), (8, 2, 40, 1, [4], [37]), (5, 1, 120, 33, [17], [200]),
+    (2, 2, 8, 16, [1, 2], [5, 100]), (16, 2, 128, 16, [40], [41]), (8, 8, 72, 128, [70, 2], [90, 1000]), (64, 1, 128, 256, [2], [3000]),
+    (4, 2, 64, 16, [9, 4], [5, 0]),                       # fewer keys than new tokens: the first ones see nothing
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("i", range(len(READ_CASES)))
+def test_attention_cache(i, dtype):
+    c = cache_case(100 + i, dtype, *READ_CASES[i], [torch.int32, torch.int64][i % 2])
+    check_cache_attention(c)
+    check_cache_attention(c, causal=False, scale=0.3)
+    check_cache_attention(c, cap=2.5)
+    slopes = (2.0 ** -torch.arange(1, READ_CASES[i][0] + 1, dtype=torch.float32) * 3).cuda()
+    check_cache_attention(c, slopes=slopes)
+    check_cache_attention(c, slopes=slopes, cap=30.0, causal=False)
+
+
+def trees(seed, new):
+    g, words = gen(seed), []
+    for n in new:
+        seen = []
+        for i in range(n):
+            up = seen[int(torch.randint(max(0, i - 5), i, (1,), generator=g))] if i else 0
+            seen.append(up | (1 << i if i < 64 else 0))
+        words += [x - (1 << 64) if x >> 63 else x for x in seen]
+    return torch.tensor(words, dtype=torch.int64).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("i", range(len(READ_CASES)))
+def test_attention_cache_tree(i, dtype):
+    c = cache_case(200 + i, dtype, *READ_CASES[i])
+    tree = trees(i, READ_CASES[i][4])
+    check_cache_attention(c, tree=tree)
+    tree[::3] = 0                                         # these see none of the new tokens
+    check_cache_attention(c, tree=tree, cap=10.0)
