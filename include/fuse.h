@@ -453,6 +453,23 @@ int fuse_attention_backward(const fuse_attn *attn, const fuse_attn_grads *grads,
                             void *stream);
 int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads, void *stream);
 
+/* Attention whose scores are shaped before the softmax:
+ *     S = scale * Q t(K), or cap * tanh(scale * Q t(K) / cap) where cap is not 0;  then S_ij - slopes[h] * |distance of i and j| where there are
+ *     slopes, in places among the keys (query i stands at key i + keys - queries)
+ * and with prefix_lengths, which goes with causal: all queries of sequence s see its first prefix_lengths[s] keys, beside those up to their own.
+ * All else is as in fuse_attention and its gradient: results, workspaces (fuse_attention_bytes; the gradients' have a call of their own),
+ * limits.  A shape that is NULL or has nothing set is fuse_attention itself.  Slopes are constants: they get no gradient. */
+typedef struct {
+    double cap;                             /* 0: none, else 1e-3 to 1e6 */
+    const float *slopes;                    /* heads values on the device, or NULL */
+    const void *prefix_lengths;             /* seqs values of the offsets' type on the device, or NULL */
+} fuse_attn_shape;
+int fuse_attention_shaped(const fuse_attn *attn, const fuse_attn_shape *shape, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse,
+                          void *workspace, size_t workspace_bytes, void *stream);
+size_t fuse_attention_shaped_backward_bytes(const fuse_attn *attn, const fuse_attn_shape *shape);
+int fuse_attention_shaped_backward(const fuse_attn *attn, const fuse_attn_shape *shape, const fuse_attn_grads *grads, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
 /* Norms of queries and keys per head with the rotation by their positions, in one pass: for every token and head
  *     n = x / sqrt(mean(x^2) + eps) o weight         (over the head's dim values; n = x without a weight)
  *     pair (a, b) of n:  a' = a cos(t) - b sin(t),  b' = a sin(t) + b cos(t),  t = position * freqs[pair]

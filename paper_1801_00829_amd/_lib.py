@@ -61,6 +61,10 @@ class AttnGrads(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("dq_token_ld", "dq_head_ld", "dk_token_ld", "dk_head_ld", "dv_token_ld", "dv_head_ld")]
 
 
+class AttnShape(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_double), ("slopes", ctypes.c_void_p), ("prefix_lengths", ctypes.c_void_p)]
+
+
 class Rotary(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "heads", "kv_heads", "dim", "pairs", "axes", "positions_are_64")] + \
                [("sections", ctypes.c_int32 * 4), ("tokens", ctypes.c_int64), ("position_ld", ctypes.c_int64)] + \
@@ -152,6 +156,8 @@ def load():
                        ("fuse_block_norm_backward", [P(Block), vp, i64, vp, i64, vp, i64, P(BlockGrads), vp, size, vp]),
                        ("fuse_attention", [P(Attn), vp, i64, i64, vp, vp, size, vp]),
                        ("fuse_attention_backward", [P(Attn), P(AttnGrads), vp, size, vp]),
+                       ("fuse_attention_shaped", [P(Attn), P(AttnShape), vp, i64, i64, vp, vp, size, vp]),
+                       ("fuse_attention_shaped_backward", [P(Attn), P(AttnShape), P(AttnGrads), vp, size, vp]),
                        ("fuse_attention_zero_rest", [P(Attn), P(AttnGrads), vp]),
                        ("fuse_qk_rotary", [P(Rotary), vp, i64, i64, vp, i64, i64, vp]),
                        ("fuse_qk_rotary_backward", [P(Rotary), P(RotaryGrads), vp, size, vp]),
@@ -161,7 +167,8 @@ def load():
                        ("fuse_grad_clip", [vp, i64, f64, f64, vp, vp, vp, size, vp])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, ci
     for name, args in (("fuse_block_norm_backward_bytes", [P(Block)]), ("fuse_attention_bytes", [P(Attn)]),
-                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_qk_rotary_backward_bytes", [P(Rotary)]),
+                       ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_attention_shaped_backward_bytes", [P(Attn), P(AttnShape)]),
+                        ("fuse_qk_rotary_backward_bytes", [P(Rotary)]),
                        ("fuse_attention_cache_bytes", [P(Cache), P(CacheQuery)]), ("fuse_grad_norm_bytes", [vp, i64])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, size
     lib.fuse_last_error.restype = ctypes.c_char_p

@@ -265,16 +265,30 @@ def _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale):
                   qs[2] ** -0.5 if scale is None else scale, qp, kp, vp, q_token, q_head, k_token, k_head, v_token, v_head)
 
 
-def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=True, scale=None, out=None, lse=None, stream=None):
-    """C: fuse_attention.  softmax(scale * q k^T + mask) v for packed sequences; returns (out, lse).
+def _shape(f, q, offsets, causal, cap, slopes, prefix):
+    """What is done to the scores; None: nothing."""
+    if cap is None and slopes is None and prefix is None:
+        return None
+    if prefix is not None and not causal:
+        raise ValueError("a prefix goes with causal: without it all queries see all keys")
+    return L.AttnShape(_cap(cap), None if slopes is None else _row(slopes, q, torch.float32, f.heads, "slopes"),
+                       None if prefix is None else _places(prefix, offsets, q.device, f.seqs, "prefix"))
+
+
+def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=True, scale=None, out=None, lse=None, stream=None, cap=None,
+                   slopes=None, prefix=None):
+    """C: fuse_attention, fuse_attention_shaped.  softmax(scale * q k^T + mask) v for packed sequences; returns (out, lse).
 
     q: (tokens, heads, dim), k and v: (key tokens, key heads, dim), bfloat16 or float16, heads a multiple of key heads; parts of
     one projection can be passed as they are.  offsets: the sequences' first queries and the end of the last one; key_offsets likewise
     for the keys (None: the same), with key_lengths only so many keys from each sequence's first one on (a cache with room).
     causal: the last query sees all keys, the one before it all but the last, and so on.  scale: None is 1 / sqrt(dim).  lse:
     (tokens, heads) float32.  Rows that belong to no sequence are not written: in results made here they hold anything (NaN
-    among it: a padded batch whose other rows go on into sums over all rows takes out=torch.zeros_like(q))."""
+    among it: a padded batch whose other rows go on into sums over all rows takes out=torch.zeros_like(q)).
+    cap: scores become cap * tanh(score / cap).  slopes: (heads,) float32, slopes[h] * |distance| is taken off the scores, in places among the
+    keys.  prefix: a length per sequence, like offsets; all its queries see so many of its first keys (with causal)."""
     f = _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale)
+    shape = _shape(f, q, offsets, causal, cap, slopes, prefix)
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != q.device):
         raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % (tuple(q.shape[:2]), q.device))
     lib = L.load()
@@ -290,19 +304,22 @@ def fuse_attention(q, k, v, offsets, key_offsets=None, key_lengths=None, causal=
             op, o_token, o_head = _heads_of(o, q, "out", n, heads)
         nbytes = lib.fuse_attention_bytes(f)
         ws = _workspace(nbytes, q.device) if nbytes else None
-        _check(lib.fuse_attention(f, op, o_token, o_head, l.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, handle))
+        args = (op, o_token, o_head, l.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, handle)
+        _check(lib.fuse_attention(f, *args) if shape is None else lib.fuse_attention_shaped(f, shape, *args))
         return o, l
 
     return _run(q.device, stream, call)
 
 
 def fuse_attention_backward(dout, q, k, v, out, lse, offsets, key_offsets=None, key_lengths=None, causal=True, scale=None,
-                            dq=None, dk=None, dv=None, stream=None):
-    """C: fuse_attention_backward.  Gradients (dq, dk, dv) of fuse_attention's out, given its results and its other arguments.
+                            dq=None, dk=None, dv=None, stream=None, cap=None, slopes=None, prefix=None):
+    """C: fuse_attention_backward, fuse_attention_shaped_backward.  Gradients (dq, dk, dv) of fuse_attention's out, given its results and its
+    other arguments; slopes are constants.
 
     dq, dk, dv: tensors to write to.  Rows that belong to no sequence (before the first and behind the last one, and behind a sequence's
     key_lengths) are left as they were in these, and 0 in results made here."""
     f = _attn(q, k, v, offsets, key_offsets, key_lengths, causal, scale)
+    shape = _shape(f, q, offsets, causal, cap, slopes, prefix)
     if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.device != q.device:
         raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % (tuple(q.shape[:2]), q.device))
     lib = L.load()
@@ -317,8 +334,11 @@ def fuse_attention_backward(dout, q, k, v, out, lse, offsets, key_offsets=None, 
             own = L.AttnGrads.from_buffer_copy(g)
             own.dq, own.dk, own.dv = [a[0] if t is None else None for a, t in zip(at[2:], (dq, dk, dv))]
             _check(lib.fuse_attention_zero_rest(f, own, handle))
-        ws = _workspace(lib.fuse_attention_backward_bytes(f), q.device)
-        _check(lib.fuse_attention_backward(f, g, ws.data_ptr(), ws.numel(), handle))
+        ws = _workspace(lib.fuse_attention_backward_bytes(f) if shape is None else lib.fuse_attention_shaped_backward_bytes(f, shape), q.device)
+        if shape is None:
+            _check(lib.fuse_attention_backward(f, g, ws.data_ptr(), ws.numel(), handle))
+        else:
+            _check(lib.fuse_attention_shaped_backward(f, shape, g, ws.data_ptr(), ws.numel(), handle))
         return tuple(got)
 
     return _run(q.device, stream, call)

@@ -11,9 +11,9 @@ ARCH = "gfx950"
 
 HOST_SOURCES = ["libfuse.cpp", "expr.cpp", "runtime.cpp"]
 DEVICE_SOURCES = ["probe.hip", "check.hip", "transpose.hip", "noalloc.hip", "block_norm_f64.hip", "block_norm_f32.hip",
-                  "block_norm_bf16.hip", "block_norm_f16.hip", "attention_grad.hip", "attention.hip", "attention_cache.hip", "block_norm.hip", "qk_rotary.hip", "grad_clip.hip"]
+                  "block_norm_bf16.hip", "block_norm_f16.hip", "attention_grad_shaped_bf16.hip", "attention_grad_shaped_f16.hip", "attention_grad.hip", "attention_shaped.hip", "attention.hip", "attention_cache.hip", "block_norm.hip", "qk_rotary.hip", "grad_clip.hip"]
 TEXT_DEPS = ["fuse_args.h", "skel_common.inc", "skel_cell.inc", "skel_row_dense.inc", "skel_row_csr.inc", "skel_row_csr_stream.inc", "skel_row_mfma.inc", "skel_row_mfma_wave.inc", "skel_row_mfma_pipe.inc", "skel_row_stored.inc",
-             "skel_outer.inc", "expr.h", "runtime.h", "block_ops.h", "block_norm.h", "attention.h", "attention_tiles.h"]
+             "skel_outer.inc", "expr.h", "runtime.h", "block_ops.h", "block_norm.h", "attention.h", "attention_tiles.h", "attention_forward.h", "attention_backward.h"]
 
 
 def _gen_args_text():

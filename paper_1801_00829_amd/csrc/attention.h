@@ -28,7 +28,18 @@ struct AttnArgs {
     int seqs, heads, kv_heads, group, dim, causal, off64;
     float scale;
     unsigned div_mul, div_shift;           // rows / group, see place_of
+    // what is done to the scores, see Shape
+    float cap;
+    const float *slopes;                   // of every head
+    const void *prefix;                    // of every sequence, like q_off; NULL: none
+    int *row_place;                        // gradients: place among the keys, and slope in base 2, of every row; see stat_at
+    float *row_slope;
 };
+
+// What is done to the scores before the softmax, as kernels are compiled for it:  S = cap tanh(scale q k / cap) - slope |distance|, and a
+// prefix of the keys that all queries of a sequence see.
+enum Shape { kPlain = 0, kShaped = 1, kCapped = 2, kSloped = 4 };          // (a prefix may be there with kShaped, which all but kPlain have)
+template <int SHAPE> constexpr bool kScored = (SHAPE & (kCapped | kSloped)) != 0;
 
 struct Seq {
     long long q0, k0;                      // first query and first key
@@ -181,10 +192,17 @@ __device__ __forceinline__ Work work_of(const AttnArgs &a, int tile, unsigned b)
     return w;
 }
 
-// Keys that the query at `place` sees: 0 .. the result.
-__device__ __forceinline__ int seen_by(const AttnArgs &a, const Seq &x, int place)
+// The sequence's prefix.
+template <int SHAPE>
+__device__ __forceinline__ int prefix_of(const AttnArgs &a, int seq)
 {
-    return a.causal ? min(max(place + x.nk - x.nq + 1, 0), x.nk) : x.nk;
+    return SHAPE != kPlain && a.prefix ? (int)min(max(offset_at(a.prefix, seq, a.off64), 0LL), (1LL << 31) - 1) : 0;
+}
+
+// Keys that the query at `place` sees: 0 .. the result.
+__device__ __forceinline__ int seen_by(const AttnArgs &a, const Seq &x, int place, int prefix)
+{
+    return a.causal ? min(max(place + x.nk - x.nq + 1, prefix), x.nk) : x.nk;
 }
 
 // r / group for r < 2^31, with mul = floor(2^(31 + n) / group) + 1 and 2^n the next power of two: mul * group lies between 2^(31 + n)
@@ -195,10 +213,37 @@ __device__ __forceinline__ int place_of(const AttnArgs &a, int r)
 }
 
 // First place whose query sees key j (nq: none).
-__device__ __forceinline__ int first_that_sees(const AttnArgs &a, const Seq &x, int j)
+template <int SHAPE>
+__device__ __forceinline__ int first_that_sees(const AttnArgs &a, const Seq &x, int j, int prefix)
 {
-    return a.causal ? min(max(j - (x.nk - x.nq), 0), x.nq) : 0;
+    return a.causal && (SHAPE == kPlain || j >= prefix) ? min(max(j - (x.nk - x.nq), 0), x.nq) : 0;
 }
+
+// Scores of the matrix units, to base 2, as they go into the softmax (kScored).
+template <int SHAPE>
+struct Scores {
+    float mul, cap;
+
+    __device__ __forceinline__ explicit Scores(const AttnArgs &a)
+    {
+        constexpr float log2e = 1.44269504088896340736f;
+        mul = SHAPE & kCapped ? 2.0f * log2e * a.scale / a.cap : a.scale * log2e;
+        cap = a.cap * log2e;
+    }
+    // `far`: distance of query and key; `d`: the score's derivative by scale q k.  tanh(y) = 1 - 2 r with r = 1 / (exp(2 y) + 1): off by some
+    // 2^-23 whatever y, which is that part of the cap in a score
+    __device__ __forceinline__ float of(float p, float far, float slope, float &d) const
+    {
+        p *= mul;
+        d = 1.0f;
+        if (SHAPE & kCapped) {
+            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(p) + 1.0f);
+            p = fmaf(-2.0f * cap, r, cap);
+            d = 4.0f * fmaf(-r, r, r);
+        }
+        return SHAPE & kSloped ? fmaf(-slope, fabsf(far), p) : p;
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ T *row_of(const Mat &m, long long token, int head)
@@ -221,6 +266,9 @@ __device__ __forceinline__ long long lift_at(const AttnArgs &a, const Work &w, i
 
 // Checks of both directions, and the arguments that both have (host).
 int check_attn(const fuse_attn *f);
+int check_shape(const fuse_attn *f, const fuse_attn_shape *shape);
+int shape_of(const fuse_attn_shape *shape);                // as a Shape; NULL: kPlain
+void set_shape(AttnArgs &a, const fuse_attn_shape *shape);
 AttnArgs attn_args(const fuse_attn *f);
 int check_rows(const fuse_attn *f, const void *p, int64_t token_ld, int64_t head_ld, int64_t heads, int64_t tokens, const char *what);
 

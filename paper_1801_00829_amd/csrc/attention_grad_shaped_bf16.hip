@@ -1,0 +1,8 @@
+// Attention with capped scores, a bias by distance or a prefix, gradients.
+#include "attention_backward.h"
+
+namespace fuse {
+namespace backward {
+FUSE_BACKWARD(, __bf16, 1) FUSE_BACKWARD(, __bf16, 3) FUSE_BACKWARD(, __bf16, 5) FUSE_BACKWARD(, __bf16, 7)
+}  // namespace backward
+}  // namespace fuse

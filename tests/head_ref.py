@@ -5,7 +5,7 @@ the arithmetic in between has (fp32, fp64 for fp64) for sums of ``n`` terms, and
 """
 import torch
 
-from block_ref import F32, half_step
+from block_ref import F32, half_step, sequences
 
 F64 = 2.0 ** -53
 
@@ -195,3 +195,75 @@ def cache_attention(c, causal=True, scale=None, cap=None, slopes=None, tree=None
                 if f is not None:
                     far_lse[rows, h] = f
     return out, lse, far, far_lse
+
+
+# ------------------------------------------------------------- attention with shaped scores ---
+
+def _problems(c, causal, scale, cap, slopes, prefix):
+    """Per sequence and head: (rows, keys, head, key head, q, k, v, scores, tanh, how far off scores are, which pairs meet)."""
+    q, k, v = (c[n].double().cpu() for n in "qkv")
+    group = q.shape[1] // k.shape[1]
+    for s, (rows, keys) in enumerate(sequences(c["offsets"], c["key_offsets"], c["key_lengths"])):
+        nq, nk = rows.stop - rows.start, keys.stop - keys.start
+        place, j = torch.arange(nq) + nk - nq, torch.arange(nk)
+        first = 0 if prefix is None else int(prefix[s])
+        meet = (j[None] <= place[:, None]) | (j < first)[None] if causal else torch.ones(nq, nk, dtype=torch.bool)
+        for h in range(q.shape[1]):
+            qh, kh, vh = q[rows, h], k[keys, h // group], v[keys, h // group]
+            x, t, off = shaped_scores(qh, kh, scale, cap, 0.0 if slopes is None else float(slopes[h]), place, meet)
+            yield rows, keys, h, h // group, qh, kh, vh, x, t, off, meet
+
+
+def shaped_attention(c, causal=True, scale=None, cap=None, slopes=None, prefix=None):
+    """(out, lse, bound, bound of lse); rows of no sequence are NaN."""
+    scale = c["q"].shape[2] ** -0.5 if scale is None else scale
+    t = c["q"].dtype
+    out, lse = torch.full(c["q"].shape, torch.nan, dtype=torch.float64), torch.full(c["q"].shape[:2], torch.nan, dtype=torch.float64)
+    far, far_lse = torch.zeros_like(out), torch.zeros_like(lse)
+    for rows, _, h, _, _, _, vh, x, _, off, meet in _problems(c, causal, scale, cap, slopes, prefix):
+        def lost(p):                                       # fp16: 2^-36 of the sum, times the value
+            return 2.0 ** -36 * (meet.double() @ torch.nan_to_num(vh.abs()).amax(1, keepdim=True)) * torch.ones_like(p) / max(1, vh.shape[0])
+
+        out[rows, h], lse[rows, h], far[rows, h], f = attend(x, off, vh, vh.abs(), t, lost if t == torch.float16 else None)
+        if f is not None:
+            far_lse[rows, h] = f
+    return out, lse, far, far_lse
+
+
+def shaped_attention_grad(c, out, lse, causal=True, scale=None, cap=None, slopes=None, prefix=None):
+    """((dq, bound), (dk, bound), (dv, bound)) of the formula on these inputs; rows of no sequence are NaN."""
+    scale = c["q"].shape[2] ** -0.5 if scale is None else scale
+    t = c["q"].dtype
+    step, tiny16 = half_step(t), 2.0 ** -25 if t == torch.float16 else torch.finfo(t).tiny
+    dout, o, l = (x.double().cpu() for x in (c["dout"], out, lse))
+    dq, dk, dv = (torch.full(c[n].shape, torch.nan, dtype=torch.float64) for n in "qkv")
+    fq, fk, fv = (torch.zeros_like(x) for x in (dq, dk, dv))
+    rounded = []
+    for _, keys in sequences(c["offsets"], c["key_offsets"], c["key_lengths"]):
+        dk[keys], dv[keys] = 0.0, 0.0
+    for rows, keys, h, g, qh, kh, vh, x, tanh, off, meet in _problems(c, causal, scale, cap, slopes, prefix):
+        if not kh.shape[0]:
+            dq[rows, h] = 0.0
+            continue
+        dy = dout[rows, h]
+        p = torch.where(meet, torch.exp(torch.where(meet, x, 0.0) - l[rows, h][:, None]), 0.0)
+        delta = (dy * o[rows, h]).sum(1)[:, None]
+        dp = dy @ vh.T
+        turn = 1.0 if tanh is None else 1.0 - tanh.square()
+        ds = torch.where(meet, scale * p * (dp - delta) * turn, 0.0)
+        more = (max(x.shape) // 16 + 24) * F32
+        e = (qh.shape[1] + 8) * 2 * F32 * (dy.abs() @ vh.abs().T + (dy * o[rows, h]).abs().sum(1)[:, None])
+        fds = 1.05 * ((step + off + more) * ds.abs() + scale * p * e)
+        if cap:                                            # the tanh is off by some 2^-23, its derivative by twice that, and by the score's error
+            fds = fds + scale * p * (dp - delta).abs() * (16 * F32 + 2 * off / cap)
+        sub = 2.0 ** -36 if t == torch.float16 else 0.0    # fp16: of the largest of the row (dq), of the rows of all heads of the key head (dk)
+        rounded.append((keys, g, ds.abs().amax() if ds.numel() else 0.0, meet.double().T @ qh.abs()))
+        dq[rows, h] = _product(ds, kh)
+        fq[rows, h] = 1.01 * step * dq[rows, h].abs() + _product(fds + sub * ds.abs().amax(1, keepdim=True) * meet, kh.abs()) + tiny16
+        dk[keys, g] += _product(ds.T, qh)
+        fk[keys, g] += _product(fds.T, qh.abs())
+        dv[keys, g] += _product(p.T, dy)
+        fv[keys, g] += _product((1.05 * (step + off + more) * p + (2.0 ** -40 if sub else 0.0) * meet).T, dy.abs())
+    for keys, g, _, size in rounded if t == torch.float16 else []:
+        fk[keys, g] += 2.0 ** -36 * max(float(r[2]) for r in rounded if r[:2] == (keys, g)) * size
+    return (dq, fq), (dk, fk + 1.01 * step * dk.abs() + tiny16), (dv, fv + 1.01 * step * dv.abs() + tiny16)

@@ -7,7 +7,7 @@ import torch
 import block_ref as R
 import head_ref as H
 import paper_1801_00829_amd as F
-from test_gpu_block_ops import DT, gen, rnd
+from test_gpu_block_ops import DT, attn_case, gen, offs, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -200,3 +200,75 @@ def test_attention_cache_tree(i, dtype):
     check_cache_attention(c, tree=tree)
     tree[::3] = 0                                         # these see none of the new tokens
     check_cache_attention(c, tree=tree, cap=10.0)
+
+
+# ------------------------------------------------------------- attention with shaped scores ---
+
+SHAPED_CASES = {
+    "one": ("bf16", 1, 1, 64, [1]),
+    "two_of_one": ("fp16", 4, 2, 128, [1, 1]),
+    "odd": ("bf16", 6, 2, 64, [37, 1, 130]),
+    "none_between": ("fp16", 4, 4, 72, [5, 0, 200, 0]),
+    "wide_group": ("bf16", 8, 1, 8, [65]),
+    "group_3": ("fp16", 6, 2, 80, [129, 63]),
+    "long": ("bf16", 4, 2, 128, [600, 257]),
+    "seventy": ("bf16", 2, 2, 64, [1, 3, 0, 7, 33, 2, 64] * 10),
+    "shared_by_8": ("bf16", 8, 1, 128, [700, 90, 0]),
+    "shared_by_6": ("fp16", 6, 1, 80, [1, 801]),
+    "dim_96": ("fp16", 2, 1, 96, [191]),
+    # other keys than queries: lengths of both, room of a cache
+    "token": ("bf16", 8, 2, 128, [1, 1, 1], [1, 77, 300], 320),
+    "tokens_long": ("fp16", 4, 4, 128, [1, 1], [2500, 1300], 2560),
+    "more_queries": ("bf16", 4, 2, 64, [50, 130], [20, 1], None),
+    "no_keys": ("bf16", 4, 2, 128, [5, 3], [0, 9], None),
+    "chunk": ("bf16", 4, 2, 128, [100, 64], [400, 1000], 1024),
+    "chunk_long": ("fp16", 2, 1, 80, [40], [3000], None),
+}
+SHAPES = {"cap": (2.5, False, False), "slopes": (None, True, False), "prefix": (None, False, True), "cap_prefix": (30.0, False, True),
+          "slopes_prefix": (None, True, True), "all": (5.0, True, True)}
+
+
+def shape_of(c, name, seed=5):
+    """Arguments of a shape: for the call, and for the reference."""
+    cap, sloped, prefixed = SHAPES[name]
+    g, seqs = gen(seed), c["offsets"].numel() - 1
+    slopes = 2.0 ** (-8.0 * torch.rand(c["q"].shape[1], generator=g)) if sloped else None
+    longest = int((c["key_offsets"] if c["key_offsets"] is not None else c["offsets"]).diff().max())
+    prefix = torch.randint(-1, longest + 3, (seqs,), generator=g, dtype=torch.int32) if prefixed else None
+    if prefixed and seqs > 1:
+        prefix[1] = 0
+    return dict(cap=cap, slopes=slopes, prefix=prefix)
+
+
+def on_gpu(shape, wide=False):
+    prefix = shape["prefix"]
+    return dict(cap=shape["cap"], slopes=None if shape["slopes"] is None else shape["slopes"].cuda(),
+                prefix=None if prefix is None else prefix.to(torch.int64 if wide else torch.int32).cuda())
+
+
+def check_shaped(c, shape, causal=True, scale=None, wide=False):
+    out, lse = torch.full_like(c["dout"], 7.0), torch.full(c["q"].shape[:2], 7.0, device="cuda")
+    F.fuse_attention(c["q"], c["k"], c["v"], **offs(c, wide), causal=causal, scale=scale, out=out, lse=lse, **on_gpu(shape, wide))
+    ref, ref_lse, far, far_lse = H.shaped_attention(c, causal, scale, **shape)
+    n = int(c["offsets"][-1])
+    R.within(out[:n], ref[:n], far[:n], "out")
+    R.within(lse[:n], ref_lse[:n], far_lse[:n], "lse")
+    assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()       # rows of no sequence are left as they were
+    d = [torch.full(t.shape, 7.0, dtype=t.dtype, device="cuda") for t in (c["q"], c["k"], c["v"])]
+    F.fuse_attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, **offs(c, wide), causal=causal, scale=scale, dq=d[0], dk=d[1], dv=d[2],
+                              **on_gpu(shape, wide))
+    want = H.shaped_attention_grad(c, out, lse, causal, scale, **shape)
+    for got, (w, f), name in zip(d, want, ("dq", "dk", "dv")):
+        mine = ~w.isnan().reshape(w.shape[0], -1).all(1)
+        R.within(got[mine.cuda()], w[mine], f[mine], name)
+        assert (got[~mine.cuda()] == 7.0).all(), name
+
+
+@pytest.mark.parametrize("shape", sorted(SHAPES))
+@pytest.mark.parametrize("name", sorted(SHAPED_CASES))
+def test_shaped_attention(name, shape):
+    dtype, heads, kv_heads, dim, *rest = SHAPED_CASES[name]
+    c = attn_case(13, dtype, heads, kv_heads, dim, *rest, spare=3)
+    check_shaped(c, shape_of(c, shape), wide=heads == 4)
+    if SHAPES[shape][2] is False:
+        check_shaped(c, shape_of(c, shape), causal=False, scale=0.4)
