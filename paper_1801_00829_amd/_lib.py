@@ -159,17 +159,17 @@ def load():
                        ("fuse_attention_shaped", [P(Attn), P(AttnShape), vp, i64, i64, vp, vp, size, vp]),
                        ("fuse_attention_shaped_backward", [P(Attn), P(AttnShape), P(AttnGrads), vp, size, vp]),
                        ("fuse_attention_zero_rest", [P(Attn), P(AttnGrads), vp]),
-                       ("fuse_qk_rotary", [P(Rotary), vp, i64, i64, vp, i64, i64, vp]),
-                       ("fuse_qk_rotary_backward", [P(Rotary), P(RotaryGrads), vp, size, vp]),
-                       ("fuse_cache_write", [P(Cache), vp, i64, i64, vp, i64, i64, vp]),
-                       ("fuse_attention_cache", [P(Cache), P(CacheQuery), vp, i64, i64, vp, vp, size, vp]),
+                       ("fuse_qk_rotary", [vp, vp, i64, i64, vp, i64, i64, vp]),
+                       ("fuse_qk_rotary_backward", [vp, vp, vp, size, vp]),
+                       ("fuse_cache_write", [vp, vp, i64, i64, vp, i64, i64, vp]),
+                       ("fuse_attention_cache", [vp, vp, vp, i64, i64, vp, vp, size, vp]),
                        ("fuse_grad_norm", [vp, i64, vp, vp, size, vp]),
                        ("fuse_grad_clip", [vp, i64, f64, f64, vp, vp, vp, size, vp])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, ci
     for name, args in (("fuse_block_norm_backward_bytes", [P(Block)]), ("fuse_attention_bytes", [P(Attn)]),
                        ("fuse_attention_backward_bytes", [P(Attn)]), ("fuse_attention_shaped_backward_bytes", [P(Attn), P(AttnShape)]),
-                        ("fuse_qk_rotary_backward_bytes", [P(Rotary)]),
-                       ("fuse_attention_cache_bytes", [P(Cache), P(CacheQuery)]), ("fuse_grad_norm_bytes", [vp, i64])):
+                        ("fuse_qk_rotary_backward_bytes", [vp]),
+                       ("fuse_attention_cache_bytes", [vp, vp]), ("fuse_grad_norm_bytes", [vp, i64])):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, size
     lib.fuse_last_error.restype = ctypes.c_char_p
     lib.fuse_last_kernel.restype = ctypes.c_char_p

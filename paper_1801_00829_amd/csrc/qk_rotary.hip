@@ -19,8 +19,8 @@ using namespace fuse;
 constexpr int kMaxDim = 256;
 constexpr int kMaxPairs = kMaxDim / 2;
 constexpr int kMaxAxes = 4;
-constexpr int kTokens = 4;                 // per block at a time
-constexpr int kGradBlocks = 1024;          // of a gradient call: each leaves one partial row of both weights' sums
+constexpr int kTokens = 8;                 // per block at a time, at most
+constexpr int kGradBlocks = 512;          // of a gradient call: each leaves one partial row of both weights' sums
 
 struct Heads {                             // queries, or keys
     const void *x, *w;                     // w NULL: no norm
@@ -50,23 +50,44 @@ __device__ __forceinline__ int token_of(const Heads &h, int r)
     return h.heads == 1 ? r : (int)(__umulhi((unsigned)r, h.div_mul) >> h.div_shift);
 }
 
-// Sum over aligned groups of `lanes` lanes, in all of them.
-template <typename A>
-__device__ __forceinline__ A row_sum(A v, int lanes)
+// Sums of N values over aligned groups of `lanes` lanes, in all of them.
+template <typename A, int N>
+__device__ __forceinline__ void row_sums(A (&v)[N], int lanes)
 {
+#define FUSE_ALL(...)                                                                                                      \
+    do {                                                                                                                  \
+        _Pragma("unroll") for (int n = 0; n < N; ++n) __VA_ARGS__;                                                        \
+    } while (0)
     if (lanes > 1)
-        v += moved<0xB1>(v);
+        FUSE_ALL(v[n] += moved<0xB1>(v[n]));
     if (lanes > 2)
-        v += moved<0x4E>(v);
+        FUSE_ALL(v[n] += moved<0x4E>(v[n]));
     if (lanes > 4)
-        v += moved<0x141>(v);
+        FUSE_ALL(v[n] += moved<0x141>(v[n]));
     if (lanes > 8)
-        v += moved<0x140>(v);
+        FUSE_ALL(v[n] += moved<0x140>(v[n]));
     if (lanes > 16)
-        v = swapped_sum<16>(v);
+        FUSE_ALL(v[n] = swapped_sum<16>(v[n]));
     if (lanes > 32)
-        v = swapped_sum<32>(v);
-    return v;
+        FUSE_ALL(v[n] = swapped_sum<32>(v[n]));
+}
+
+// Sums of N values over the lanes of a wave that are the same place of their groups, in all of them.
+template <typename A, int N>
+__device__ __forceinline__ void place_sums(A (&v)[N], int lanes)
+{
+    if (lanes <= 8)
+        FUSE_ALL(v[n] += moved<0x128>(v[n]));              // eight lanes on within sixteen, then four, two, one
+    if (lanes <= 4)
+        FUSE_ALL(v[n] += moved<0x124>(v[n]));
+    if (lanes <= 2)
+        FUSE_ALL(v[n] += moved<0x122>(v[n]));
+    if (lanes <= 1)
+        FUSE_ALL(v[n] += moved<0x121>(v[n]));
+    if (lanes <= 16)
+        FUSE_ALL(v[n] = swapped_sum<16>(v[n]));
+    if (lanes <= 32)
+        FUSE_ALL(v[n] = swapped_sum<32>(v[n]));
 }
 
 template <typename A> struct Turn { A c, s; };
@@ -216,9 +237,10 @@ __global__ void __launch_bounds__(256) qk_rotary_kernel(const RotaryArgs a)
                 x.load(row_at<const T>(h.x, first + t, head, h.x_token, h.x_head), at);
                 A scale = (A)1;
                 if (h.w) {
-                    A sum = (A)0;
-                    FUSE_PAIRS(sum += x.first(k, i) * x.first(k, i) + x.second(k, i) * x.second(k, i));
-                    scale = (A)1 / sqrt(row_sum(sum, a.lanes) / (A)a.dim + (A)a.eps);
+                    A sum[1] = {(A)0};
+                    FUSE_PAIRS(sum[0] += x.first(k, i) * x.first(k, i) + x.second(k, i) * x.second(k, i));
+                    row_sums(sum, a.lanes);
+                    scale = (A)1 / sqrt(sum[0] / (A)a.dim + (A)a.eps);
                 }
                 const Turn<A> *turn = table + t * pairs;
                 FUSE_PAIRS(
@@ -227,7 +249,7 @@ __global__ void __launch_bounds__(256) qk_rotary_kernel(const RotaryArgs a)
                         u *= scale * w.first(k, i);
                         v *= scale * w.second(k, i);
                     }
-                    const Turn<A> c = turn[min((k * a.lanes + lane) * V + i, pairs - 1)];
+                    const Turn<A> c = turn[min((k * a.lanes + lane) * V, pairs - V) + i];
                     x.set(k, i, u * c.c - v * c.s, u * c.s + v * c.c));
                 x.store(row_at<T>(h.out, first + t, head, h.out_token, h.out_head), at);
             }
@@ -242,13 +264,24 @@ __global__ void __launch_bounds__(256) qk_rotary_grad_kernel(const RotaryArgs a)
     using A = typename acc_of<T>::type;
     using P = Pairs<T, V, K, NEIGHBOURS>;
     __shared__ Turn<A> table[kTokens * kMaxPairs];
-    __shared__ A sums[2 * 256 * V * K];
+    __shared__ A sums[2][4][kMaxDim];
     const int lane = threadIdx.x & (a.lanes - 1), mine = threadIdx.x / a.lanes, step = 256 / a.lanes, pairs = a.dim / 2;
     int at[K][2];
     places<V, K, NEIGHBOURS>(a, lane, at);
-    A dw[2][K][V][2] = {};
+    A dw[2][2 * K * V] = {};
     for (long long first = (long long)blockIdx.x * a.per_turn; first < a.tokens; first += (long long)gridDim.x * a.per_turn) {
         const int tokens = (int)min((long long)a.per_turn, a.tokens - first);
+        auto load = [&](const Heads &h, int r, P &x, P &g) {
+            if (r < tokens * h.heads) {
+                const int t = token_of(h, r), head = r - t * h.heads;
+                g.load(row_at<const T>(h.dy, first + t, head, h.dy_token, h.dy_head), at);
+                if (h.w)
+                    x.load(row_at<const T>(h.x, first + t, head, h.x_token, h.x_head), at);
+            }
+        };
+        P ahead_x[2], ahead_g[2];          // the first rows of both are asked for before the table is made
+        load(a.side[0], mine, ahead_x[0], ahead_g[0]);
+        load(a.side[1], mine, ahead_x[1], ahead_g[1]);
         fill_table<A>(a, table, first, tokens);
         __syncthreads();
 #pragma unroll
@@ -260,26 +293,25 @@ __global__ void __launch_bounds__(256) qk_rotary_grad_kernel(const RotaryArgs a)
                 w.load(h.w, at);
             for (int r = mine; r < rows; r += step) {
                 const int t = token_of(h, r), head = r - t * h.heads;
-                P x, g;
-                g.load(row_at<const T>(h.dy, first + t, head, h.dy_token, h.dy_head), at);
-                if (h.w)
-                    x.load(row_at<const T>(h.x, first + t, head, h.x_token, h.x_head), at);
+                P x = ahead_x[side], g = ahead_g[side];
+                load(h, r + step, ahead_x[side], ahead_g[side]);
                 const Turn<A> *turn = table + t * pairs;
                 A gu[K][V], gv[K][V];      // turned back
                 FUSE_PAIRS(
-                    const Turn<A> c = turn[min((k * a.lanes + lane) * V + i, pairs - 1)];
+                    const Turn<A> c = turn[min((k * a.lanes + lane) * V, pairs - V) + i];
                     gu[k][i] = g.first(k, i) * c.c + g.second(k, i) * c.s;
                     gv[k][i] = g.second(k, i) * c.c - g.first(k, i) * c.s);
                 if (h.w) {
-                    A squares = (A)0, both = (A)0;
+                    A sum[2] = {(A)0, (A)0};               // of squares, and of the products with the gradient
                     FUSE_PAIRS(
-                        squares += x.first(k, i) * x.first(k, i) + x.second(k, i) * x.second(k, i);
-                        both += gu[k][i] * w.first(k, i) * x.first(k, i) + gv[k][i] * w.second(k, i) * x.second(k, i));
-                    const A scale = (A)1 / sqrt(row_sum(squares, a.lanes) / (A)a.dim + (A)a.eps);
-                    const A mean = row_sum(both, a.lanes) / (A)a.dim * scale * scale;
+                        sum[0] += x.first(k, i) * x.first(k, i) + x.second(k, i) * x.second(k, i);
+                        sum[1] += gu[k][i] * w.first(k, i) * x.first(k, i) + gv[k][i] * w.second(k, i) * x.second(k, i));
+                    row_sums(sum, a.lanes);
+                    const A scale = (A)1 / sqrt(sum[0] / (A)a.dim + (A)a.eps);
+                    const A mean = sum[1] / (A)a.dim * scale * scale;
                     FUSE_PAIRS(
-                        dw[side][k][i][0] += gu[k][i] * (x.first(k, i) * scale);
-                        dw[side][k][i][1] += gv[k][i] * (x.second(k, i) * scale);
+                        dw[side][2 * (k * V + i)] += gu[k][i] * (x.first(k, i) * scale);
+                        dw[side][2 * (k * V + i) + 1] += gv[k][i] * (x.second(k, i) * scale);
                         gu[k][i] = scale * (gu[k][i] * w.first(k, i) - x.first(k, i) * mean);
                         gv[k][i] = scale * (gv[k][i] * w.second(k, i) - x.second(k, i) * mean));
                 }
@@ -289,31 +321,31 @@ __global__ void __launch_bounds__(256) qk_rotary_grad_kernel(const RotaryArgs a)
         }
         __syncthreads();
     }
-    // the weights' sums of this block, over its rows' lanes in order
+    // the weights' sums of this block: over the rows of a wave, then over its waves
+    const int wave = threadIdx.x >> 6;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         if (!a.side[side].w)
             continue;
-        FUSE_PAIRS(
-            A *s = sums + mine * a.dim;
-            if (at[k][0] >= 0) {
-                const int e = NEIGHBOURS && V > 1 ? 2 * i : i;
-                const int f = NEIGHBOURS && V > 1 ? 2 * i + 1 : i;
-                s[at[k][0] + e] = dw[side][k][i][0];
-                s[(NEIGHBOURS && V > 1 ? at[k][0] : at[k][1]) + f] = dw[side][k][i][1];
-            });
-        __syncthreads();
-        for (int c = threadIdx.x; c < a.dim; c += 256) {
-            A s = (A)0;
-            for (int j = 0; j < step; ++j)
-                s += sums[j * a.dim + c];
-            const long long to = ((long long)side * gridDim.x + blockIdx.x) * a.dim + c;
-            if constexpr (sizeof(A) == 8)
-                a.partial_f64[to] = s;
-            else
-                a.partial_f32[to] = s;
-        }
-        __syncthreads();
+        place_sums(dw[side], a.lanes);
+        if ((threadIdx.x & 63) < a.lanes)
+            FUSE_PAIRS(
+                if (at[k][0] >= 0) {
+                    sums[side][wave][at[k][0] + (NEIGHBOURS && V > 1 ? 2 * i : i)] = dw[side][2 * (k * V + i)];
+                    sums[side][wave][NEIGHBOURS && V > 1 ? at[k][0] + 2 * i + 1 : at[k][1] + i] = dw[side][2 * (k * V + i) + 1];
+                });
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.dim; i += 256) {
+        const int side = i >= a.dim, c = i - side * a.dim;
+        if (!a.side[side].w)
+            continue;
+        const A s = (sums[side][0][c] + sums[side][1][c]) + (sums[side][2][c] + sums[side][3][c]);
+        const long long to = ((long long)side * gridDim.x + blockIdx.x) * a.dim + c;
+        if constexpr (sizeof(A) == 8)
+            a.partial_f64[to] = s;
+        else
+            a.partial_f32[to] = s;
     }
 }
 
@@ -490,8 +522,13 @@ void launch_any(int dtype, const RotaryArgs &a, bool vec, unsigned blocks, hipSt
     }
 }
 
-// Tokens of a block at a time: one where there are few, so that all of them start at once.
-int per_turn_for(const fuse_rotary *f) { return f->tokens >= 4096 ? kTokens : 1; }
+// Tokens of a block at a time: as many as it takes for the keys' rows to fill a block's lanes, but no more than leave 512 blocks.
+int per_turn_for(const fuse_rotary *f)
+{
+    const int rows = 256 / lanes_for(f->dim / 2, 16 / (int)dtype_size(f->dtype)), heads = f->kv_heads > 0 ? std::min(f->heads, f->kv_heads) : f->heads;
+    const int64_t full = (rows + heads - 1) / heads, few = (f->tokens + kGradBlocks - 1) / kGradBlocks;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(full, few), kTokens));
+}
 
 int rotary_impl(const fuse_rotary *f, void *q_out, int64_t q_token_ld, int64_t q_head_ld, void *k_out, int64_t k_token_ld, int64_t k_head_ld,
                 void *stream)
@@ -518,8 +555,8 @@ int rotary_impl(const fuse_rotary *f, void *q_out, int64_t q_token_ld, int64_t q
 
 int grad_blocks(const fuse_rotary *f)
 {
-    const int64_t per = per_turn_for(f);
-    return (int)std::min<int64_t>((f->tokens + per - 1) / per, kGradBlocks);
+    const int64_t per = per_turn_for(f), turns = (f->tokens + per - 1) / per, each = (turns + kGradBlocks - 1) / kGradBlocks;
+    return each ? (int)((turns + each - 1) / each) : 0;    // (all blocks with as many turns)
 }
 
 size_t grad_bytes(const fuse_rotary *f) { return (size_t)2 * grad_blocks(f) * f->dim * (f->dtype == FUSE_F64 ? 8 : 4); }
