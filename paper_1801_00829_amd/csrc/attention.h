@@ -220,6 +220,8 @@ __device__ __forceinline__ int first_that_sees(const AttnArgs &a, const Seq &x, 
 }
 
 // Scores of the matrix units, to base 2, as they go into the softmax (kScored).
+//
+// tanh(y) = 1 - 2 r with r = 1 / (exp(2 y) + 1): off by some 2^-23 whatever y, which is that part of the cap in a score.
 template <int SHAPE>
 struct Scores {
     float mul, cap;
@@ -230,8 +232,7 @@ struct Scores {
         mul = SHAPE & kCapped ? 2.0f * log2e * a.scale / a.cap : a.scale * log2e;
         cap = a.cap * log2e;
     }
-    // `far`: distance of query and key; `d`: the score's derivative by scale q k.  tanh(y) = 1 - 2 r with r = 1 / (exp(2 y) + 1): off by some
-    // 2^-23 whatever y, which is that part of the cap in a score
+    // `far`: distance of query and key; `d`: the score's derivative by scale q k
     __device__ __forceinline__ float of(float p, float far, float slope, float &d) const
     {
         p *= mul;

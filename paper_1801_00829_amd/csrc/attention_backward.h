@@ -325,18 +325,12 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
             const char *qt = lds[B][0], *gt = lds[B][1];
             const bool work = r0 + half * 32 + 32 > from_lo;
             f32x4u lse[4], delta[4];           // of rows 8 i + 4 h ..; behind the last row they are anything, and masked
-            i32x4u places[4];
-            f32x4u slopes[4];
-            if (work) {
+            if (work && !(SHAPE & kSloped)) {
                 const long long at = sbase + r0 + half * 32 + 4 * h;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     lse[i] = *reinterpret_cast<const f32x4u *>(a.lse2 + at + 8 * i);
                     delta[i] = *reinterpret_cast<const f32x4u *>(a.delta + at + 8 * i);
-                    if (SHAPE & kSloped) {
-                        places[i] = *reinterpret_cast<const i32x4u *>(a.row_place + at + 8 * i);
-                        slopes[i] = *reinterpret_cast<const f32x4u *>(a.row_slope + at + 8 * i);
-                    }
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -352,24 +346,40 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
                 }
                 ahead<L::kSteps * 2, 6>();
                 float w[16], ds[16];
+                if (kScored<SHAPE>) {
+                    // With slopes all that is kept of the rows is asked for only here: there are no registers to keep it in meanwhile (8192 packed
+                    // tokens, 32 heads over 8, dim 128, whole backward pass: 1044 us, 1091 with lse and delta asked for above as without slopes;
+                    // plain scores 845, with a cap 973, 1013 if they too are asked for here).
+                    i32x4u places[4];
+                    f32x4u slopes[4];
+                    if (SHAPE & kSloped)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if (kScored<SHAPE>) {
-                            float d, far = 0.0f, slope = 0.0f;
-                            if (SHAPE & kSloped)
-                                far = (float)(places[i][u] - key), slope = slopes[i][u];
-                            w[i * 4 + u] = __builtin_amdgcn_exp2f(scores.of(p[i * 4 + u], far, slope, d) - lse[i][u]);
-                            ds[i * 4 + u] = w[i * 4 + u] * ((dp[i * 4 + u] - delta[i][u]) * d);
-                        } else {
-                            w[i * 4 + u] = __builtin_amdgcn_exp2f(fmaf(p[i * 4 + u], c, -lse[i][u]));
-                            ds[i * 4 + u] = w[i * 4 + u] * (dp[i * 4 + u] - delta[i][u]);
+                        for (int i = 0; i < 4; ++i) {
+                            const long long at = sbase + r0 + half * 32 + 4 * h + 8 * i;
+                            places[i] = *reinterpret_cast<const i32x4u *>(a.row_place + at);
+                            slopes[i] = *reinterpret_cast<const f32x4u *>(a.row_slope + at);
+                            lse[i] = *reinterpret_cast<const f32x4u *>(a.lse2 + at);
+                            delta[i] = *reinterpret_cast<const f32x4u *>(a.delta + at);
                         }
-                        if (kLifted<T>)
-                            ds[i * 4 + u] *= lift_ds;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float d, far = 0.0f, slope = 0.0f;
+                        if (SHAPE & kSloped)
+                            far = (float)(places[i / 4][i % 4] - key), slope = slopes[i / 4][i % 4];
+                        w[i] = __builtin_amdgcn_exp2f(scores.of(p[i], far, slope, d) - lse[i / 4][i % 4]);
+                        ds[i] = w[i] * ((dp[i] - delta[i / 4][i % 4]) * d);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        w[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -lse[i / 4][i % 4]));
+                        ds[i] = w[i] * (dp[i] - delta[i / 4][i % 4]);
                     }
                 }
+                if (kLifted<T>)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        ds[i] *= lift_ds;
                 if (r0 + half * 32 < from_hi || r0 + half * 32 + 32 > rows) {
                     const int skip = from - r0 - half * 32 - 4 * h, left = rows - r0 - half * 32 - 4 * h;
 #pragma unroll
