@@ -50,6 +50,7 @@ struct CacheArgs {
     const float *slopes;
     long long q_tokens;
     int seqs, heads, kv_heads, group, dim, causal, off64, splits;
+    int tile;                              // rows of a block
     float scale, cap;
     Divider by_group;
     Divider by_row;                        // writing: rows of a token
@@ -149,10 +150,21 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const CacheArgs a)
 
 // ----------------------------------------------------------------------------------- reading ---
 
-constexpr int kRows = 32;                  // per block, as the columns of all products
 constexpr int kKeys = 32;                  // per step and wave
 constexpr int kWaves = 4;
 constexpr int kMaxSplits = 64;
+
+// One product D += A B of a wave: A is 16 x 32, B is 32 x 16.  Lane l (quarter g = l / 16) holds row l % 16 of A and column l % 16 of B, eight
+// neighbours 8 g .. 8 g + 7 of each, and of D column l % 16, rows 4 g .. 4 g + 3.
+template <typename T> __device__ __forceinline__ f32x4 product16(s16x8 a, s16x8 b, f32x4 c);
+template <> __device__ __forceinline__ f32x4 product16<__bf16>(s16x8 a, s16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 product16<_Float16>(s16x8 a, s16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
 
 template <typename T> __device__ __forceinline__ s16x8 widened(uint2 v);
 template <> __device__ __forceinline__ s16x8 widened<__bf16>(uint2 v)
@@ -187,80 +199,73 @@ __device__ __forceinline__ long long shuffled(long long v, int from)
     return (long long)((unsigned long long)(unsigned)lo | (unsigned long long)(unsigned)hi << 32);
 }
 
-// One block: 32 rows (queries of the heads of one key head, see attention.h) as columns; its keys in steps of 32 per wave, the four waves
-// beside each other, each with its own tiles, maxima and sums, which are joined at the end.  Values stay in 8 bits up to the registers that
-// feed the matrix units.  Scales of keys multiply the scores, those of values the weights before these are rounded.
+// The larger, or the sum, of the four lanes of a column.
+__device__ __forceinline__ float column_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return both_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float column_sum(float v) { return swapped_sum<32>(swapped_sum<16>(v)); }
+
+// One block: ROWS rows (queries of the heads of one key head, see attention.h) as columns, sixteen to a tile; its keys in steps of 32 per wave,
+// the four waves beside each other, each with its own tiles, maxima and sums, which are joined at the end.  Values stay in 8 bits up to the
+// registers that feed the matrix units.  Scales of keys multiply the scores, those of values the weights before these are rounded.
+//
+// All products are taken with the kept side as columns: S = K t(Q) leaves a lane the scores of keys 4 g .. and 16 + 4 g .. of its column, which,
+// as weights, are the B operand of the next product as they lie; its A is the transposed tile of values, read in that order.
 //
 // Weights times scales are rounded to fp16 for the product with the values, whatever T is: it has three digits more than bf16, and holds e4m3
 // exactly.  Its range: the maximum that a column's weights are taken against is that of score + log2(scale of the value), so that
 // weights times scales lie where fp16 has most digits, whatever the scales are; the sum of the weights carries the same factor.  With
 // weights in bf16, results of 32 tokens over 16384 places are 0.0023 off instead of 0.0017, which is what rounding them leaves.
-template <typename T, int DP, int CHUNK>
-__global__ void __launch_bounds__(256, 2) attention_cache_kernel(const CacheArgs a)
+template <typename T, int DP, int CHUNK, int ROWS>
+__global__ void __launch_bounds__(256, ROWS == 16 ? 3 : 2) attention_cache_kernel(const CacheArgs a)
 {
-    using Q = Tile<DP>;
     using L = Tiles8<DP, CHUNK>;
     using W = _Float16;                                    // of the weights
-    constexpr int kJoinPitch = 36;                         // floats, per column of 32 dims
-    static_assert(kWaves * L::kBytes >= kWaves * 32 * kJoinPitch * 4, "the joining takes the tiles' place");
+    using lds_i32x2 = __attribute__((address_space(3))) i32x2;
+    constexpr int NT = ROWS / 16, kSteps = DP / 32, kDims = DP / 16;
+    constexpr int kJoinDims = 64 / NT, kJoinPitch = kJoinDims + 4;         // of all waves' sums at a time
+    static_assert(kWaves * L::kBytes >= kWaves * ROWS * kJoinPitch * 4, "the joining takes the tiles' place");
     __shared__ __attribute__((aligned(256))) char lds[kWaves * L::kBytes];
-    __shared__ float stats[kWaves][2][32];
+    __shared__ float stats[kWaves][2][ROWS];
 
     const int kvh = blockIdx.x % a.kv_heads;
     const unsigned rest = blockIdx.x / a.kv_heads;
     const int split = rest % a.splits;
-    const Work work = tile_at<false>(a, kRows, rest / a.splits);
+    const Work work = tile_at<false>(a, ROWS, rest / a.splits);
     if (!work.any)
         return;
     const Seq &x = work.x;
     const int first = work.first, rows = x.nq * a.group;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
-    const int r = first + col;
-    const bool in = r < rows;
-    const int place = quotient(a.by_group, in ? r : rows - 1), head = kvh * a.group + (in ? r : rows - 1) - place * a.group;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
     const int before = x.nk - x.nq;                        // keys that are there already
-    int seen = x.nk, seen_lo = x.nk, end = x.nk;
-    if (a.tree) {
-        seen_lo = max(before, 0);
-    } else if (a.causal) {
-        seen = min(max(place + x.nk - x.nq + 1, 0), x.nk);
-        seen_lo = __builtin_amdgcn_readfirstlane(seen);
-        end = __builtin_amdgcn_readlane(seen, 31);
-    }
-    const unsigned long long tree = a.tree ? (unsigned long long)a.tree[x.q0 + place] : 0;
-    const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+    auto seen_by = [&](int place) { return a.causal && !a.tree ? min(max(place + before + 1, 0), x.nk) : x.nk; };
+    const int seen_lo = a.tree ? max(before, 0) : seen_by(quotient(a.by_group, first));
 
-    int begin = 0;
+    int begin = 0, end = seen_by(quotient(a.by_group, min(first + ROWS, rows) - 1));
     if (a.splits > 1) {
         const int per = ((end + a.splits - 1) / a.splits + kKeys * kWaves - 1) / (kKeys * kWaves) * (kKeys * kWaves);
         begin = min(split * per, end);
         end = min(begin + per, end);
     }
 
-    s16x8 q[Q::kSteps];
-    operands<T, DP>(q, row_of<const T>(a.q, x.q0 + place, head), in, a.dim);
-
-    char *const tiles = lds + wave * L::kBytes;
-    char *const kt = tiles, *const vt = tiles + kKeys * L::kPitch;
-    float *const kscale = reinterpret_cast<float *>(tiles + 2 * kKeys * L::kPitch), *const vscale = kscale + kKeys, *const vlog = vscale + kKeys;
-    if (a.dim < DP) {                                      // zeros behind dim
-        for (int i = lane * 16; i < 2 * kKeys * L::kPitch; i += 1024)
-            *reinterpret_cast<uint4 *>(tiles + i) = make_uint4(0, 0, 0, 0);
-    }
-    const Pages &g = a.pages;
-    const int *table = g.table + work.seq * g.table_ld;
-    const int load_row = lane / L::kLanes, load_at = lane % L::kLanes * CHUNK;
+    // what is loaded of a step: a row's place is that of lane % 32
+    char *const kt = lds + wave * L::kBytes, *const vt = kt + kKeys * L::kPitch;
+    float *const kscale = reinterpret_cast<float *>(vt + kKeys * L::kPitch), *const vscale = kscale + kKeys, *const vlog = vscale + kKeys;
+    const Pages &pages = a.pages;
+    const int *table = pages.table + work.seq * pages.table_ld;
+    const int row = lane & 31, load_row = lane / L::kLanes, load_at = lane % L::kLanes * CHUNK;
     const bool loads = load_at < a.dim;
-    const unsigned char *const kbase = g.k + kvh * g.head_ld + load_at, *const vbase = g.v + kvh * g.head_ld + load_at;
-    const float *const sbase = (h ? g.v_scale : g.k_scale) + kvh * g.scale_head_ld;
-
+    const unsigned char *const kbase = pages.k + kvh * pages.head_ld + load_at, *const vbase = pages.v + kvh * pages.head_ld + load_at;
+    const float *const sbase = (lane >= 32 ? pages.v_scale : pages.k_scale) + kvh * pages.scale_head_ld;
     typename L::Part kp[L::kPasses], vp[L::kPasses];
     float sc = 0.0f;
-    auto page_at = [&](int j) { return min(max(table[quotient(g.size, min(j + col, x.nk - 1))], 0), g.count - 1); };
+    auto page_at = [&](int j) { return min(max(table[quotient(pages.size, min(j + row, x.nk - 1))], 0), pages.count - 1); };
     auto load = [&](int j, int page) {
-        const int key = min(j + col, x.nk - 1), within = key - quotient(g.size, key) * (int)g.size.d;
-        const long long at = page * g.page_ld + within * g.place_ld;
-        sc = sbase[page * g.scale_page_ld + within];
+        const int key = min(j + row, x.nk - 1), within = key - quotient(pages.size, key) * (int)pages.size.d;
+        const long long at = page * pages.page_ld + within * pages.place_ld;
+        sc = sbase[page * pages.scale_page_ld + within];
 #pragma unroll
         for (int i = 0; i < L::kPasses; ++i) {
             const long long from = shuffled(at, i * L::kPerPass + load_row);
@@ -270,33 +275,62 @@ __global__ void __launch_bounds__(256, 2) attention_cache_kernel(const CacheArgs
             }
         }
     };
-
-    f32x16 o[Q::kCols];
-#pragma unroll
-    for (int d = 0; d < Q::kCols; ++d)
-        o[d] = f32x16{};
-    float m = -INFINITY, mc = 0.0f, l = 0.0f;
-    const float c = a.cap > 0.0f ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e, cap = a.cap * kLog2e;
     constexpr int kStride = kKeys * kWaves;
     int j = begin + wave * kKeys, page = 0;
-    if (j < end) {
+    if (j < end) {                                         // a step is loaded ahead, the pages of the one behind it too
         load(j, page_at(j));
         page = page_at(j + kStride);
     }
+
+    int place[NT], seen[NT];
+    float slope[NT];
+    unsigned long long tree[NT];
+    s16x8 q[NT][kSteps];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = first + n * 16 + col, at = min(r, rows - 1);
+        place[n] = quotient(a.by_group, at);
+        const int head = kvh * a.group + at - place[n] * a.group;
+        seen[n] = seen_by(place[n]);
+        tree[n] = a.tree ? (unsigned long long)a.tree[x.q0 + place[n]] : 0;
+        slope[n] = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+        const T *from = row_of<const T>(a.q, x.q0 + place[n], head);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            q[n][i] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            if (r < rows && i * 32 + g * 8 < a.dim)
+                q[n][i] = *reinterpret_cast<const s16x8 *>(from + i * 32 + g * 8);
+        }
+    }
+    if (a.dim < DP) {                                      // zeros behind dim
+        for (int i = lane * 16; i < 2 * kKeys * L::kPitch; i += 1024)
+            *reinterpret_cast<uint4 *>(kt + i) = make_uint4(0, 0, 0, 0);
+    }
+
+    f32x4 o[NT][kDims];
+    float m[NT], mc[NT], l[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = -INFINITY, mc[n] = 0.0f, l[n] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+            o[n][d] = f32x4{};
+    }
+    const float c = a.cap > 0.0f ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e, cap = a.cap * kLog2e;
     for (; j < end; j += kStride) {
         const bool masked = j + kKeys > seen_lo;
         // the tiles that were loaded, to LDS
-        if (h == 0) {
-            kscale[col] = sc * c;
+        if (lane < 32) {
+            kscale[row] = sc * c;
         } else {
-            vscale[col] = sc;
-            vlog[col] = __builtin_amdgcn_logf(fmaxf(sc, 0x1p-90f));
+            vscale[row] = sc;
+            vlog[row] = __builtin_amdgcn_logf(fmaxf(sc, 0x1p-90f));
         }
         if (loads)
 #pragma unroll
             for (int i = 0; i < L::kPasses; ++i) {
-                const int row = i * L::kPerPass + load_row;
-                *reinterpret_cast<typename L::Part *>(kt + row * L::kPitch + load_at) = kp[i];
+                const int to = i * L::kPerPass + load_row;
+                *reinterpret_cast<typename L::Part *>(kt + to * L::kPitch + load_at) = kp[i];
                 if (masked) {              // bytes that are no number would reach rows that do not see them: their row's scale says it instead
                     unsigned any = 0;
 #pragma unroll
@@ -306,9 +340,9 @@ __global__ void __launch_bounds__(256, 2) attention_cache_kernel(const CacheArgs
                         any |= bad;
                     }
                     if (any)
-                        vscale[row] = NAN;
+                        vscale[to] = NAN;
                 }
-                *reinterpret_cast<typename L::Part *>(vt + row * L::kPitch + load_at) = vp[i];
+                *reinterpret_cast<typename L::Part *>(vt + to * L::kPitch + load_at) = vp[i];
             }
         if (j + kStride < end) {
             load(j + kStride, page);
@@ -316,131 +350,166 @@ __global__ void __launch_bounds__(256, 2) attention_cache_kernel(const CacheArgs
         }
         wave_sees();
 
-        f32x16 p = {};
+        f32x4 p[NT][2];
 #pragma unroll
-        for (int i = 0; i < Q::kSteps; ++i)
-            p = product<T>(widened<T>(*reinterpret_cast<const uint2 *>(kt + col * L::kPitch + i * 16 + h * 8)), q[i], p);
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 s = *reinterpret_cast<const f32x4 *>(kscale + i * 8 + h * 4);
+            for (int n = 0; n < NT; ++n)
+                p[n][t] = f32x4{};
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                p[i * 4 + e] *= s[e];
-        }
-        if (a.cap > 0.0f)
+            for (int i = 0; i < kSteps; ++i) {
+                const s16x8 k = widened<T>(*reinterpret_cast<const uint2 *>(kt + (t * 16 + col) * L::kPitch + i * 32 + g * 8));
 #pragma unroll
-            for (int i = 0; i < 16; ++i)   // tanh(y) = 1 - 2 / (exp(2 y) + 1)
-                p[i] = fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(p[i]) + 1.0f), cap);
-        if (a.slopes) {
-            const float far = (float)(j + 4 * h - (place + x.nk - x.nq));
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                p[i] = fmaf(-slope, fabsf(far + (float)(8 * (i / 4) + i % 4)), p[i]);
-        }
-        if (masked) {
-            const int left = seen - j - 4 * h, drafted = j + 4 * h - before;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int k = 8 * (i / 4) + i % 4, bit = drafted + k;
-                bool sees = k < left;
-                if (a.tree && bit >= 0)
-                    sees = sees && bit < 64 && (tree >> (bit & 63) & 1);
-                if (!sees)
-                    p[i] = -INFINITY;
+                for (int n = 0; n < NT; ++n)
+                    p[n][t] = product16<T>(k, q[n][i], p[n][t]);
             }
         }
-        float s[16];                       // what the maximum is taken of
+        f32x4 ks[2], vs[2], vl[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(vlog + i * 8 + h * 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                s[i * 4 + e] = p[i * 4 + e] + v[e];
+        for (int t = 0; t < 2; ++t) {
+            ks[t] = *reinterpret_cast<const f32x4 *>(kscale + t * 16 + g * 4);
+            vs[t] = *reinterpret_cast<const f32x4 *>(vscale + t * 16 + g * 4);
+            vl[t] = *reinterpret_cast<const f32x4 *>(vlog + t * 16 + g * 4);
         }
-        float top = s[0];
+        float top[NT];
+        bool moves = false;
 #pragma unroll
-        for (int i = 1; i < 16; ++i)
-            top = fmaxf(top, s[i]);
-        follow_max<W, Q::kCols>(both_max(top), 1.0f, m, mc, l, o);
-        float w[16];
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(vscale + i * 8 + h * 4);
+            for (int t = 0; t < 2; ++t)
+                p[n][t] *= ks[t];
+            if (a.cap > 0.0f)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float weight = __builtin_amdgcn_exp2f(p[i * 4 + e] - mc);
-                l += weight;
-                w[i * 4 + e] = weight * v[e];
-                if (masked && p[i * 4 + e] == -INFINITY)
-                    w[i * 4 + e] = 0.0f;   // (its scale may be no number)
+                for (int i = 0; i < 8; ++i)    // tanh(y) = 1 - 2 / (exp(2 y) + 1)
+                    p[n][i / 4][i % 4] = fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(p[n][i / 4][i % 4]) + 1.0f), cap);
+            if (a.slopes) {
+                const float far = (float)(j + 4 * g - (place[n] + before));
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    p[n][i / 4][i % 4] = fmaf(-slope[n], fabsf(far + (float)(i / 4 * 16 + i % 4)), p[n][i / 4][i % 4]);
+            }
+            if (masked) {
+                const int left = seen[n] - j - 4 * g, drafted = j + 4 * g - before;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int k = i / 4 * 16 + i % 4, bit = drafted + k;
+                    bool sees = k < left;
+                    if (a.tree && bit >= 0)
+                        sees = sees && bit < 64 && (tree[n] >> (bit & 63) & 1);
+                    if (!sees)
+                        p[n][i / 4][i % 4] = -INFINITY;
+                }
+            }
+            top[n] = p[n][0][0] + vl[0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i)
+                top[n] = fmaxf(top[n], p[n][i / 4][i % 4] + vl[i / 4][i % 4]);
+            top[n] = column_max(top[n]);
+            moves = moves || top[n] - m[n] > (float)kSlack<W>;
+        }
+        if (__any(moves)) {                                // see follow_max
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float next = fmaxf(m[n], top[n]), to = (next == -INFINITY ? 0.0f : next) - (float)kLift<W>;
+                const float f = m[n] == -INFINITY ? 0.0f : exp2f(mc[n] - to);
+                m[n] = next;
+                mc[n] = to;
+                l[n] *= f;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d)
+                    o[n][d] *= f;
             }
         }
+        s16x8 b[NT];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const s16x8 b = rounded<W>(w + 8 * u);
+        for (int n = 0; n < NT; ++n) {
+            float w[8];
 #pragma unroll
-            for (int d = 0; d < Q::kCols; ++d) {
-                // eight keys of one dim, in the order that the weights lie in (attention_tiles.h)
-                using P = __attribute__((address_space(3))) i32x2 *;
-                const int i = lane & 15, key = u * 16 + h * 4 + (i >> 1) % 4 + (i >> 3) * 8;
-                const auto v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((P)(vt + key * L::kPitch + d * 32 + ((lane >> 4) & 1) * 16 + (i & 1) * 8));
-                o[d] = product<W>(widened<W>(make_uint2(v[0], v[1])), b, o[d]);
+            for (int i = 0; i < 8; ++i) {
+                const float weight = __builtin_amdgcn_exp2f(p[n][i / 4][i % 4] - mc[n]);
+                l[n] += weight;
+                w[i] = weight * vs[i / 4][i % 4];
+                if (masked && p[n][i / 4][i % 4] == -INFINITY)
+                    w[i] = 0.0f;           // (its scale may be no number)
             }
+            b[n] = rounded<W>(w);
+        }
+        const int i8 = col >> 1, key = g * 4 + (i8 & 3) + (i8 >> 2) * 16;          // this lane's part of the transposing load
+        const char *const from = vt + key * L::kPitch + (col & 1) * 8;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            const auto v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(from + d * 16));
+            const s16x8 w = widened<W>(make_uint2(v[0], v[1]));
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                o[n][d] = product16<W>(w, b[n], o[n][d]);
         }
         wave_sees();
     }
 
     // the four waves' sums
-    l = both_sum(l);
-    if (h == 0) {
-        stats[wave][0][col] = l == 0.0f ? -INFINITY : m;   // (nothing seen: a sum of 0)
-        stats[wave][1][col] = l;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        l[n] = column_sum(l[n]);
+        if (g == 0) {
+            stats[wave][0][n * 16 + col] = l[n] == 0.0f ? -INFINITY : m[n];        // (nothing seen: a sum of 0)
+            stats[wave][1][n * 16 + col] = l[n];
+        }
     }
     __syncthreads();
-    float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i)
-        top = fmaxf(top, stats[i][0][col]);
+    for (int n = 0; n < NT; ++n) {
+        const int at = n * 16 + col, r = first + at;
+        float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i)
-        sum += stats[i][1][col] == 0.0f ? 0.0f : stats[i][1][col] * exp2f(stats[i][0][col] - top);
-    const float mine = l == 0.0f ? 0.0f : exp2f(m - top);
-    const float f = a.splits > 1 ? mine : sum > 0.0f ? mine / sum : sum == 0.0f ? 0.0f : NAN;
-    if (in && wave == 0 && h == 0) {
-        const long long row = (x.q0 + place) * a.heads + head;
-        if (a.splits > 1) {
-            float *stat = a.parts + a.q_tokens * a.heads * a.splits * a.dim;
-            stat[row * a.splits + split] = top;
-            stat[(a.q_tokens * a.heads + row) * a.splits + split] = sum;
-        } else if (a.lse) {
-            a.lse[row] = sum == 0.0f ? -INFINITY : fmaf(top, 1.0f / kLog2e, log_of<_Float16>(sum));
+        for (int i = 0; i < kWaves; ++i)
+            top = fmaxf(top, stats[i][0][at]);
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i)
+            sum += stats[i][1][at] == 0.0f ? 0.0f : stats[i][1][at] * exp2f(stats[i][0][at] - top);
+        const float mine = l[n] == 0.0f ? 0.0f : exp2f(m[n] - top);
+        const float f = a.splits > 1 ? mine : sum > 0.0f ? mine / sum : sum == 0.0f ? 0.0f : NAN;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+            o[n][d] *= f;
+        if (r < rows && wave == 0 && g == 0) {
+            const long long to = (x.q0 + place[n]) * a.heads + kvh * a.group + r - place[n] * a.group;
+            if (a.splits > 1) {
+                float *stat = a.parts + a.q_tokens * a.heads * a.splits * a.dim;
+                stat[to * a.splits + split] = top;
+                stat[(a.q_tokens * a.heads + to) * a.splits + split] = sum;
+            } else if (a.lse) {
+                a.lse[to] = sum == 0.0f ? -INFINITY : fmaf(top, 1.0f / kLog2e, log_of<W>(sum));
+            }
         }
     }
     float *const join = reinterpret_cast<float *>(lds);
-    const int jc = threadIdx.x >> 3, jd = (threadIdx.x & 7) * 4, jr = first + jc;
+    const int jc = threadIdx.x / (kJoinDims / 4), jd = threadIdx.x % (kJoinDims / 4) * 4, jr = first + jc;
 #pragma unroll
-    for (int d = 0; d < Q::kCols; ++d) {
-        if (d * 32 >= a.dim)
+    for (int d0 = 0; d0 < DP; d0 += kJoinDims) {
+        if (d0 >= a.dim)
             break;
-        if (d > 0)
+        if (d0 > 0)
             __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4 *>(join + (wave * 32 + col) * kJoinPitch + i * 8 + h * 4) =
-                f32x4{o[d][i * 4] * f, o[d][i * 4 + 1] * f, o[d][i * 4 + 2] * f, o[d][i * 4 + 3] * f};
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int d = 0; d < kJoinDims / 16; ++d)
+                if (d0 / 16 + d < kDims)
+                    *reinterpret_cast<f32x4 *>(join + (wave * ROWS + n * 16 + col) * kJoinPitch + d * 16 + g * 4) = o[n][d0 / 16 + d < kDims ? d0 / 16 + d : 0];
         __syncthreads();
-        if (jr >= rows || d * 32 + jd >= a.dim)
+        if (jr >= rows || d0 + jd >= a.dim)
             continue;
         f32x4 v = *reinterpret_cast<const f32x4 *>(join + jc * kJoinPitch + jd);
 #pragma unroll
         for (int i = 1; i < kWaves; ++i)
-            v += *reinterpret_cast<const f32x4 *>(join + (i * 32 + jc) * kJoinPitch + jd);
+            v += *reinterpret_cast<const f32x4 *>(join + (i * ROWS + jc) * kJoinPitch + jd);
         const int jp = quotient(a.by_group, jr), jh = kvh * a.group + jr - jp * a.group;
         if (a.splits > 1) {
-            *reinterpret_cast<f32x4 *>(a.parts + (((x.q0 + jp) * a.heads + jh) * a.splits + split) * a.dim + d * 32 + jd) = v;
+            *reinterpret_cast<f32x4 *>(a.parts + (((x.q0 + jp) * a.heads + jh) * a.splits + split) * a.dim + d0 + jd) = v;
         } else {
             typedef T t4 __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<t4 *>(row_of<T>(a.out, x.q0 + jp, jh) + d * 32 + jd) = t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+            *reinterpret_cast<t4 *>(row_of<T>(a.out, x.q0 + jp, jh) + d0 + jd) = t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
         }
     }
 }
@@ -450,12 +519,12 @@ template <typename T>
 __global__ void __launch_bounds__(256) attention_cache_join_kernel(const CacheArgs a)
 {
     const int kvh = blockIdx.x % a.kv_heads;
-    const Work work = tile_at<false>(a, kRows, blockIdx.x / a.kv_heads);
+    const Work work = tile_at<false>(a, a.tile, blockIdx.x / a.kv_heads);
     if (!work.any)
         return;
     const Seq &x = work.x;
     const int lane = threadIdx.x & 63, r = work.first + blockIdx.y * 4 + (threadIdx.x >> 6);
-    if (r >= x.nq * a.group || r >= work.first + kRows)
+    if (r >= x.nq * a.group || r >= work.first + a.tile)
         return;
     const int place = quotient(a.by_group, r), head = kvh * a.group + r - place * a.group;
     const long long row = (x.q0 + place) * a.heads + head;
@@ -595,6 +664,17 @@ int write_impl(const fuse_cache *f, const void *k, int64_t k_token_ld, int64_t k
     return launched("cache_write_kernel");
 }
 
+// Rows of a block: sixteen where that is what a sequence has, on average.
+int tile_of(const fuse_cache *f, const fuse_cache_query *q)
+{
+    return f->tokens * (q->heads / f->kv_heads) <= 16 * f->seqs ? 16 : 32;
+}
+
+long long tiles_of(const fuse_cache *f, const fuse_cache_query *q)
+{
+    return first_tile(f->tokens * (q->heads / f->kv_heads), (int)f->seqs, tile_of(f, q));
+}
+
 int check_read(const fuse_cache *f, const fuse_cache_query *q)
 {
     int rc = check_cache(f);
@@ -614,17 +694,20 @@ int check_read(const fuse_cache *f, const fuse_cache_query *q)
         return report(FUSE_EINVAL, "a tree goes with causal, and without slopes");
     if (reinterpret_cast<uintptr_t>(q->slopes) % 4 || reinterpret_cast<uintptr_t>(q->tree) % 8)
         return report(FUSE_EINVAL, "slopes or tree are not aligned to their type");
-    if (f->tokens * q->heads >= (INT64_C(1) << 36) || first_tile(f->tokens * (q->heads / f->kv_heads), (int)f->seqs, kRows) * f->kv_heads >= (1 << 24))
+    if (f->tokens * q->heads >= (INT64_C(1) << 36) || tiles_of(f, q) * f->kv_heads >= (1 << 24))
         return report(FUSE_EUNSUPPORTED, "more tiles of queries than one launch has blocks");
     return check_rows16("q", q->q, f->tokens, q->q_token_ld, q->q_head_ld, q->heads, f->dim);
 }
 
-long long tiles_of(const fuse_cache *f, const fuse_cache_query *q) { return first_tile(f->tokens * (q->heads / f->kv_heads), (int)f->seqs, kRows); }
-
+// Splits of the keys: as many as it takes to have three blocks for each of 256 compute units, of at least four steps of all waves each where
+// all sequences fill their room, or eight blocks of at least eight steps.  A split costs a block's beginning and end, some five steps, and the
+// launch that joins them.  32 heads over 8, dim 128: 32 tokens over 16384 places each (filled to two thirds, as below) take 226, 162, 155 and 148
+// us with 512, 768, 1024 and 2048 blocks for a goal; 16 over 2048: 22, 21, 21, 21; four times 40 over 4096: 34, 33, 34, 40; one over
+// 32768: 22 us with splits of four steps, 20 with eight; one of 8 heads over 700: 9 us with two splits, 7 without.
 int splits_of(const fuse_cache *f, const fuse_cache_query *q)
 {
-    const long long blocks = tiles_of(f, q) * f->kv_heads, room = f->table_width * f->page_size;
-    const long long n = std::min(blocks > 0 ? 1024 / blocks : 1, room / (2 * kKeys * kWaves));
+    const long long blocks = std::max(1LL, tiles_of(f, q) * f->kv_heads), room = f->table_width * f->page_size, step = kKeys * kWaves;
+    const long long n = std::max(std::min(2048 / blocks, room / (8 * step)), std::min(768 / blocks, room / (4 * step)));
     return (int)std::max(1LL, std::min<long long>(n, kMaxSplits));
 }
 
@@ -634,15 +717,15 @@ size_t read_bytes(const fuse_cache *f, const fuse_cache_query *q)
     return splits > 1 ? (size_t)f->tokens * q->heads * splits * (f->dim + 2) * sizeof(float) : 0;
 }
 
-template <typename T, int CHUNK>
+template <typename T, int CHUNK, int ROWS>
 void launch_dim(const CacheArgs &a, unsigned blocks, hipStream_t s)
 {
     if (a.dim <= 64)
-        attention_cache_kernel<T, 64, CHUNK><<<blocks, 256, 0, s>>>(a);
+        attention_cache_kernel<T, 64, CHUNK, ROWS><<<blocks, 256, 0, s>>>(a);
     else if (a.dim <= 96)
-        attention_cache_kernel<T, 96, CHUNK><<<blocks, 256, 0, s>>>(a);
+        attention_cache_kernel<T, 96, CHUNK, ROWS><<<blocks, 256, 0, s>>>(a);
     else
-        attention_cache_kernel<T, 128, CHUNK><<<blocks, 256, 0, s>>>(a);
+        attention_cache_kernel<T, 128, CHUNK, ROWS><<<blocks, 256, 0, s>>>(a);
 }
 
 template <typename T>
@@ -650,14 +733,19 @@ int launch_read(const CacheArgs &a, unsigned tiles, hipStream_t s)
 {
     const Pages &g = a.pages;
     const bool wide = a.dim % 16 == 0 && on_16_bytes(g.k) && on_16_bytes(g.v) && g.page_ld % 16 == 0 && g.head_ld % 16 == 0 && g.place_ld % 16 == 0;
-    if (wide)
-        launch_dim<T, 16>(a, tiles * a.kv_heads * a.splits, s);
+    const unsigned blocks = tiles * a.kv_heads * a.splits;
+    if (wide && a.tile == 16)
+        launch_dim<T, 16, 16>(a, blocks, s);
+    else if (wide)
+        launch_dim<T, 16, 32>(a, blocks, s);
+    else if (a.tile == 16)
+        launch_dim<T, 8, 16>(a, blocks, s);
     else
-        launch_dim<T, 8>(a, tiles * a.kv_heads * a.splits, s);
+        launch_dim<T, 8, 32>(a, blocks, s);
     int rc = launched("attention_cache_kernel");
     if (rc || a.splits == 1)
         return rc;
-    attention_cache_join_kernel<T><<<dim3(tiles * a.kv_heads, kRows / 4), 256, 0, s>>>(a);
+    attention_cache_join_kernel<T><<<dim3(tiles * a.kv_heads, a.tile / 4), 256, 0, s>>>(a);
     rc = launched("attention_cache_join_kernel");
     if (!rc)
         set_last_kernel("attention_cache_kernel");
@@ -686,7 +774,7 @@ int read_impl(const fuse_cache *f, const fuse_cache_query *q, void *out, int64_t
     a.lse = lse, a.parts = static_cast<float *>(workspace);
     a.heads = q->heads, a.group = q->heads / f->kv_heads, a.by_group = divider((unsigned)a.group);
     a.causal = q->causal != 0, a.scale = (float)q->scale, a.cap = (float)q->cap, a.slopes = q->slopes;
-    a.tree = reinterpret_cast<const long long *>(q->tree), a.splits = splits_of(f, q);
+    a.tree = reinterpret_cast<const long long *>(q->tree), a.splits = splits_of(f, q), a.tile = tile_of(f, q);
     const unsigned tiles = (unsigned)tiles_of(f, q);
     return f->dtype == FUSE_BF16 ? launch_read<__bf16>(a, tiles, (hipStream_t)stream) : launch_read<_Float16>(a, tiles, (hipStream_t)stream);
 }
