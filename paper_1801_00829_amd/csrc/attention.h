@@ -221,29 +221,34 @@ __device__ __forceinline__ int first_that_sees(const AttnArgs &a, const Seq &x, 
 
 // Scores of the matrix units, to base 2, as they go into the softmax (kScored).
 //
-// tanh(y) = 1 - 2 r with r = 1 / (exp(2 y) + 1): off by some 2^-23 whatever y, which is that part of the cap in a score.
+// tanh(y) = 1 - 2 r with r = 1 / (exp(2 y) + 1): off by some 2^-23 whatever y, which is that part of the cap in a score.  A capped score is
+// cap - 2 cap r; what it has in common with all others of its row goes where the row's own constant goes.  Its derivative is 4 (r - r^2), of
+// which the 4 goes to the end of the sums.
 template <int SHAPE>
 struct Scores {
-    float mul, cap;
+    float mul, cap;                        // cap: 0 without one
 
     __device__ __forceinline__ explicit Scores(const AttnArgs &a)
     {
         constexpr float log2e = 1.44269504088896340736f;
         mul = SHAPE & kCapped ? 2.0f * log2e * a.scale / a.cap : a.scale * log2e;
-        cap = a.cap * log2e;
+        cap = SHAPE & kCapped ? a.cap * log2e : 0.0f;
     }
-    // `far`: distance of query and key; `d`: the score's derivative by scale q k
-    __device__ __forceinline__ float of(float p, float far, float slope, float &d) const
+    __device__ __forceinline__ float turned(float p) const { return __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(p * mul) + 1.0f); }
+    // The score plus `from` less cap.  `far`: distance of query and key; `d`: the derivative by scale q k, times kSlope
+    __device__ __forceinline__ float of(float p, float from, float far, float slope, float &d) const
     {
-        p *= mul;
         d = 1.0f;
         if (SHAPE & kCapped) {
-            const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(p) + 1.0f);
-            p = fmaf(-2.0f * cap, r, cap);
-            d = 4.0f * fmaf(-r, r, r);
+            const float r = turned(p);
+            p = fmaf(-2.0f * cap, r, from);
+            d = fmaf(-r, r, r);
+        } else {
+            p = fmaf(p, mul, from);
         }
         return SHAPE & kSloped ? fmaf(-slope, fabsf(far), p) : p;
     }
+    static constexpr float kSlope = SHAPE & kCapped ? 0.25f : 1.0f;
 };
 
 template <typename T>

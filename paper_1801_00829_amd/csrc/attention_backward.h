@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
         lse2 = a.lse[(x.q0 + place) * a.heads + head] * kLog2e;
         if (h == 0) {
             a.delta[at] = delta;
-            a.lse2[at] = kLifted<T> ? lse2 - kLiftP : lse2;
+            a.lse2[at] = (kLifted<T> ? lse2 - kLiftP : lse2) - scores.cap;
             if (SHAPE & kSloped) {
                 a.row_place[at] = place + x.nk - x.nq;
                 a.row_slope[at] = slope;
@@ -169,8 +169,8 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             float d;
-                            w[i] = scores.of(p[i], far + (float)(8 * (i / 4) + i % 4), slope, d) + from;
-                            w[i] = __builtin_amdgcn_exp2f(w[i]) * ((dp[i] - delta) * d);
+                            const float x = scores.of(p[i], from + scores.cap, far + (float)(8 * (i / 4) + i % 4), slope, d);
+                            w[i] = __builtin_amdgcn_exp2f(x) * ((dp[i] - delta) * d);
                         }
                     } else {
 #pragma unroll
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
         sum_up(std::true_type());
 
     if (in)
-        write_columns<T>(o, kLifted<T> ? ldexpf(a.scale, -lift) : a.scale, row_of<T>(a.dq, x.q0 + place, head), h, a.dim);
+        write_columns<T>(o, (kLifted<T> ? ldexpf(a.scale, -lift) : a.scale) / Scores<SHAPE>::kSlope, row_of<T>(a.dq, x.q0 + place, head), h, a.dim);
     if (kLifted<T> && first + wave * 32 < rows) {
 #pragma unroll
         for (int i = 16; i > 0; i >>= 1)
@@ -347,9 +347,9 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
                 ahead<L::kSteps * 2, 6>();
                 float w[16], ds[16];
                 if (kScored<SHAPE>) {
-                    // With slopes all that is kept of the rows is asked for only here: there are no registers to keep it in meanwhile (8192 packed
-                    // tokens, 32 heads over 8, dim 128, whole backward pass: 1044 us, 1091 with lse and delta asked for above as without slopes;
-                    // plain scores 845, with a cap 973, 1013 if they too are asked for here).
+                    // With slopes all that is kept of the rows is asked for only here: there are no registers to keep it in meanwhile.  Whole backward
+                    // passes over 8192 packed tokens, 32 heads over 8, dim 128: plain scores 800 us, with a cap 895, with slopes 958; with slopes
+                    // and all of it asked for above 4 % more, with a cap and lse and delta asked for here 4 % more.
                     i32x4u places[4];
                     f32x4u slopes[4];
                     if (SHAPE & kSloped)
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
                         float d, far = 0.0f, slope = 0.0f;
                         if (SHAPE & kSloped)
                             far = (float)(places[i / 4][i % 4] - key), slope = slopes[i / 4][i % 4];
-                        w[i] = __builtin_amdgcn_exp2f(scores.of(p[i], far, slope, d) - lse[i / 4][i % 4]);
+                        w[i] = __builtin_amdgcn_exp2f(scores.of(p[i], -lse[i / 4][i % 4], far, slope, d));
                         ds[i] = w[i] * ((dp[i] - delta[i / 4][i % 4]) * d);
                     }
                 } else {
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
         sum_up(std::true_type());
 
     const int d0 = half * kHalfCols * 32;
-    const float fk = kLifted<T> ? ldexpf(a.scale, -lift) : a.scale, fv = kLifted<T> ? 1.0f / (1 << kLiftP) : 1.0f;
+    const float fk = (kLifted<T> ? ldexpf(a.scale, -lift) : a.scale) / Scores<SHAPE>::kSlope, fv = kLifted<T> ? 1.0f / (1 << kLiftP) : 1.0f;
     if (in && a.splits > 1) {
         float *part = a.parts + (((x.k0 + key) * a.kv_heads + kvh) * a.splits + split) * 2 * a.dim + d0;
         write_columns<float>(dk, fk, part, h, a.dim - d0);

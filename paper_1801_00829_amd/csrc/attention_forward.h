@@ -24,6 +24,24 @@ __device__ __forceinline__ long long part_at(const AttnArgs &a, const Parts &p, 
     return (token * a.heads + head) * p.splits + split;
 }
 
+// What the scores in registers are multiplied with in the exponent, to base 2.  Capped ones are kept as -r (see Scores): the cap is taken twice, and
+// added once to what a row's scores have in common.
+template <int SHAPE> constexpr bool kCapOnly = (SHAPE & (kCapped | kSloped)) == kCapped;
+template <int SHAPE>
+__device__ __forceinline__ float factor_of(const AttnArgs &a)
+{
+    return kCapOnly<SHAPE> ? 2.0f * a.cap * kLog2e : kScored<SHAPE> ? 1.0f : a.scale * kLog2e;
+}
+
+// lse of a row, of the maximum of its scores in registers and the sum of its weights.
+template <typename T, int SHAPE>
+__device__ __forceinline__ float lse_of(const AttnArgs &a, float m, float l)
+{
+    if (kCapOnly<SHAPE>)
+        return fmaf(m, 2.0f * a.cap, a.cap + log_of<T>(l));
+    return fmaf(m, kScored<SHAPE> ? 1.0f / kLog2e : a.scale, log_of<T>(l));
+}
+
 // One block: 128 rows, 32 per wave as columns (attention_tiles.h), the keys and values that they see in steps of 64 through LDS, loaded
 // a step ahead.  One pass: running maximum and sum per column, exp(S - max), rounded, straight into the product with the values.
 //
@@ -33,6 +51,10 @@ __device__ __forceinline__ long long part_at(const AttnArgs &a, const Parts &p, 
 // and compute unit do not hide entirely behind two blocks.  Tried without gain: the next step's scores among this one's exp
 // (500 to 510 us), transposed loads with waits of their own (509), a higher priority for waves in their products (528); blocks of 256
 // rows, which read half as much, take 472 us here but lose 4 to 24 % with fewer rows, fewer blocks or a dim of 64.
+//
+// Shaped scores: 8192 packed tokens in four sequences, heads as above: plain 266 us, with a cap 287 (two more exponentials' worth per score),
+// slopes 265 (an operation each), both 313.  A polynomial for scores within half the cap, instead of the exponential and the division, takes
+// as long (293 us where the two took 293).
 template <typename T, int DP, int SHAPE>
 __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const AttnArgs a, const Parts parts)
 {
@@ -80,8 +102,8 @@ __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const 
 
     f32x16 o[L::kCols];
     float m, mc, l;
-    const float c = kScored<SHAPE> ? 1.0f : a.scale * kLog2e;
     const Scores<SHAPE> scores(a);
+    const float c = factor_of<SHAPE>(a);
     const float slope = SHAPE & kSloped ? a.slopes[head] * kLog2e : 0.0f;
 
     const T *kbase = row_of<const T>(a.k, x.k0, kvh), *vbase = row_of<const T>(a.v, x.k0, kvh);
@@ -120,7 +142,8 @@ __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const 
                     float d;
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        p[i / 16][i % 16] = scores.of(p[i / 16][i % 16], far + (float)(i / 16 * 32 + 8 * (i % 16 / 4) + i % 4), slope, d);
+                        p[i / 16][i % 16] = kCapOnly<SHAPE> ? -scores.turned(p[i / 16][i % 16])
+                                                            : scores.of(p[i / 16][i % 16], scores.cap, far + (float)(i / 16 * 32 + 8 * (i % 16 / 4) + i % 4), slope, d);
                 }
                 const bool masked = j + kKeys > seen_lo;
                 if (masked) {
@@ -200,12 +223,12 @@ __global__ void __launch_bounds__(256, DP == 64 ? 3 : 2) attention_kernel(const 
     if (in) {
         write_columns<T>(o, f, row_of<T>(a.out, x.q0 + place, head), h, a.dim);
         if (a.lse && h == 0)
-            a.lse[(x.q0 + place) * a.heads + head] = l == 0.0f ? -INFINITY : fmaf(m, kScored<SHAPE> ? 1.0f / kLog2e : a.scale, log_of<T>(l));
+            a.lse[(x.q0 + place) * a.heads + head] = l == 0.0f ? -INFINITY : lse_of<T, SHAPE>(a, m, l);
     }
 }
 
 // Joins the splits of every row: a wave per row.  6 to 7 us, most of it the launch.
-template <typename T>
+template <typename T, int SHAPE>
 __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, const Parts parts)
 {
     const int kvh = blockIdx.x % a.kv_heads;
@@ -221,7 +244,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
 #pragma unroll
         for (int i = 32; i > 0; i >>= 1)
             top = fmaxf(top, __shfl_xor(top, i, 64));
-        const float w = l == 0.0f ? 0.0f : exp2f((m - top) * (a.scale * kLog2e));
+        const float w = l == 0.0f ? 0.0f : exp2f((m - top) * factor_of<SHAPE>(a));
         const float sum = wave_sum(w * l);
         float o0 = 0.0f, o1 = 0.0f;
         // eight splits' loads in flight, without a branch around them: one by one, 64 splits took 35 us
@@ -250,7 +273,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, c
         if (lane + 64 < a.dim)
             out[lane + 64] = (T)(o1 * f);
         if (a.lse && lane == 0)
-            a.lse[(x.q0 + place) * a.heads + head] = sum == 0.0f ? -INFINITY : fmaf(top, a.scale, log_of<T>(sum));
+            a.lse[(x.q0 + place) * a.heads + head] = sum == 0.0f ? -INFINITY : lse_of<T, SHAPE>(a, top, sum);
     }
 }
 
@@ -267,10 +290,7 @@ int launch(const AttnArgs &a, const Parts &p, unsigned tiles, hipStream_t s)
     int rc = launched("attention_kernel");
     if (rc || p.splits == 1)
         return rc;
-    AttnArgs join = a;
-    if (kScored<SHAPE>)
-        join.scale = 1.0f / kLog2e;        // (maxima are in base 2 already)
-    attention_join_kernel<T><<<dim3(tiles * a.kv_heads, kJoinBlocks), 256, 0, s>>>(join, p);
+    attention_join_kernel<T, SHAPE><<<dim3(tiles * a.kv_heads, kJoinBlocks), 256, 0, s>>>(a, p);
     rc = launched("attention_join_kernel");
     if (!rc)
         set_last_kernel("attention_kernel");
