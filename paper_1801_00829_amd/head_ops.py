@@ -6,7 +6,7 @@ import torch
 
 from . import _lib as L
 from .api import _check
-from .block_ops import DTYPE, _cap, _dtype, _heads_of, _like, _places, _row, _run, _vector, _workspace
+from .block_ops import DTYPE, _cap, _dtype, _heads_of, _places, _row, _run, _vector, _workspace
 
 PAIRS = {"halves": 0, "neighbours": 1}
 
@@ -28,7 +28,7 @@ _ROTARY_GRADS = struct.Struct("@PPqqqqPPqqqqPP")
 def _weight(t, like, dim, what):
     if t is None:
         return 0
-    if t.dtype is like.dtype and t.device == like.device and t.shape == (dim,) and (t.stride(0) == 1 or dim == 1):
+    if t.dtype is like.dtype and t.get_device() == like.get_device() and t.shape == (dim,) and (t.stride(0) == 1 or dim == 1):
         return t.data_ptr()
     return _vector(t, like, dim, what)
 
@@ -38,7 +38,7 @@ def _rotary(q, k, positions, freqs, q_weight, k_weight, sections, pairs, eps, wh
     dtype = DTYPE.get(q.dtype) if isinstance(q, torch.Tensor) else None
     if dtype is None:
         _dtype(q, what)
-    shape, device = q.shape, q.device
+    shape = q.shape
     if len(shape) != 3 or shape[1] < 1 or shape[2] < 1:
         raise ValueError("%s must be (tokens, heads, dim)" % what)
     tokens, heads, dim = shape
@@ -56,8 +56,8 @@ def _rotary(q, k, positions, freqs, q_weight, k_weight, sections, pairs, eps, wh
         raise TypeError("positions must be an int32 or int64 tensor")
     if not isinstance(freqs, torch.Tensor) or freqs.dtype is not torch.float64:
         raise TypeError("freqs must be a float64 tensor")
-    if positions.device != device or freqs.device != device:
-        raise ValueError("positions are on %s and freqs on %s, not on %s" % (positions.device, freqs.device, device))
+    if not positions.get_device() == freqs.get_device() == q.get_device():
+        raise ValueError("positions are on %s and freqs on %s, not on %s" % (positions.device, freqs.device, q.device))
     if freqs.dim() != 1 or not freqs.is_contiguous():
         raise ValueError("freqs must be a contiguous vector of a value per pair")
     half, at = freqs.numel(), positions.shape
@@ -87,13 +87,22 @@ def _rotary(q, k, positions, freqs, q_weight, k_weight, sections, pairs, eps, wh
 _NONE = (0, 0, 0)
 
 
+def _at(t, like, what, tokens, heads):
+    """_heads_of, in short where a tensor is as it should be."""
+    if isinstance(t, torch.Tensor) and t.dtype is like.dtype and t.get_device() == like.get_device():
+        shape, (token, head, step) = t.shape, t.stride() if t.dim() == 3 else (0, 0, 0)
+        if step == 1 and shape[0] == tokens > 1 and shape[1] == heads > 1 and shape[2] == like.shape[2]:
+            return t.data_ptr(), token, head
+    return _heads_of(t, like, what, tokens, heads)
+
+
 def _result(t, like, what):
     """A result of like's shape to write to, and its place."""
     if t is None:
         _, heads, dim = like.shape
         t = torch.empty_like(like, memory_format=torch.contiguous_format)
         return t, (t.data_ptr(), heads * dim, dim)
-    return t, _heads_of(t, like, what, *like.shape[:2])
+    return t, _at(t, like, what, *like.shape[:2])
 
 
 def _pointer(t):
@@ -109,7 +118,8 @@ def fuse_qk_rotary(q, k, positions, freqs, q_weight=None, k_weight=None, section
     every axis.  pairs: "halves" (dims i and i + number of pairs) or "neighbours" (2 i and 2 i + 1).  q_out, k_out: tensors to write to; they
     may be q and k themselves."""
     pack = _rotary(q, k, positions, freqs, q_weight, k_weight, sections, pairs, eps, "q")
-    f = pack(_heads_of(q, q, "q"), _NONE if k is None else _heads_of(k, q, "k", q.shape[0]))
+    tokens, heads, _ = q.shape
+    f = pack(_at(q, q, "q", tokens, heads), _NONE if k is None else _at(k, q, "k", tokens, k.shape[1]))
     if k is None and k_out is not None:
         raise ValueError("k_out needs keys")
 
@@ -132,10 +142,10 @@ def fuse_qk_rotary_backward(dq_out, dk_out, q, k, positions, freqs, q_weight=Non
     if dk_out is None and dk is not None:
         raise ValueError("dk needs keys")
     tokens, heads, _ = dq_out.shape
-    at_dq = _heads_of(dq_out, dq_out, "dq_out")
-    at_dk = _NONE if dk_out is None else _heads_of(dk_out, dq_out, "dk_out", tokens)
-    f = pack(_NONE if q_weight is None else _heads_of(_like(q, dq_out, "q"), dq_out, "q", tokens, heads),
-             _NONE if k_weight is None else _heads_of(_like(k, dq_out, "k"), dq_out, "k", tokens, dk_out.shape[1]))
+    at_dq = _at(dq_out, dq_out, "dq_out", tokens, heads)
+    at_dk = _NONE if dk_out is None else _at(dk_out, dq_out, "dk_out", tokens, dk_out.shape[1])
+    f = pack(_NONE if q_weight is None else _at(q, dq_out, "q", tokens, heads),
+             _NONE if k_weight is None else _at(k, dq_out, "k", tokens, dk_out.shape[1]))
     lib = L.load()
 
     def call(handle):
@@ -166,18 +176,22 @@ _CACHE_QUERY = struct.Struct("@PqqiiddPP")
 
 def _cache(cache, x, offsets, page_table, lengths):
     """(packed descriptor, key heads) of a call with packed arrays (tokens, any, dim) like x."""
-    dtype = _dtype(x, "packed rows")
+    dtype = DTYPE.get(x.dtype) if isinstance(x, torch.Tensor) else None
+    if dtype is None:
+        _dtype(x, "packed rows")
     k, v, k_scale, v_scale = cache
-    device, shape, strides = x.device, k.shape, k.stride()
-    for t, name, want in ((k, "k", torch.float8_e4m3fn), (v, "v", torch.float8_e4m3fn), (k_scale, "k_scale", torch.float32),
-                          (v_scale, "v_scale", torch.float32)):
-        if t.dtype is not want:
-            raise TypeError("the cache's %s must be a %s tensor" % (name, want))
-        if t.device != device:
-            raise ValueError("the cache's %s is on %s, not on %s" % (name, t.device, device))
-    scales = k_scale.stride()
+    index, shape, strides = x.get_device(), k.shape, k.stride()
+    if not (k.dtype is v.dtype is torch.float8_e4m3fn and k_scale.dtype is v_scale.dtype is torch.float32 and
+            k.get_device() == v.get_device() == k_scale.get_device() == v_scale.get_device() == index):
+        for t, name, want in ((k, "k", torch.float8_e4m3fn), (v, "v", torch.float8_e4m3fn), (k_scale, "k_scale", torch.float32),
+                              (v_scale, "v_scale", torch.float32)):
+            if t.dtype is not want:
+                raise TypeError("the cache's %s must be a %s tensor" % (name, want))
+            if t.get_device() != index:
+                raise ValueError("the cache's %s is on %s, not on %s" % (name, t.device, x.device))
     if len(shape) != 4 or v.shape != shape or k_scale.shape != shape[:3] or v_scale.shape != shape[:3]:
         raise ValueError("the cache's k and v must be (pages, key heads, places per page, dim), their scales the same without dim")
+    scales = k_scale.stride()
     pages, kv_heads, page_size, dim = shape
     if dim != x.shape[2] or kv_heads < 1 or page_size < 1:
         raise ValueError("the cache has shape %s, rows have dim %d" % (tuple(shape), x.shape[2]))
@@ -187,24 +201,25 @@ def _cache(cache, x, offsets, page_table, lengths):
         raise ValueError("the cache needs unit stride along dim, and its scales along the places")
     if offsets is None or offsets.dim() != 1 or offsets.numel() < 1:
         raise ValueError("offsets must be a vector of the number of sequences + 1 values")
-    wide = offsets.dtype is torch.int64
-    if not wide and offsets.dtype is not torch.int32:
+    kind, seqs = offsets.dtype, offsets.numel() - 1
+    if kind is not torch.int32 and kind is not torch.int64:
         raise TypeError("offsets must be int32 or int64")
-    seqs = offsets.numel() - 1
-    qo = _places(offsets, offsets, device, seqs + 1, "offsets")
-    kl = _places(lengths, offsets, device, seqs, "lengths")
+    if not (lengths.dtype is kind and offsets.get_device() == lengths.get_device() == index and lengths.dim() == 1 and lengths.numel() == seqs and
+            offsets.is_contiguous() and lengths.is_contiguous()):
+        _places(offsets, offsets, x.device, seqs + 1, "offsets")
+        _places(lengths, offsets, x.device, seqs, "lengths")
     if page_table.dtype is not torch.int32:
         raise TypeError("page_table must be an int32 tensor")
-    if page_table.device != device:
-        raise ValueError("page_table is on %s, not on %s" % (page_table.device, device))
-    table = page_table.shape
-    if len(table) != 2 or table[0] != seqs or (table[1] > 1 and page_table.stride(1) != 1):
+    if page_table.get_device() != index:
+        raise ValueError("page_table is on %s, not on %s" % (page_table.device, x.device))
+    table, steps = page_table.shape, page_table.stride()
+    if len(table) != 2 or table[0] != seqs or (table[1] > 1 and steps[1] != 1):
         raise ValueError("page_table must be (%d, pages of a sequence) with unit stride along the pages" % seqs)
     # (a stride of a single page, head or place means nothing)
-    return _CACHE.pack(dtype, kv_heads, dim, wide, x.shape[0], seqs, pages, page_size, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
-                       v_scale.data_ptr(), strides[0] if pages > 1 else 0, strides[1] if kv_heads > 1 else 0, strides[2] if page_size > 1 else 0,
-                       scales[0] if pages > 1 else 0, scales[1] if kv_heads > 1 else 0, page_table.data_ptr(),
-                       page_table.stride(0) if seqs > 1 else table[1], table[1], qo, kl), kv_heads
+    return _CACHE.pack(dtype, kv_heads, dim, kind is torch.int64, x.shape[0], seqs, pages, page_size, k.data_ptr(), v.data_ptr(),
+                       k_scale.data_ptr(), v_scale.data_ptr(), strides[0] if pages > 1 else 0, strides[1] if kv_heads > 1 else 0,
+                       strides[2] if page_size > 1 else 0, scales[0] if pages > 1 else 0, scales[1] if kv_heads > 1 else 0,
+                       page_table.data_ptr(), steps[0] if seqs > 1 else table[1], table[1], offsets.data_ptr(), lengths.data_ptr()), kv_heads
 
 
 def fuse_cache_write(k, v, cache, offsets, page_table, lengths, stream=None):
@@ -216,7 +231,7 @@ def fuse_cache_write(k, v, cache, offsets, page_table, lengths, stream=None):
     if k.dim() != 3:
         raise ValueError("k must be (tokens, heads, dim)")
     f, kv_heads = _cache(cache, k, offsets, page_table, lengths)
-    at_k, at_v = _heads_of(k, k, "k", None, kv_heads), _heads_of(v, k, "v", k.shape[0], kv_heads)
+    at_k, at_v = _at(k, k, "k", k.shape[0], kv_heads), _at(v, k, "v", k.shape[0], kv_heads)
     return _run(k.device, stream, lambda handle: _check(L.load().fuse_cache_write(f, *at_k, *at_v, handle)))
 
 
@@ -235,7 +250,7 @@ def fuse_attention_cache(q, cache, offsets, page_table, lengths, causal=True, sc
     n, heads, dim = q.shape
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.device != q.device):
         raise ValueError("lse must be a contiguous float32 tensor of shape %s on %s" % ((n, heads), q.device))
-    d = _CACHE_QUERY.pack(*_heads_of(q, q, "q"), heads, 1 if causal else 0, dim ** -0.5 if scale is None else scale, _cap(cap),
+    d = _CACHE_QUERY.pack(*_at(q, q, "q", n, heads), heads, 1 if causal else 0, dim ** -0.5 if scale is None else scale, _cap(cap),
                           0 if slopes is None else _row(slopes, q, torch.float32, heads, "slopes"),
                           0 if tree is None else _row(tree, q, torch.int64, n, "tree"))
     lib = L.load()
