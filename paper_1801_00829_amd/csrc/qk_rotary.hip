@@ -522,12 +522,14 @@ void launch_any(int dtype, const RotaryArgs &a, bool vec, unsigned blocks, hipSt
     }
 }
 
-// Tokens of a block at a time: as many as it takes for the keys' rows to fill a block's lanes, but no more than leave 512 blocks.
+// Tokens of a block at a time: as many as it takes for the keys' rows to fill a block's lanes, but no more than leave 512 blocks, all with as
+// many turns.
 int per_turn_for(const fuse_rotary *f)
 {
     const int rows = 256 / lanes_for(f->dim / 2, 16 / (int)dtype_size(f->dtype)), heads = f->kv_heads > 0 ? std::min(f->heads, f->kv_heads) : f->heads;
-    const int64_t full = (rows + heads - 1) / heads, few = (f->tokens + kGradBlocks - 1) / kGradBlocks;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(full, few), kTokens));
+    const int64_t most = std::min((rows + heads - 1) / heads, kTokens);
+    const int64_t each = std::max<int64_t>(1, (f->tokens + kGradBlocks * most - 1) / (kGradBlocks * most));
+    return (int)std::max<int64_t>(1, (f->tokens + kGradBlocks * each - 1) / (kGradBlocks * each));
 }
 
 int rotary_impl(const fuse_rotary *f, void *q_out, int64_t q_token_ld, int64_t q_head_ld, void *k_out, int64_t k_token_ld, int64_t k_head_ld,
