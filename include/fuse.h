@@ -346,7 +346,8 @@ int fuse_check_csr(const fuse_csr *X, void *stream);
 
 /* --------------------------------------------------------------------------
  * Operators of a transformer block: what training and serving one needs beside the templates, of the same three
- * kinds -- the norms around a block (row-wise), attention (an outer product that is never formed) and the norm of
+ * kinds -- the norms around a block and of its heads, with rotary positions, and the rounding of keys and values for a
+ * cache in 8 bits (row-wise), attention, over 16 bit arrays or that cache (an outer product that is never formed) and the norm of
  * all gradients (a full aggregate over many inputs).  They are compiled with the library: no descriptor, no plan
  * cache, nothing to warm up.  They differ from the calls above in two points:
  *   - element types: fuse_dtype; sums, statistics and all arithmetic in between are fp64 for fp64 and fp32 for the others,

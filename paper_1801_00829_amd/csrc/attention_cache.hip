@@ -212,6 +212,11 @@ __device__ __forceinline__ float column_sum(float v) { return swapped_sum<32>(sw
 // the four waves beside each other, each with its own tiles, maxima and sums, which are joined at the end.  Values stay in 8 bits up to the
 // registers that feed the matrix units.  Scales of keys multiply the scores, those of values the weights before these are rounded.
 //
+// Bound by memory where a sequence has few rows: 32 tokens over histories of up to 16384 places, 32 heads over 8, dim 128 (695 MB) take 140 us (4.96
+// TB/s, 5.2 in the kernel; a large copy reaches 4.9); vector units are busy for a quarter of the time, matrix units for 7 %.  With products
+// of 32 columns, whose sums and queries take twice the registers (two waves per SIMD instead of three), 157 us; with two steps loaded
+// ahead 158 at two waves, at three they do not fit.  A small call's 7 to 12 us are the waits from one lookup to the next: sequence, page, keys.
+//
 // All products are taken with the kept side as columns: S = K t(Q) leaves a lane the scores of keys 4 g .. and 16 + 4 g .. of its column, which,
 // as weights, are the B operand of the next product as they lie; its A is the transposed tile of values, read in that order.
 //
