@@ -478,8 +478,8 @@ int fuse_attention_shaped_backward(const fuse_attn *attn, const fuse_attn_shape 
  *   FUSE_PAIR_HALVES     : pair i is dims i and i + number of pairs
  *   FUSE_PAIR_NEIGHBOURS : pair i is dims 2 i and 2 i + 1
  * A token has a position on each of 1 to 4 axes (text: one; images and video: height, width, time): the first sections[0] pairs turn by its
- * position on axis 0, the next sections[1] by that on axis 1, and so on.  positions: axes x tokens of int32 or int64, position_ld apart,
- * of any sign; freqs: an fp64 value per pair, in radians per position.  Angles are taken in fp64.
+ * position on axis 0, the next sections[1] by that on axis 1, and so on.  positions: axes x tokens of int32 or int64, position_ld apart
+ * (0: the same on all axes), of any sign; freqs: an fp64 value per pair, in radians per position.  Angles are taken in fp64.
  * dim even, up to 256 (FUSE_EUNSUPPORTED otherwise).  Unit stride along dim; strides between tokens and heads in elements, so parts of one
  * projection can be passed as they are.  Rows of any alignment; rows on 16 bytes and numbers of pairs (turning, and others for
  * FUSE_PAIR_HALVES) that are a multiple of 16 bytes' worth are faster.  kv_heads may be 0: no keys.  A result may be its own input, with

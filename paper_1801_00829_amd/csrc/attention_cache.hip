@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(256, ROWS == 16 ? 3 : 2) attention_cache_kerne
         const bool masked = j + kKeys > seen_lo;
         // the tiles that were loaded, to LDS
         if (lane < 32) {
-            kscale[row] = sc * c;
+            kscale[row] = sc * c > 0x1.fffffep127f ? 0x1.fffffep127f : sc * c;     // (a score of 0 stays one; NaN stays NaN)
         } else {
             vscale[row] = sc;
             vlog[row] = __builtin_amdgcn_logf(fmaxf(sc, 0x1p-90f));
@@ -797,7 +797,7 @@ int fuse_cache_write(const fuse_cache *cache, const void *k, int64_t k_token_ld,
 
 size_t fuse_attention_cache_bytes(const fuse_cache *cache, const fuse_cache_query *query)
 {
-    return check_read(cache, query) ? 0 : read_bytes(cache, query);
+    return fuse::guard_bytes([&] { return check_read(cache, query) ? 0 : read_bytes(cache, query); });
 }
 
 int fuse_attention_cache(const fuse_cache *cache, const fuse_cache_query *query, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse,

@@ -168,7 +168,7 @@ size_t fuse_attention_backward_bytes(const fuse_attn *attn)
 
 size_t fuse_attention_shaped_backward_bytes(const fuse_attn *attn, const fuse_attn_shape *shape)
 {
-    return fuse::check_attn(attn) || fuse::check_shape(attn, shape) || attn->q_tokens == 0 ? 0 : backward_bytes(attn, shape);
+    return fuse::guard_bytes([&] { return fuse::check_attn(attn) || fuse::check_shape(attn, shape) || attn->q_tokens == 0 ? 0 : backward_bytes(attn, shape); });
 }
 
 int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads, void *stream)

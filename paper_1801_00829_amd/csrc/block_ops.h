@@ -48,6 +48,14 @@ int guard(F f)
     }
 }
 
+// The same for calls that return a number of bytes: 0.
+template <typename F>
+size_t guard_bytes(F f)
+{
+    size_t n = 0;
+    return guard([&] { n = f(); return FUSE_OK; }) == FUSE_OK ? n : 0;
+}
+
 // v of another lane of the same sixteen, by the pattern CTRL (a move within the registers: no LDS latency).
 template <int CTRL>
 __device__ __forceinline__ float moved(float v)

@@ -428,8 +428,8 @@ int check_rotary(const fuse_rotary *f)
         return report(FUSE_EINVAL, "positions or freqs is NULL");
     if (reinterpret_cast<uintptr_t>(f->positions) % (f->positions_are_64 ? 8 : 4) || reinterpret_cast<uintptr_t>(f->freqs) % 8)
         return report(FUSE_EINVAL, "positions or freqs are not aligned to their type");
-    if (f->axes > 1 && (f->position_ld < f->tokens || f->position_ld > (INT64_C(1) << 40)))
-        return report(FUSE_ESHAPE, "position_ld < tokens");
+    if (f->axes > 1 && f->position_ld != 0 && (f->position_ld < f->tokens || f->position_ld > (INT64_C(1) << 40)))
+        return report(FUSE_ESHAPE, "position_ld is neither 0 nor as many as tokens");
     for (const void *p : {f->q_weight, f->k_weight})
         if (reinterpret_cast<uintptr_t>(p) % dtype_size(f->dtype))
             return report(FUSE_EINVAL, "a weight is not aligned to its type");
@@ -643,7 +643,7 @@ int fuse_qk_rotary(const fuse_rotary *rotary, void *q_out, int64_t q_token_ld, i
 
 size_t fuse_qk_rotary_backward_bytes(const fuse_rotary *rotary)
 {
-    return check_rotary(rotary) || (!rotary->q_weight && !rotary->k_weight) ? 0 : grad_bytes(rotary);
+    return fuse::guard_bytes([&] { return check_rotary(rotary) || (!rotary->q_weight && !rotary->k_weight) ? 0 : grad_bytes(rotary); });
 }
 
 int fuse_qk_rotary_backward(const fuse_rotary *rotary, const fuse_rotary_grads *grads, void *workspace, size_t workspace_bytes, void *stream)

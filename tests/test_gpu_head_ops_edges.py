@@ -68,6 +68,14 @@ def test_qk_rotary_turns_as_it_says():
     R.within(out[:, 0], want, torch.full_like(want, 1e-6), "axes")
 
 
+def test_qk_rotary_same_positions_on_all_axes():
+    c = rotary_case(45, "bf16", 30, 4, 2, 64, (10, 12, 10), "halves", True)
+    at = c["positions"][1].clone()
+    want = F.fuse_qk_rotary(c["q"], c["k"], at, c["freqs"], q_weight=c["q_weight"], k_weight=c["k_weight"])
+    got = F.fuse_qk_rotary(c["q"], c["k"], at.expand(3, 30), c["freqs"], **rotary_args(c))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_qk_rotary_gradient_against_differences():
     c = rotary_case(42, "fp64", 5, 3, 2, 24, (4, 5), "neighbours", True)
     got = F.fuse_qk_rotary_backward(c["dq_out"], c["dk_out"], c["q"], c["k"], c["positions"], c["freqs"], eps=0.1, **rotary_args(c))
@@ -291,6 +299,18 @@ def test_cache_scales_far_apart(dtype):
     R.within(lse, H.cache_attention(c)[1], H.cache_attention(c)[3], "lse")
     c["cache"].v_scale.fill_(2.0 ** -100 / 448.0)
     check_cache_attention(c)
+
+
+def test_cache_of_keys_beyond_the_scores_range():
+    """Scales of keys that no score holds: infinities where they are met, and 0 for a query of zeros."""
+    c = cache_case(65, "bf16", 2, 1, 64, 16, [2], [50])
+    c["q"][:, 0] = 0.0
+    c["cache"].k_scale.fill_(1e38)
+    out, lse = F.fuse_attention_cache(c["q"], c["cache"], c["offsets"], c["table"], c["lengths"], scale=100.0)
+    even = dict(c, q=c["q"][:, :1].clone(), cache=c["cache"]._replace(k_scale=torch.ones_like(c["cache"].k_scale)))
+    want = H.cache_attention(even, scale=100.0)
+    R.within(out[:, :1], want[0], want[2], "out")
+    R.within(lse[:, :1], want[1], want[3], "lse")
 
 
 def test_cache_far_places():
