@@ -520,20 +520,17 @@ __global__ void __launch_bounds__(256, ROWS == 16 ? 3 : 2) attention_cache_kerne
     }
 }
 
-// Joins the splits of every row: a wave per row.
-template <typename T>
+// Joins the splits of every row: a wave per row, whichever sequence it is of.  WIDE: a block per row, whose waves take eight splits each in turn (32
+// rows of 48 splits: 10 us by waves, 5 by blocks).
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) attention_cache_join_kernel(const CacheArgs a)
 {
-    const int kvh = blockIdx.x % a.kv_heads;
-    const Work work = tile_at<false>(a, a.tile, blockIdx.x / a.kv_heads);
-    if (!work.any)
+    __shared__ float parts[4][128];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long row = WIDE ? (long long)blockIdx.x : (long long)blockIdx.x * 4 + wave, token = (unsigned)row / (unsigned)a.heads;
+    if (token < offset_at(a.q_off, 0, a.off64) || token >= min(offset_at(a.q_off, a.seqs, a.off64), a.q_tokens))
         return;
-    const Seq &x = work.x;
-    const int lane = threadIdx.x & 63, r = work.first + blockIdx.y * 4 + (threadIdx.x >> 6);
-    if (r >= x.nq * a.group || r >= work.first + a.tile)
-        return;
-    const int place = quotient(a.by_group, r), head = kvh * a.group + r - place * a.group;
-    const long long row = (x.q0 + place) * a.heads + head;
+    const int head = (int)(row - token * a.heads);
     const float *stat = a.parts + a.q_tokens * a.heads * a.splits * a.dim;
     const bool mine = lane < a.splits;
     const float m = mine ? stat[row * a.splits + lane] : -INFINITY, l = mine ? stat[(a.q_tokens * a.heads + row) * a.splits + lane] : 0.0f;
@@ -546,7 +543,7 @@ __global__ void __launch_bounds__(256) attention_cache_join_kernel(const CacheAr
     float o0 = 0.0f, o1 = 0.0f;
     const float *o = a.parts + row * a.splits * a.dim;
     const int d0 = min(lane, a.dim - 1), d1 = min(lane + 64, a.dim - 1);
-    for (int i = 0; i < a.splits; i += 8) {                // eight splits' loads in flight
+    for (int i = WIDE ? wave * 8 : 0; i < a.splits; i += WIDE ? 32 : 8) {          // eight splits' loads in flight
         float v0[8], v1[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -562,8 +559,17 @@ __global__ void __launch_bounds__(256) attention_cache_join_kernel(const CacheAr
                 o1 = fmaf(f, v1[u], o1);
             }
     }
+    if (WIDE) {
+        parts[wave][lane] = o0;
+        parts[wave][lane + 64] = o1;
+        __syncthreads();
+        if (wave > 0)
+            return;
+        o0 = (parts[0][lane] + parts[1][lane]) + (parts[2][lane] + parts[3][lane]);
+        o1 = (parts[0][lane + 64] + parts[1][lane + 64]) + (parts[2][lane + 64] + parts[3][lane + 64]);
+    }
     const float f = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : NAN;
-    T *out = row_of<T>(a.out, x.q0 + place, head);
+    T *out = row_of<T>(a.out, token, head);
     if (lane < a.dim)
         out[lane] = (T)(o0 * f);
     if (lane + 64 < a.dim)
@@ -751,7 +757,11 @@ int launch_read(const CacheArgs &a, unsigned tiles, hipStream_t s)
     int rc = launched("attention_cache_kernel");
     if (rc || a.splits == 1)
         return rc;
-    attention_cache_join_kernel<T><<<dim3(tiles * a.kv_heads, a.tile / 4), 256, 0, s>>>(a);
+    const long long rows = a.q_tokens * a.heads;           // (fewer than 2^31: splits are for few rows)
+    if (a.splits > 8)
+        attention_cache_join_kernel<T, true><<<(unsigned)rows, 256, 0, s>>>(a);
+    else
+        attention_cache_join_kernel<T, false><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(a);
     rc = launched("attention_cache_join_kernel");
     if (!rc)
         set_last_kernel("attention_cache_kernel");

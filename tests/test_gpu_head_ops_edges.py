@@ -301,6 +301,22 @@ def test_cache_scales_far_apart(dtype):
     check_cache_attention(c)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_cache_over_long_histories(dtype):
+    """Up to the most splits that a call takes, joined by waves and by blocks, beside short sequences."""
+    for heads, kv_heads, dim, page, new, lengths in ((8, 2, 128, 64, [1, 1, 1], [9000, 20, 0]), (4, 4, 64, 256, [1], [40000]), (6, 1, 72, 100, [3, 2], [7000, 5000]),
+                                                     (32, 2, 96, 16, [2], [5003])):
+        c = cache_case(66, dtype, heads, kv_heads, dim, page, new, lengths)
+        check_cache_attention(c)
+        check_cache_attention(c, tree=trees(3, new), cap=25.0)
+        first = torch.full_like(c["q"], 7.0)               # rows of no sequence are not joined either
+        off = (c["offsets"] - 1).clamp_min(0) if len(new) == 1 and new[0] > 1 else None
+        if off is not None:
+            want, _ = F.fuse_attention_cache(c["q"][:1].contiguous(), c["cache"], off, c["table"], c["lengths"])
+            got, _ = F.fuse_attention_cache(c["q"], c["cache"], off, c["table"], c["lengths"], out=first)
+            assert torch.equal(got[:1], want) and (got[1:] == 7.0).all()
+
+
 def test_cache_of_keys_beyond_the_scores_range():
     """Scales of keys that no score holds: infinities where they are met, and 0 for a query of zeros."""
     c = cache_case(65, "bf16", 2, 1, 64, 16, [2], [50])
