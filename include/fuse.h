@@ -521,10 +521,12 @@ int fuse_qk_rotary_backward(const fuse_rotary *rotary, const fuse_rotary_grads *
  *   scales : k_scale, v_scale: pages x kv_heads x page_size, unit stride along the places
  *   table  : seqs x table_width int32, table_ld apart: place p of sequence s is place p % page_size of page table[s][p / page_size]
  * Sequence s has the new tokens offsets[s] .. offsets[s + 1] of packed arrays, and with them lengths[s] keys: its new tokens are its last
- * keys.  offsets and lengths are device arrays of int32 or int64, not read on the host; values beyond the arrays are cut down to them.  Pages that
- * do not exist are not written, and the nearest one that exists is read in their place: no access leaves the arrays, whatever the tables say.
+ * keys.  offsets and lengths are device arrays of int32 or int64, not read on the host; offsets beyond the arrays are cut down to them.  Places behind
+ * the last one of the table do not exist: tokens that would be there are not written, and seen by none.  Pages that do not exist are
+ * not written, and the nearest one that exists is read in their place: no access leaves the arrays, whatever the tables say.
  * dim a multiple of 8 up to 128, dtype (of the packed arrays) FUSE_BF16 or FUSE_F16, their rows on 16 bytes, those of the cache on 8 (on 16 with
- * dim a multiple of 16: faster); table_width * page_size < 2^31 - 4096 (FUSE_EUNSUPPORTED otherwise). */
+ * dim a multiple of 16: faster); table_width * page_size < 2^31 - 4096, fewer than some 2^27 tokens
+ * (FUSE_EUNSUPPORTED otherwise). */
 typedef struct {
     int32_t dtype, kv_heads, dim, offsets_are_64;
     int64_t tokens, seqs, pages, page_size;
@@ -550,8 +552,8 @@ int fuse_cache_write(const fuse_cache *cache, const void *k, int64_t k_token_ld,
  * over the keys that a query may see: all of the sequence's, or with `causal` those up to its own place, or with a tree all keys before
  * the new tokens and of these the ones whose bits are set in the query's word: bit b of tree[token] is new token b of its sequence, up to 64 of them
  * (those behind are seen by none).  A query that sees no key gets out = 0 and lse = -inf.  What masked keys and values hold has no influence.
- * Query head h reads key head h / (heads / kv_heads).  S and sums are fp32; exp(S - max) times the value's scale is rounded to dtype before the
- * product with V, for FUSE_F16 multiplied with powers of two first.  Scales must not be negative.  For a single new token per sequence up to a
+ * Query head h reads key head h / (heads / kv_heads).  S and sums are fp32; exp(S - max) times the value's scale is rounded to fp16 before the
+ * product with V, whatever dtype is, multiplied with powers of two first.  Scales must not be negative.  For a single new token per sequence up to a
  * few dozen; rows of no sequence are neither read nor written.
  * Results overlap neither each other nor any input.
  *   fuse_attention_cache_bytes : bytes of the workspace (0 where none is needed, and for a call that is refused). */

@@ -56,7 +56,8 @@ struct CacheArgs {
     Divider by_row;                        // writing: rows of a token
 };
 
-// Sequence s: its new tokens, and its keys, the last of which are those of the new tokens.
+// Sequence s: its new tokens, and its keys that have a place; k0 is that of the first new token (also where that is before the first place, or
+// behind the last one that the table has).
 __device__ __forceinline__ Seq seq_at(const CacheArgs &a, int s)
 {
     Seq x;
@@ -64,8 +65,9 @@ __device__ __forceinline__ Seq seq_at(const CacheArgs &a, int s)
     const long long room = (long long)a.pages.width * a.pages.size.d;      // (below 2^31 - 4096, which the host checks)
     x.q0 = min(max(q0, 0LL), a.q_tokens);
     x.nq = (int)(min(max(q1, x.q0), a.q_tokens) - x.q0);
-    x.k0 = 0;
-    x.nk = (int)min(max(offset_at(a.lengths, s, a.off64), 0LL), room);
+    const long long keys = min(max(offset_at(a.lengths, s, a.off64), 0LL), (1LL << 31) - 4096);
+    x.k0 = keys - x.nq;
+    x.nk = (int)min(keys, room);
     return x;
 }
 
@@ -96,11 +98,11 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const CacheArgs a)
         int head[kAtOnce], page[kAtOnce], within[kAtOnce];                 // page -1: no such place
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            const int r = r0 + u * 16, t = quotient(a.by_row, r), place = w.first + t + w.x.nk - w.x.nq;
+            const int r = r0 + u * 16, t = quotient(a.by_row, r), place = (int)w.x.k0 + w.first + t;
             head[u] = (r - t * 2 * a.kv_heads) >> 1;
             page[u] = -1;
             x8[u] = t8{};
-            if (r < rows && place >= 0) {
+            if (r < rows && place >= 0 && place < w.x.nk) {
                 const int n = quotient(g.size, place);
                 page[u] = g.table[w.seq * g.table_ld + n];
                 within[u] = place - n * (int)g.size.d;
@@ -245,9 +247,9 @@ __global__ void __launch_bounds__(256, ROWS == 16 ? 3 : 2) attention_cache_kerne
     const Seq &x = work.x;
     const int first = work.first, rows = x.nq * a.group;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
-    const int before = x.nk - x.nq;                        // keys that are there already
+    const int before = (int)x.k0;                          // keys that are there already
     auto seen_by = [&](int place) { return a.causal && !a.tree ? min(max(place + before + 1, 0), x.nk) : x.nk; };
-    const int seen_lo = a.tree ? max(before, 0) : seen_by(quotient(a.by_group, first));
+    const int seen_lo = a.tree ? min(max(before, 0), x.nk) : seen_by(quotient(a.by_group, first));
 
     int begin = 0, end = seen_by(quotient(a.by_group, min(first + ROWS, rows) - 1));
     if (a.splits > 1) {
@@ -330,7 +332,7 @@ __global__ void __launch_bounds__(256, ROWS == 16 ? 3 : 2) attention_cache_kerne
             kscale[row] = sc * c > 0x1.fffffep127f ? 0x1.fffffep127f : sc * c;     // (a score of 0 stays one; NaN stays NaN)
         } else {
             vscale[row] = sc;
-            vlog[row] = __builtin_amdgcn_logf(fmaxf(sc, 0x1p-90f));
+            vlog[row] = __builtin_amdgcn_logf(fmaxf(sc, 0x1p-90f));        // (so that sums of weights stay within fp32's range)
         }
         if (loads)
 #pragma unroll
@@ -668,11 +670,13 @@ int write_impl(const fuse_cache *f, const void *k, int64_t k_token_ld, int64_t k
     a.k = {const_cast<void *>(k), k_token_ld, k_head_ld};
     a.v = {const_cast<void *>(v), v_token_ld, v_head_ld};
     a.by_row = divider(2 * (unsigned)f->kv_heads);
-    const unsigned blocks = (unsigned)first_tile(f->tokens, (int)f->seqs, kWriteTokens);
+    const long long blocks = first_tile(f->tokens, (int)f->seqs, kWriteTokens);
+    if (blocks >= 1 << 24)
+        return report(FUSE_EUNSUPPORTED, "more tokens and sequences than one launch has blocks");
     if (f->dtype == FUSE_BF16)
-        cache_write_kernel<__bf16><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
+        cache_write_kernel<__bf16><<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(a);
     else
-        cache_write_kernel<_Float16><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
+        cache_write_kernel<_Float16><<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(a);
     return launched("cache_write_kernel");
 }
 
@@ -714,8 +718,9 @@ int check_read(const fuse_cache *f, const fuse_cache_query *q)
 // Splits of the keys: as many as it takes to have three blocks for each of 256 compute units, of at least four steps of all waves each where
 // all sequences fill their room, or eight blocks of at least eight steps.  A split costs a block's beginning and end, some five steps, and the
 // launch that joins them.  32 heads over 8, dim 128: 32 tokens over 16384 places each (filled to two thirds, as below) take 226, 162, 155 and 148
-// us with 512, 768, 1024 and 2048 blocks for a goal; 16 over 2048: 22, 21, 21, 21; four times 40 over 4096: 34, 33, 34, 40; one over
-// 32768: 22 us with splits of four steps, 20 with eight; one of 8 heads over 700: 9 us with two splits, 7 without.
+// us with 512, 768, 1024 and 2048 blocks for a goal; four times 40 over 4096: 34, 33, 34, 40; 16 over 2048: 24 us with splits of eight steps alone,
+// 21 so; 8 heads of dim 64, 16 over 4096: 20 us with 768 blocks for the second goal, 18 with 1536, which take four times 40 over 4096 from 32 to 40;
+// one of 8 heads over 700: 9 us with splits of two steps, 7 without a split.
 int splits_of(const fuse_cache *f, const fuse_cache_query *q)
 {
     const long long blocks = std::max(1LL, tiles_of(f, q) * f->kv_heads), room = f->table_width * f->page_size, step = kKeys * kWaves;

@@ -227,7 +227,7 @@ def fuse_cache_write(k, v, cache, offsets, page_table, lengths, stream=None):
 
     k, v: (tokens, key heads, dim), bfloat16 or float16; parts of one projection can be passed as they are.  offsets: the sequences' first new tokens
     and the end of the last one; lengths: their keys, the new ones among them (the last ones): a new token goes to the place of its key.
-    page_table: (sequences, pages) int32, the pages of every sequence in order."""
+    page_table: (sequences, pages) int32, the pages of every sequence in order; tokens that it has no place for are not written."""
     if k.dim() != 3:
         raise ValueError("k must be (tokens, heads, dim)")
     f, kv_heads = _cache(cache, k, offsets, page_table, lengths)

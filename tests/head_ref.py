@@ -174,11 +174,12 @@ def cache_attention(c, causal=True, scale=None, cap=None, slopes=None, tree=None
     for s, length in enumerate(c["lengths"].tolist()):
         rows = slice(offsets[s], offsets[s + 1])
         nq, nk = rows.stop - rows.start, min(max(length, 0), room)
-        place = torch.arange(nq) + nk - nq
+        first = max(length, 0) - nq                        # (also where the table has no room for it)
+        place = torch.arange(nq) + first
         j = torch.arange(nk)
         meet = (j[None] <= place[:, None]) if causal else torch.ones(nq, nk, dtype=torch.bool)
         if tree is not None:
-            b = j - (nk - nq)
+            b = j - first
             bits = tree.cpu()[rows]
             meet = (b < 0)[None] | ((b >= 0) & (b < 64))[None] & ((bits[:, None] >> b.clamp(0, 63)[None]) & 1).bool()
         for g in range(hk):

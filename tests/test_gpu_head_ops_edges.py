@@ -183,7 +183,7 @@ def test_cache_tables_that_say_too_much():
     c["table"][0, 2], c["table"][1, 1] = -1, 1000000
     check_write(c)
     check_cache_attention(c)                               # (the reference reads the nearest page that exists, too)
-    c["lengths"][0] = 1 << 30                              # cut down to the room of the table
+    c["lengths"][0] = 1 << 30                              # all places of the table, and none of the new tokens
     check_cache_attention(c)
     c["lengths"][1] = -5
     out, lse = F.fuse_attention_cache(c["q"], c["cache"], c["offsets"], c["table"], c["lengths"])
@@ -204,6 +204,19 @@ def test_cache_tables_that_say_too_much():
     for q in (c["q"], c["q"][:0]):
         F.fuse_cache_write(q[:, :2], q[:, 2:], c["cache"], none, c["table"][:0], none[:0])
         assert F.fuse_attention_cache(q, c["cache"], none, c["table"][:0], none[:0])[0].shape == q.shape
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_cache_of_sequences_that_outgrow_their_tables(dtype):
+    """New tokens behind the table's last place are dropped, not written over older ones; the others stay where they belong."""
+    c = cache_case(58, dtype, 6, 2, 64, 16, [5, 1, 20, 3], [40, 33, 45, 20])
+    room = c["table"].shape[1] * 16                        # 48
+    c["lengths"][:3] = torch.tensor([room + 2, room + 1, 5000], dtype=torch.int32)
+    check_write(c)
+    check_cache_attention(c)
+    check_cache_attention(c, causal=False)
+    check_cache_attention(c, slopes=torch.tensor([0.5, 0.25, 0.1, 0.0, 1.0, 0.01], device="cuda"))
+    check_cache_attention(c, tree=torch.tensor([(2 << (i % 20)) - 1 for i in range(29)], device="cuda"))
 
 
 def test_cache_rows_of_no_sequence():

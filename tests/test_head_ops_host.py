@@ -167,6 +167,7 @@ def test_attention_cache_refuses(kw, code, word):
 def test_cache_refuses_rows_and_results():
     lib, f, q = L.load(), cache(), query()
     refused(lib.fuse_cache_write(None, FAR, 512, 128, FAR, 512, 128, None), EINVAL, "cache")
+    refused(lib.fuse_cache_write(ctypes.byref(cache(tokens=1 << 28)), FAR, 512, 128, FAR, 512, 128, None), EUNSUPPORTED, "blocks")
     refused(lib.fuse_cache_write(ctypes.byref(f), None, 512, 128, FAR, 512, 128, None), EINVAL, "k")
     refused(lib.fuse_cache_write(ctypes.byref(f), FAR, 512, 128, FAR, 512, 32, None), ESHAPE, "v")
     refused(lib.fuse_cache_write(ctypes.byref(f), FAR, 512, 128, FAR + 2, 512, 128, None), EUNSUPPORTED, "v")
