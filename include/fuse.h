@@ -459,9 +459,10 @@ int fuse_attention_zero_rest(const fuse_attn *attn, const fuse_attn_grads *grads
  *     slopes, in places among the keys (query i stands at key i + keys - queries)
  * and with prefix_lengths, which goes with causal: all queries of sequence s see its first prefix_lengths[s] keys, beside those up to their own.
  * All else is as in fuse_attention and its gradient: results, workspaces (fuse_attention_bytes; the gradients' have a call of their own),
- * limits.  A shape that is NULL or has nothing set is fuse_attention itself.  Slopes are constants: they get no gradient. */
+ * limits.  Capped scores are off by some 2^-22 of the cap.  A shape that is NULL or has nothing set is fuse_attention itself.  Slopes are constants:
+ * they get no gradient. */
 typedef struct {
-    double cap;                             /* 0: none, else 1e-3 to 1e6 */
+    double cap;                             /* 0: none, else 1e-3 to 1e4 */
     const float *slopes;                    /* heads values on the device, or NULL */
     const void *prefix_lengths;             /* seqs values of the offsets' type on the device, or NULL */
 } fuse_attn_shape;
@@ -561,7 +562,7 @@ typedef struct {
     const void *q;
     int64_t q_token_ld, q_head_ld;
     int32_t heads, causal;
-    double scale, cap;                      /* scale > 0; cap: 0 for none, else 1e-3 to 1e6 */
+    double scale, cap;                      /* scale > 0; cap: 0 for none, else 1e-3 to 1e4 */
     const float *slopes;                    /* heads values, or NULL */
     const int64_t *tree;                    /* tokens values, or NULL; goes with causal, and without slopes */
 } fuse_cache_query;

@@ -136,8 +136,8 @@ int check_shape(const fuse_attn *f, const fuse_attn_shape *shape)
 {
     if (!shape)
         return FUSE_OK;
-    if (shape->cap != 0.0 && (!(shape->cap >= 1e-3) || !(shape->cap <= 1e6)))
-        return report(FUSE_EINVAL, "cap must be 0 (none) or lie between 1e-3 and 1e6");
+    if (shape->cap != 0.0 && (!(shape->cap >= 1e-3) || !(shape->cap <= 1e4)))
+        return report(FUSE_EINVAL, "cap must be 0 (none) or lie between 1e-3 and 1e4 (capped scores are off by some 2^-22 of it)");
     if (reinterpret_cast<uintptr_t>(shape->slopes) % 4 || reinterpret_cast<uintptr_t>(shape->prefix_lengths) % (f->offsets_are_64 ? 8 : 4))
         return report(FUSE_EINVAL, "slopes or prefix_lengths are not aligned to their type");
     if (shape->prefix_lengths && !f->causal)

@@ -704,8 +704,8 @@ int check_read(const fuse_cache *f, const fuse_cache_query *q)
         return report(FUSE_ESHAPE, "heads is no multiple of kv_heads");
     if (!(q->scale >= 1e-30) || !(q->scale <= 1e30))
         return report(FUSE_EINVAL, "scale must lie between 1e-30 and 1e30");
-    if (q->cap != 0.0 && (!(q->cap >= 1e-3) || !(q->cap <= 1e6)))
-        return report(FUSE_EINVAL, "cap must be 0 (none) or lie between 1e-3 and 1e6");
+    if (q->cap != 0.0 && (!(q->cap >= 1e-3) || !(q->cap <= 1e4)))
+        return report(FUSE_EINVAL, "cap must be 0 (none) or lie between 1e-3 and 1e4 (capped scores are off by some 2^-22 of it)");
     if (q->tree && (!q->causal || q->slopes))
         return report(FUSE_EINVAL, "a tree goes with causal, and without slopes");
     if (reinterpret_cast<uintptr_t>(q->slopes) % 4 || reinterpret_cast<uintptr_t>(q->tree) % 8)

@@ -186,7 +186,7 @@ def test_cache_refuses_rows_and_results():
 
 # ------------------------------------------------------------- attention with shaped scores ---
 
-SHAPE_REFUSALS = [(dict(cap=-2.0), EINVAL, "cap"), (dict(cap=1e-4), EINVAL, "cap"), (dict(cap=1e7), EINVAL, "cap"), (dict(cap=float("nan")), EINVAL, "cap"),
+SHAPE_REFUSALS = [(dict(cap=-2.0), EINVAL, "cap"), (dict(cap=1e-4), EINVAL, "cap"), (dict(cap=1.1e4), EINVAL, "cap"), (dict(cap=float("nan")), EINVAL, "cap"),
                   (dict(slopes=FAR + 1), EINVAL, "aligned"), (dict(prefix_lengths=FAR + 2), EINVAL, "aligned")]
 
 
