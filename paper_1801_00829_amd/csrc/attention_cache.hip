@@ -716,15 +716,17 @@ int check_read(const fuse_cache *f, const fuse_cache_query *q)
 }
 
 // Splits of the keys: as many as it takes to have three blocks for each of 256 compute units, of at least four steps of all waves each where
-// all sequences fill their room, or eight blocks of at least eight steps.  A split costs a block's beginning and end, some five steps, and the
+// all sequences fill their room (six blocks for 16 rows of dim 64, of which four fit at a time), or eight blocks of at least eight steps.  A split costs a block's beginning and end, some five steps, and the
 // launch that joins them.  32 heads over 8, dim 128: 32 tokens over 16384 places each (filled to two thirds, as below) take 226, 162, 155 and 148
 // us with 512, 768, 1024 and 2048 blocks for a goal; four times 40 over 4096: 34, 33, 34, 40; 16 over 2048: 24 us with splits of eight steps alone,
-// 21 so; 8 heads of dim 64, 16 over 4096: 20 us with 768 blocks for the second goal, 18 with 1536, which take four times 40 over 4096 from 32 to 40;
-// one of 8 heads over 700: 9 us with splits of two steps, 7 without a split.
+// 21 so; one of 8 heads over 700: 9 us with splits of two steps, 7 without a split.  Dim 64, 768 and 1536 blocks for the goal of four steps: 16 tokens of 8
+// heads over 4096 take 21 and 18 us, 60 of 14 over 2 over 3000: 20 and 19, 48 of 4 over 1 over 22826: 30 and 30; of dim 80, 8 of 64 over 8
+// over 8192: 24 and 27.
 int splits_of(const fuse_cache *f, const fuse_cache_query *q)
 {
     const long long blocks = std::max(1LL, tiles_of(f, q) * f->kv_heads), room = f->table_width * f->page_size, step = kKeys * kWaves;
-    const long long n = std::max(std::min(2048 / blocks, room / (8 * step)), std::min(768 / blocks, room / (4 * step)));
+    const long long goal = f->dim <= 64 && tile_of(f, q) == 16 ? 1536 : 768;
+    const long long n = std::max(std::min(2048 / blocks, room / (8 * step)), std::min(goal / blocks, room / (4 * step)));
     return (int)std::max(1LL, std::min<long long>(n, kMaxSplits));
 }
 
