@@ -53,13 +53,18 @@ __global__ void __launch_bounds__(256) attention_rest_kernel(const AttnArgs a)
 // they are not equally long), of at least three steps each where all sequences are equally long and half of the pairs are masked.  Whole
 // backward passes, without splits and with them: 2048 tokens, 32 heads over 1, dim 128: 1639 and 200 us; two sequences of 2048, 32 over 4: 499 and
 // 308 us (with 512 blocks for a goal 499, with 1536 313); 4000 tokens, 32 over 8: 255 and 227 us; 256 tokens, 8 over 8: 22 us either way.
-int key_splits(const fuse_attn *f)
+// With a prefix there may be no masked pairs: up to half as many blocks, of three steps of all rows.  Without and with this: 308 tokens of a sequence
+// under a prefix, 6 heads over 2, dim 128, 55 and 45 us; 2353 in 16 sequences, 8 over 1, 62 and 53; 5863 in seven, 3 over 1, whose blocks are enough
+// already, 131 (148 with such steps up to the whole goal).
+int key_splits(const fuse_attn *f, const fuse_attn_shape *shape)
 {
     if (f->seqs == 0)
         return 1;
     const long long blocks = first_tile(f->k_tokens, (int)f->seqs, kKeys) * f->kv_heads;
-    const long long steps = f->q_tokens * (f->heads / f->kv_heads) / f->seqs / kStep / 2;
-    const long long n = std::min(1280 / blocks, steps / 3);
+    const long long steps = f->q_tokens * (f->heads / f->kv_heads) / f->seqs / kStep;
+    long long n = std::min(1280 / blocks, steps / 2 / 3);
+    if (shape && shape->prefix_lengths)
+        n = std::max(n, std::min(640 / blocks, steps / 3));
     return (int)(n < 1 ? 1 : n > 32 ? 32 : n);
 }
 
@@ -72,7 +77,7 @@ size_t lift_ints(const fuse_attn *f)
 }
 size_t backward_bytes(const fuse_attn *f, const fuse_attn_shape *shape)
 {
-    const int splits = key_splits(f);
+    const int splits = key_splits(f, shape);
     return (stat_floats(f) * (shape_of(shape) & kSloped ? 4 : 2) + lift_ints(f) + (splits > 1 ? (size_t)f->k_tokens * f->kv_heads * splits * 2 * f->dim : 0)) * sizeof(float);
 }
 
@@ -152,7 +157,7 @@ int backward_impl(const fuse_attn *f, const fuse_attn_shape *shape, const fuse_a
         a.row_slope = a.parts + stat_floats(f);
         a.parts += 2 * stat_floats(f);
     }
-    a.splits = key_splits(f);
+    a.splits = key_splits(f, shape);
     return f->dtype == FUSE_BF16 ? launch_shape<__bf16>(shape_of(shape), a, (hipStream_t)stream)
                                  : launch_shape<_Float16>(shape_of(shape), a, (hipStream_t)stream);
 }
