@@ -345,6 +345,10 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
                     dp = product<T>(read_row(gt + half * 32 * L::kRowBytes, row_at[i]), v[i], dp);
                 }
                 ahead<L::kSteps * 2, 6>();
+                // fp16's lift goes into the loops that make dS: as a loop of its own it takes the kernels of 64 dims without slopes from 163 to 170
+                // registers, and so from three waves per SIMD to two.  Whole backward passes with three and two: 1542 tokens, 8 heads over
+                // 4, dim 64: 66 and 70 us; 4117 in four sequences, 32 over 16, dim 32: 100 and 109; 7183 in four, 32 over 8, dim 64, whose blocks fill two
+                // rounds of two waves: 287 and 280.
                 float w[16], ds[16];
                 if (kScored<SHAPE>) {
                     // With slopes all that is kept of the rows is asked for only here: there are no registers to keep it in meanwhile.  Whole backward
@@ -368,18 +372,18 @@ __global__ void __launch_bounds__(256, 2) attention_key_grad_kernel(const AttnAr
                             far = (float)(places[i / 4][i % 4] - key), slope = slopes[i / 4][i % 4];
                         w[i] = __builtin_amdgcn_exp2f(scores.of(p[i], -lse[i / 4][i % 4], far, slope, d));
                         ds[i] = w[i] * ((dp[i] - delta[i / 4][i % 4]) * d);
+                        if (kLifted<T>)
+                            ds[i] *= lift_ds;
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         w[i] = __builtin_amdgcn_exp2f(fmaf(p[i], c, -lse[i / 4][i % 4]));
                         ds[i] = w[i] * (dp[i] - delta[i / 4][i % 4]);
+                        if (kLifted<T>)
+                            ds[i] *= lift_ds;
                     }
                 }
-                if (kLifted<T>)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        ds[i] *= lift_ds;
                 if (r0 + half * 32 < from_hi || r0 + half * 32 + 32 > rows) {
                     const int skip = from - r0 - half * 32 - 4 * h, left = rows - r0 - half * 32 - 4 * h;
 #pragma unroll
