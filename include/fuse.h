@@ -554,8 +554,10 @@ int fuse_cache_write(const fuse_cache *cache, const void *k, int64_t k_token_ld,
  * the new tokens and of these the ones whose bits are set in the query's word: bit b of tree[token] is new token b of its sequence, up to 64 of them
  * (those behind are seen by none).  A query that sees no key gets out = 0 and lse = -inf.  What masked keys and values hold has no influence.
  * Query head h reads key head h / (heads / kv_heads).  S and sums are fp32; exp(S - max) times the value's scale is rounded to fp16 before the
- * product with V, whatever dtype is, multiplied with powers of two first.  Scales must not be negative.  For a single new token per sequence up to a
- * few dozen; rows of no sequence are neither read nor written.
+ * product with V, whatever dtype is, multiplied with powers of two first.  Scales must not be negative.  A scale of a value that is
+ * infinite or no number leaves nothing finite in out for the rows that see it; their lse, and other rows, are as without it.  Beside a scale
+ * of a value s above 2^90, weights below s * 2^-137 of its own are lost.  For a single new token per sequence up to a few dozen; rows of no
+ * sequence are neither read nor written.
  * Results overlap neither each other nor any input.
  *   fuse_attention_cache_bytes : bytes of the workspace (0 where none is needed, and for a call that is refused). */
 typedef struct {

@@ -332,7 +332,9 @@ __global__ void __launch_bounds__(256, ROWS == 16 ? 3 : 2) attention_cache_kerne
             kscale[row] = sc * c > 0x1.fffffep127f ? 0x1.fffffep127f : sc * c;     // (a score of 0 stays one; NaN stays NaN)
         } else {
             vscale[row] = sc;
-            vlog[row] = __builtin_amdgcn_logf(fmaxf(sc, 0x1p-90f));        // (so that sums of weights stay within fp32's range)
+            // (at least 2^-90, so that sums of weights stay within fp32's range; a scale that is not finite is no measure of the others: with an
+            // infinite one as the maximum all weights, and their sum, would be 0)
+            vlog[row] = __builtin_amdgcn_logf(sc < INFINITY ? fmaxf(sc, 0x1p-90f) : 0x1p-90f);
         }
         if (loads)
 #pragma unroll
