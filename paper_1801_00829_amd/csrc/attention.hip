@@ -183,9 +183,7 @@ extern "C" {
 
 size_t fuse_attention_bytes(const fuse_attn *attn)
 {
-    if (fuse::check_attn(attn))
-        return 0;
-    return parts_floats(attn, splits_of(attn)) * sizeof(float);
+    return fuse::guard_bytes([&] { return fuse::check_attn(attn) ? 0 : parts_floats(attn, splits_of(attn)) * sizeof(float); });
 }
 
 int fuse_attention(const fuse_attn *attn, void *out, int64_t out_token_ld, int64_t out_head_ld, float *lse, void *workspace,

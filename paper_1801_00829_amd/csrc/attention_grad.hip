@@ -168,7 +168,7 @@ extern "C" {
 
 size_t fuse_attention_backward_bytes(const fuse_attn *attn)
 {
-    return fuse::check_attn(attn) || attn->q_tokens == 0 ? 0 : backward_bytes(attn, nullptr);
+    return fuse::guard_bytes([&] { return fuse::check_attn(attn) || attn->q_tokens == 0 ? 0 : backward_bytes(attn, nullptr); });
 }
 
 size_t fuse_attention_shaped_backward_bytes(const fuse_attn *attn, const fuse_attn_shape *shape)

@@ -3,8 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
-#include <exception>
-#include <new>
 #include <string>
 
 #include "../../include/fuse.h"
@@ -41,10 +39,8 @@ int guard(F f)
 {
     try {
         return f();
-    } catch (const std::bad_alloc &) {
-        return report(FUSE_ENOMEM, "out of host memory");
-    } catch (const std::exception &ex) {
-        return report(FUSE_ERUNTIME, std::string("internal error: ") + ex.what());
+    } catch (...) {
+        return report_exception();
     }
 }
 

@@ -1911,10 +1911,8 @@ int guarded(F f)
 {
     try {
         return f();
-    } catch (const std::bad_alloc &) {
-        return fail(FUSE_ENOMEM, "out of host memory");
-    } catch (const std::exception &ex) {
-        return fail(FUSE_ERUNTIME, std::string("internal error: ") + ex.what());
+    } catch (...) {
+        return fuse::report_exception();
     }
 }
 
@@ -1923,6 +1921,22 @@ int guarded(F f)
 namespace fuse {
 
 int report(int code, const std::string &message) { return fail(code, message); }
+
+int report_exception() noexcept
+{
+    try {
+        throw;
+    } catch (const std::bad_alloc &) {
+    } catch (const std::exception &ex) {
+        try {
+            return fail(FUSE_ERUNTIME, std::string("internal error: ") + ex.what());
+        } catch (...) {                    // no room for the text
+        }
+    } catch (...) {
+        return fail(FUSE_ERUNTIME, "internal error");
+    }
+    return fail(FUSE_ENOMEM, "out of memory");     // (both texts are short enough for a string to hold without an allocation)
+}
 
 void set_last_kernel(const char *name) { g_last_kernel = name; }
 

@@ -140,6 +140,8 @@ long long transpose_row_grain(long long m, long long n, long long nnz);
 
 // The calling thread's fuse_last_error() / fuse_last_kernel() (libfuse.cpp); report returns its code.
 int report(int code, const std::string &message);
+// Within a handler at the C boundary: reports what was thrown and returns the code for it.  Throws nothing itself, out of memory or not.
+int report_exception() noexcept;
 void set_last_kernel(const char *name);
 
 int iota_launch(double *dst, long long n, hipStream_t stream);     // dst[i] = (double)i
