@@ -227,7 +227,9 @@ __global__ void __launch_bounds__(256, 2) attention_query_grad_kernel(const Attn
 // Two waves share 32 keys, as columns.  Each takes half of a step's rows for S, dP, P and dS, the two exchange P and dS through LDS, and
 // each adds all rows' products to half of the dims of dV and dK.  That is the same work as a wave for itself, but 64 registers of sums
 // instead of 128: with those, next to 64 of keys and values, nothing is left to load operands ahead of the products.  For a dim of 128 all 256
-// registers are taken and 16 to 20 bytes per lane are in scratch memory.
+// registers are taken, and bytes per lane in scratch memory (EVEN and not): plain scores and a prefix 20 and 16, a cap 28 and 20 (fp16 44 and 20),
+// slopes 40 and 12 (68 and 32), both 88 and 48 (88 and 52); the queries' kernel has 12 with a cap in fp16, and none else.  Dims up to 64 take 155 to 164
+// registers, three waves per SIMD, and with slopes 186 to 200, two.
 //
 // EVEN: the rows of one pass of a tile's loads are whole tokens (the group divides their number), so they lie the same distance from
 // the next pass's and their addresses are scalars with 32 bit offsets per lane: 481 against 521 us for a group of four.  Else, and where

@@ -218,6 +218,8 @@ __device__ __forceinline__ float column_sum(float v) { return swapped_sum<32>(sw
 // TB/s, 5.2 in the kernel; a large copy reaches 4.9); vector units are busy for a quarter of the time, matrix units for 7 %.  With products
 // of 32 columns, whose sums and queries take twice the registers (two waves per SIMD instead of three), 157 us; with two steps loaded
 // ahead 158 at two waves, at three they do not fit.  A small call's 7 to 12 us are the waits from one lookup to the next: sequence, page, keys.
+// Where a sequence has many rows every 32 of them load and widen its keys anew: 2048 new tokens over 16384 places, 32 heads over 8, dim 128, take 985
+// us (0.52 PFLOP/s).
 //
 // All products are taken with the kept side as columns: S = K t(Q) leaves a lane the scores of keys 4 g .. and 16 + 4 g .. of its column, which,
 // as weights, are the B operand of the next product as they lie; its A is the transposed tile of values, read in that order.
@@ -718,12 +720,16 @@ int check_read(const fuse_cache *f, const fuse_cache_query *q)
 }
 
 // Splits of the keys: as many as it takes to have three blocks for each of 256 compute units, of at least four steps of all waves each where
-// all sequences fill their room (six blocks for 16 rows of dim 64, of which four fit at a time), or eight blocks of at least eight steps.  A split costs a block's beginning and end, some five steps, and the
-// launch that joins them.  32 heads over 8, dim 128: 32 tokens over 16384 places each (filled to two thirds, as below) take 226, 162, 155 and 148
-// us with 512, 768, 1024 and 2048 blocks for a goal; four times 40 over 4096: 34, 33, 34, 40; 16 over 2048: 24 us with splits of eight steps alone,
-// 21 so; one of 8 heads over 700: 9 us with splits of two steps, 7 without a split.  Dim 64, 768 and 1536 blocks for the goal of four steps: 16 tokens of 8
-// heads over 4096 take 21 and 18 us, 60 of 14 over 2 over 3000: 20 and 19, 48 of 4 over 1 over 22826: 30 and 30; of dim 80, 8 of 64 over 8
-// over 8192: 24 and 27.
+// all sequences fill their room (six blocks for 16 rows of dim 64, of which four fit at a time), or eight blocks of at least eight steps.  A split costs a
+// block's beginning and end, some five steps, and the launch that joins them.  Calls from Python, one after the other:
+//   eight steps, a goal of 512, 1024, 2048 and 4096 blocks: 32 tokens of 32 heads over 8, dim 128, over 16384 places each, filled to two thirds, take
+//     151, 140, 143 and 149 us; 4 over 8192 places 21 with each;
+//   four steps, a goal of 512, 768 and 1536: 16 tokens of these heads over 2048: 22.3, 21.6 and 21.7 us; 36 of 4 over 1 over 12168, filled to two thirds: 23.4,
+//     22.8, 25.3; 8 of 64 over 8 of dim 80 over 8192: 25.1, 25.0, 29.4;
+//   dim 64, four steps, 768 and 1536: 16 tokens of 8 heads over 4096: 21.6 and 20.5 us, of 16 over 8 22.2 and 21.2; 60 of 14 over 2 over 3000: 19.5 and 19.6; but
+//     48 of 4 over 1 over 22826: 34.1 and 37.7.
+// The room is the table's width; lengths are the device's.  Short sequences under wide tables have splits without keys, each of which ends, and is
+// joined, like any other: 300 keys of a token of 32 heads over 8 take 11.7 us in a table of 320 places and 15.4 in one of 32768; 32 such tokens 11.4 and 18.9.
 int splits_of(const fuse_cache *f, const fuse_cache_query *q)
 {
     const long long blocks = std::max(1LL, tiles_of(f, q) * f->kv_heads), room = f->table_width * f->page_size, step = kKeys * kWaves;
